@@ -15,6 +15,9 @@
  *                       quest_select_decode the last two; quest_decode_step
  *                       is the whole step in one call)
  *
+ * and what comes before and beside it, many tokens at a time: quest_append_tokens,
+ * quest_prompt_attention, quest_tree_attention.
+ *
  * Conventions for every entry point
  *   - All data pointers are DEVICE pointers owned by the caller.  The library
  *     never allocates or frees device memory and keeps no state between calls
@@ -299,6 +302,67 @@ int quest_decode_step_static(const quest_cache* cache, const void* k_new, const 
                              int32_t k_pool_write, const void* q, int32_t k_pages,
                              float sm_scale, float* scores, int32_t* topk_idx, int32_t* k_eff,
                              void* out, int32_t out_is_fp16, float* lse, void* stream);
+
+/* ---- Many tokens a sequence: prompts, parts of prompts, drafted tokens ----
+ *
+ * Tokens come packed: rows [cu_tokens[b], cu_tokens[b+1]) of the packed arrays belong to
+ * sequence b (n_b of them, 0 allowed).  cu_tokens (device, int32 [batch + 1], trusted) starts at 0
+ * and does not fall; cu_tokens[batch] <= total_tokens, which is all that the host has to
+ * know: rows from cu_tokens[batch] on are neither read nor written, so a captured graph can
+ * serve any lengths up to total_tokens.  q_stride and new_stride are the elements between
+ * two tokens of q and of k_new / v_new (the heads of a token lie next to each other: q
+ * [rows][num_heads][head_dim], k_new and v_new [rows][KV heads][head_dim]); a
+ * fused projection's parts can be passed as they lie.  Data and strides lie on 16 bytes,
+ * else QUEST_ERR_SHAPE.  total_tokens == 0 is no work.  Grouped-query attention as above.
+ *
+ *     prompt, or its next part :  quest_append_tokens -> quest_prompt_attention
+ *     drafted tokens           :  quest_tree_attention, then quest_append_tokens of the accepted ones
+ */
+
+/* Insertion of many tokens (Algorithm 1, first half, for all of them).  seq_lens[b] already counts
+ * sequence b's n_b new tokens; token i goes to position seq_lens[b] - n_b + i: its key and
+ * value into k_pool / v_pool, its key into the metadata of its page, as n_b calls of
+ * quest_append_meta with k_pool_write would leave them, bit for bit.  Token i of sequence b is row
+ * cu_tokens[b] + i of k_new / v_new, or, with rows (nullable, device int32, total_tokens entries,
+ * trusted), row rows[cu_tokens[b] + i]: the accepted ones among drafted tokens. */
+int quest_append_tokens(const quest_cache* cache, const void* k_new, const void* v_new, int64_t new_stride,
+                        const int32_t* rows, const int32_t* cu_tokens, int32_t total_tokens, void* stream);
+
+/* Bytes of device workspace for quest_prompt_attention and quest_tree_attention on this cache
+ * with at most total_tokens packed tokens (it grows and falls with total_tokens; 0: none is used).
+ * Pure host function.  The workspace holds partial results of calls that walk the
+ * tokens in several splits.  It need not be initialised and keeps nothing between calls; calls that
+ * share a workspace must not overlap in time.  A smaller workspace, or NULL, is accepted: fewer splits,
+ * slower, results equal within rounding. */
+int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens, size_t* out_bytes);
+
+/* Causal attention of packed queries over the cache: the last n_b of the seq_lens[b] cached tokens
+ * of sequence b are the ones whose queries are given, so query i stands at position
+ * p = seq_lens[b] - n_b + i (a whole prompt: n_b == seq_lens[b]) and
+ *   out[row][h][:] = sum_{j <= p} softmax_j(sm_scale * q.k_j) * v_j,
+ *   lse[row][h]    = log sum_{j <= p} exp(sm_scale * q.k_j)            (nullable),
+ * out [total_tokens][num_heads][head_dim] and lse [total_tokens][num_heads] dense.  fp32 logits, softmax and
+ * sums; out is fp32 or fp16 as in quest_sparse_decode.  With fp16 out the softmax weights are
+ * rounded to fp16 before they meet the values, with fp32 out they keep 22 bits.
+ * Results must not overlap what the call reads. */
+int quest_prompt_attention(const quest_cache* cache, const void* q, int64_t q_stride, const int32_t* cu_tokens,
+                           int32_t total_tokens, float sm_scale, void* out, int32_t out_is_fp16, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of drafted tokens, which are not in the cache: node i of sequence b attends to all
+ * seq_lens[b] cached tokens (0 is allowed here) and to those drafted nodes j of its own sequence whose
+ * bit is set in its mask: bit j % 64 of tree_mask[row][j / 64] (device, [total_tokens][mask_words], n_b <= 64 *
+ * mask_words; bits from n_b on are ignored).  A tree sets the bits of a node's ancestors and its
+ * own; any mask will do.  Keys and values of the nodes are rows of k_new and v_new: cache and
+ * metadata are not touched, so that rejected nodes leave no trace; quest_append_tokens
+ * puts the accepted ones in.  A node that attends to nothing gets out 0 and lse -infinity.
+ * topk_idx (nullable): [batch][KV heads][k_pages] as in quest_sparse_decode: of the cache only the listed pages'
+ * tokens, for all nodes of the sequence (the drafted nodes as before).
+ * out, lse, their rounding and the workspace as in quest_prompt_attention. */
+int quest_tree_attention(const quest_cache* cache, const void* q, int64_t q_stride, const void* k_new, const void* v_new,
+                         int64_t new_stride, const int32_t* cu_tokens, int32_t total_tokens, const int64_t* tree_mask,
+                         int32_t mask_words, const int32_t* topk_idx, int32_t k_pages, float sm_scale, void* out,
+                         int32_t out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable description of the last error on the calling thread.  Host
  * string owned by the library, valid until the thread's next failing call. */

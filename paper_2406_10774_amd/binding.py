@@ -24,7 +24,8 @@ STATUS_NAMES = {0: "QUEST_OK", -1: "QUEST_ERR_NULL", -2: "QUEST_ERR_SHAPE",
 EXPORTS = ("quest_workspace_bytes", "quest_build_meta", "quest_append_meta", "quest_estimate",
            "quest_append_estimate", "quest_topk", "quest_topk_workspace_bytes", "quest_sparse_decode",
            "quest_select_decode", "quest_step_workspace_bytes", "quest_decode_step",
-           "quest_decode_step_static", "quest_last_error")
+           "quest_decode_step_static", "quest_append_tokens", "quest_tokens_workspace_bytes",
+           "quest_prompt_attention", "quest_tree_attention", "quest_last_error")
 
 
 class QuestError(RuntimeError):
@@ -73,6 +74,12 @@ def load():
     lib.quest_decode_step.argtypes = [cp, vp, vp, i32, vp, i32, f32, vp, vp, vp, vp, i32, vp, vp,
                                       ctypes.c_size_t, vp]
     lib.quest_decode_step_static.argtypes = [cp, vp, vp, i32, vp, i32, f32, vp, vp, vp, vp, i32, vp, vp]
+    i64 = ctypes.c_int64
+    lib.quest_append_tokens.argtypes = [cp, vp, vp, i64, vp, vp, i32, vp]
+    lib.quest_tokens_workspace_bytes.argtypes = [cp, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.quest_prompt_attention.argtypes = [cp, vp, i64, vp, i32, f32, vp, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.quest_tree_attention.argtypes = [cp, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, f32, vp, i32, vp, vp,
+                                         ctypes.c_size_t, vp]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = ctypes.c_int
     lib.quest_last_error.argtypes = []
@@ -226,3 +233,43 @@ def quest_decode_step_static(cache: Cache, k_new, v_new, k_pool_write, q, k_page
         cache.ref, _ptr(k_new), _ptr(v_new), int(bool(k_pool_write)), _ptr(q), int(k_pages),
         float(sm_scale), _ptr(scores), _ptr(topk_idx), _ptr(k_eff), _ptr(out),
         _is_half(out), _ptr(lse), _stream(stream)))
+
+
+# ---- many tokens a sequence.  Packed tensors are [rows][heads][head_dim] with any stride between rows.
+
+def _row_stride(t, other=None):
+    """Elements between the rows of t, and of `other`, whose heads have to lie next to each other."""
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    for x in (t,) if other is None else (t, other):
+        if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or x.shape != t.shape \
+                or (x.shape[0] > 1 and x.stride(0) != stride):
+            raise QuestError(-2, f"packed rows of shape {tuple(x.shape)} and strides {x.stride()}: heads have to lie "
+                                 "next to each other, and keys as values do")
+    return stride
+
+
+def quest_append_tokens(cache: Cache, k_new, v_new, cu_tokens, rows=None, stream=None):
+    total = k_new.shape[0] if rows is None else rows.shape[0]
+    _check(load().quest_append_tokens(cache.ref, _ptr(k_new), _ptr(v_new), _row_stride(k_new, v_new), _ptr(rows),
+                                      _ptr(cu_tokens), total, _stream(stream)))
+
+
+def quest_tokens_workspace_bytes(cache: Cache, total_tokens: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().quest_tokens_workspace_bytes(cache.ref, int(total_tokens), ctypes.byref(out)))
+    return out.value
+
+
+def quest_prompt_attention(cache: Cache, q, cu_tokens, sm_scale, out, lse=None, workspace=None, stream=None):
+    _check(load().quest_prompt_attention(
+        cache.ref, _ptr(q), _row_stride(q), _ptr(cu_tokens), q.shape[0], float(sm_scale), _ptr(out), _is_half(out),
+        _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def quest_tree_attention(cache: Cache, q, k_new, v_new, cu_tokens, tree_mask, sm_scale, out, topk_idx=None, lse=None,
+                         workspace=None, stream=None):
+    """tree_mask: int64 [rows][words]; topk_idx: int32 [batch][KV heads][k_pages], or None for all pages."""
+    _check(load().quest_tree_attention(
+        cache.ref, _ptr(q), _row_stride(q), _ptr(k_new), _ptr(v_new), _row_stride(k_new, v_new), _ptr(cu_tokens),
+        q.shape[0], _ptr(tree_mask), tree_mask.shape[1], _ptr(topk_idx), 0 if topk_idx is None else topk_idx.shape[2],
+        float(sm_scale), _ptr(out), _is_half(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream)))

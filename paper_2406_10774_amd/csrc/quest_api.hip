@@ -99,6 +99,46 @@ size_t workspace_bytes_of(const quest_cache& c) {
   return attention_workspace_bytes(c) + selection_workspace_bytes(c);
 }
 
+// What the calls on packed tokens have in common.  `stride`: elements between tokens of `heads` heads.
+int check_packed(const quest_cache* c, const int32_t* cu, int32_t total, const char* who) {
+  const int r = check_cache(c, who);
+  if (r != QUEST_OK) return r;
+  if (cu == nullptr) {
+    set_error("%s: cu_tokens must not be NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  if (total < 0 || (int64_t)total * c->num_heads > INT32_MAX || !rows_fit_a_launch(*c, total)) {
+    set_error("%s: total_tokens must be >= 0 and total_tokens * num_heads fit a launch (got %d)", who, total);
+    return QUEST_ERR_SHAPE;
+  }
+  return QUEST_OK;
+}
+
+int check_rows(const void* data, int64_t stride, int heads, const char* what, const char* who) {
+  if (data == nullptr) {
+    set_error("%s: %s must not be NULL", who, what);
+    return QUEST_ERR_NULL;
+  }
+  if ((uintptr_t)data % 16 != 0 || stride % 8 != 0 || stride < (int64_t)heads * kHeadDim) {
+    set_error("%s: %s must lie on 16 bytes, its tokens a multiple of 8 and at least %d elements apart (got %lld)", who,
+              what, heads * kHeadDim, (long long)stride);
+    return QUEST_ERR_SHAPE;
+  }
+  return QUEST_OK;
+}
+
+int check_results(const quest_cache& c, const void* out, const void* workspace, const char* who) {
+  if (c.k_pool == nullptr || c.v_pool == nullptr || out == nullptr) {
+    set_error("%s: k_pool, v_pool and out must not be NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  if ((uintptr_t)out % 16 != 0 || (uintptr_t)workspace % 16 != 0) {
+    set_error("%s: out and workspace must lie on 16 bytes", who);
+    return QUEST_ERR_SHAPE;
+  }
+  return QUEST_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -314,6 +354,67 @@ int quest_decode_step_static(const quest_cache* cache, const void* k_new, const 
   return launch_decode_step_static(*cache, k_new, v_new, k_pool_write != 0, q, k_pages, sm_scale,
                                    scores, topk_idx, k_eff, out, out_is_fp16 != 0, lse,
                                    (hipStream_t)stream);
+}
+
+int quest_append_tokens(const quest_cache* cache, const void* k_new, const void* v_new, int64_t new_stride,
+                        const int32_t* rows, const int32_t* cu_tokens, int32_t total_tokens, void* stream) {
+  const char* who = "quest_append_tokens";
+  int r = check_packed(cache, cu_tokens, total_tokens, who);
+  if (r != QUEST_OK || total_tokens == 0) return r;
+  if (cache->k_pool == nullptr || cache->v_pool == nullptr || cache->meta == nullptr) {
+    set_error("%s: k_pool, v_pool and meta must not be NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  if ((r = check_rows(k_new, new_stride, kv_heads(*cache), "k_new", who)) != QUEST_OK) return r;
+  if ((r = check_rows(v_new, new_stride, kv_heads(*cache), "v_new", who)) != QUEST_OK) return r;
+  return launch_append_tokens(*cache, {cu_tokens, total_tokens}, k_new, v_new, new_stride, rows, (hipStream_t)stream);
+}
+
+int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens, size_t* out_bytes) {
+  const char* who = "quest_tokens_workspace_bytes";
+  int r = check_packed(cache, cache ? cache->seq_lens : nullptr, total_tokens, who);
+  if (r != QUEST_OK) return r;
+  if (out_bytes == nullptr) {
+    set_error("%s: out_bytes is NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  *out_bytes = tokens_workspace_bytes(*cache, total_tokens);
+  return QUEST_OK;
+}
+
+int quest_prompt_attention(const quest_cache* cache, const void* q, int64_t q_stride, const int32_t* cu_tokens,
+                           int32_t total_tokens, float sm_scale, void* out, int32_t out_is_fp16, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "quest_prompt_attention";
+  int r = check_packed(cache, cu_tokens, total_tokens, who);
+  if (r != QUEST_OK || total_tokens == 0) return r;
+  if ((r = check_rows(q, q_stride, cache->num_heads, "q", who)) != QUEST_OK) return r;
+  if ((r = check_results(*cache, out, workspace, who)) != QUEST_OK) return r;
+  return launch_prompt(*cache, {cu_tokens, total_tokens}, q, q_stride, sm_scale, out, out_is_fp16 != 0, lse, workspace,
+                       workspace_bytes, (hipStream_t)stream);
+}
+
+int quest_tree_attention(const quest_cache* cache, const void* q, int64_t q_stride, const void* k_new, const void* v_new,
+                         int64_t new_stride, const int32_t* cu_tokens, int32_t total_tokens, const int64_t* tree_mask,
+                         int32_t mask_words, const int32_t* topk_idx, int32_t k_pages, float sm_scale, void* out,
+                         int32_t out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "quest_tree_attention";
+  int r = check_packed(cache, cu_tokens, total_tokens, who);
+  if (r != QUEST_OK || total_tokens == 0) return r;
+  if ((r = check_rows(q, q_stride, cache->num_heads, "q", who)) != QUEST_OK) return r;
+  if ((r = check_rows(k_new, new_stride, kv_heads(*cache), "k_new", who)) != QUEST_OK) return r;
+  if ((r = check_rows(v_new, new_stride, kv_heads(*cache), "v_new", who)) != QUEST_OK) return r;
+  if ((r = check_results(*cache, out, workspace, who)) != QUEST_OK) return r;
+  if (tree_mask == nullptr) {
+    set_error("%s: tree_mask must not be NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  if (mask_words < 1 || (topk_idx != nullptr && k_pages < 1)) {
+    set_error("%s: mask_words, and k_pages with a page list, must be >= 1 (got %d, %d)", who, mask_words, k_pages);
+    return QUEST_ERR_SHAPE;
+  }
+  return launch_tree(*cache, {cu_tokens, total_tokens}, q, q_stride, k_new, v_new, new_stride, tree_mask, mask_words, topk_idx,
+                     k_pages, sm_scale, out, out_is_fp16 != 0, lse, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
 }  // extern "C"

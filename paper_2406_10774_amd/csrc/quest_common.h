@@ -122,6 +122,24 @@ int launch_decode_step_static(const quest_cache& c, const void* k_new, const voi
                               float* scores, int32_t* topk_idx, int32_t* k_eff, void* out,
                               int out_is_fp16, float* lse, hipStream_t s);
 
+// Many tokens a sequence, packed: sequence b has rows [cu[b], cu[b + 1]) of arrays of `total` rows.
+struct PackedTokens {
+  const int32_t* cu;
+  int32_t total;
+};
+int launch_append_tokens(const quest_cache& c, const PackedTokens& p, const void* k_new, const void* v_new,
+                         int64_t new_stride, const int32_t* rows, hipStream_t s);
+// Attention of packed query rows (strides in elements between tokens).  With less workspace than
+// tokens_workspace_bytes the tokens are walked in fewer splits; none is needed.
+size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens);
+bool rows_fit_a_launch(const quest_cache& c, int total_tokens);
+int launch_prompt(const quest_cache& c, const PackedTokens& p, const void* q, int64_t q_stride, float sm_scale, void* out,
+                  int out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, hipStream_t s);
+int launch_tree(const quest_cache& c, const PackedTokens& p, const void* q, int64_t q_stride, const void* k_new,
+                const void* v_new, int64_t new_stride, const int64_t* mask, int mask_words, const int32_t* topk_idx, int k_pages,
+                float sm_scale, void* out, int out_is_fp16, float* lse, void* workspace, size_t workspace_bytes,
+                hipStream_t s);
+
 // -------------------------------------------------------------- device side
 #if defined(__HIPCC__)
 

@@ -1,0 +1,227 @@
+"""Many tokens a sequence on the GPU: insertion against the one-token call, attention of prompts and of drafted
+tokens against 64 bits, at the lengths, pages, groups, strides and masks where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_10774_amd import binding as Q
+from packed_util import D, Packed, Trees, check_prompt, check_tree
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / math.sqrt(D)
+
+
+def run_prompt(p, half, scale=SCALE, workspace="full"):
+    out, lse = p.results(half)
+    ws = p.workspace() if workspace == "full" else None
+    Q.quest_prompt_attention(p.cache, p.q, p.cu, scale, out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def run_tree(p, t, half, scale=SCALE, workspace="full"):
+    out, lse = p.results(half)
+    ws = p.workspace() if workspace == "full" else None
+    Q.quest_tree_attention(p.cache, p.q, p.k_new, p.v_new, p.cu, t.mask, scale, out, topk_idx=t.lists, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 515])
+def test_whole_prompts(n, half):
+    p = Packed([n], [n], heads=3, kv_heads=3, seed=n)
+    for ws in ("full", None):
+        check_prompt(p, *run_prompt(p, half, workspace=ws), half, SCALE, (n, ws))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 4), (4, 1), (6, 2), (10, 2), (16, 2), (18, 1), (40, 1)])
+def test_prompt_groups_ragged(heads, kv_heads):
+    """Sequences of different lengths, one without new tokens, parts of prompts behind cached tokens."""
+    p = Packed([150, 40, 333, 1, 70], [150, 0, 37, 1, 65], heads=heads, kv_heads=kv_heads, seed=heads)
+    for half in (True, False):
+        check_prompt(p, *run_prompt(p, half), half, SCALE, (heads, kv_heads, half))
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+def test_prompt_page_sizes_and_strides(S):
+    for stride in (0, 8, 3 * D):
+        p = Packed([301, 64, 7], [301, 20, 7], heads=8, kv_heads=2, S=S, seed=S, stride=stride)
+        check_prompt(p, *run_prompt(p, True), True, SCALE, (S, stride))
+
+
+@pytest.mark.parametrize("new,past", [(1, 5000), (5, 3001), (64, 4100), (300, 2000)])
+def test_prompt_parts_behind_long_contexts(new, past):
+    """Few rows, many tokens: splits of the tokens, joined; without a workspace the same in one piece."""
+    p = Packed([past + new, past // 3 + 1], [new, 1], heads=8, kv_heads=2, seed=new)
+    for half in (True, False):
+        for ws in ("full", None):
+            check_prompt(p, *run_prompt(p, half, workspace=ws), half, SCALE, (new, past, half, ws))
+
+
+@pytest.mark.parametrize("scale", [SCALE, -SCALE, 0.0, 1.0])
+def test_prompt_scales(scale):
+    p = Packed([190], [190], heads=2, kv_heads=2, seed=5, spread=2.0)
+    for half in (True, False):
+        check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
+
+
+def test_prompt_of_more_sequences_than_lanes():
+    new = [int(x) for x in np.random.default_rng(0).integers(0, 40, 150)]
+    lens = [n + (7 * i) % 50 + 1 for i, n in enumerate(new)]
+    p = Packed(lens, new, heads=4, kv_heads=1, seed=6)
+    check_prompt(p, *run_prompt(p, True), True, SCALE)
+
+
+def test_prompt_rising_logits():
+    """The running maximum moves in every tile: logits grow along the sequence, then fall."""
+    p = Packed([700], [700], heads=2, kv_heads=1, seed=7)
+    t = torch.arange(700, device=p.dev)
+    phys = p.table[0].long()[t // p.S]
+    ramp = (torch.where(t < 400, t, 800 - t).float() * 0.25)[:, None, None].half()
+    p.k_pool[phys, :, t % p.S] = ramp * torch.ones(1, 1, D, device=p.dev, dtype=torch.float16) / 16
+    p.q[:700] = p.q[:700].abs()
+    for half in (True, False):
+        check_prompt(p, *run_prompt(p, half), half, SCALE, half)
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("n,ctx", [(1, 0), (1, 1), (1, 700), (5, 64), (8, 1000), (31, 65), (33, 129), (64, 300), (65, 300), (130, 77)])
+def test_trees(n, ctx, half):
+    p = Packed([ctx, ctx // 2], [n, max(1, n // 3)], heads=4, kv_heads=2, seed=n + ctx, stride=16)
+    t = Trees(p, seed=n)
+    for ws in ("full", None):
+        check_tree(p, t, *run_tree(p, t, half, workspace=ws), half, SCALE, (n, ctx, ws))
+
+
+@pytest.mark.parametrize("heads,kv_heads,S", [(1, 1, 16), (8, 1, 8), (6, 2, 32), (64, 2, 64), (20, 4, 16)])
+def test_tree_groups_and_pages(heads, kv_heads, S):
+    p = Packed([900, 0, 64, 1203], [12, 3, 0, 40], heads=heads, kv_heads=kv_heads, S=S, seed=S)
+    t = Trees(p, seed=S, words=2)
+    for half in (True, False):
+        check_tree(p, t, *run_tree(p, t, half), half, SCALE, (heads, kv_heads, S, half))
+
+
+def nothing(rng, n, words):
+    return np.zeros((n, n), bool)
+
+
+def everything(rng, n, words):
+    return np.ones((n, n), bool)
+
+
+def anything(rng, n, words):
+    return rng.random((n, n)) < 0.3
+
+
+@pytest.mark.parametrize("kind", [nothing, everything, anything])
+def test_tree_masks(kind):
+    """Also rows that see no drafted node, and, without a context, nothing at all: out 0, lse -inf."""
+    p = Packed([0, 50, 128], [20, 70, 64], heads=4, kv_heads=2, seed=3)
+    t = Trees(p, kind=kind, words=3)
+    for half in (True, False):
+        for ws in ("full", None):
+            out, lse = run_tree(p, t, half, workspace=ws)
+            check_tree(p, t, out, lse, half, SCALE, (kind.__name__, half))
+            if kind is nothing:
+                assert bool((out[:20] == 0).all()) and bool((lse[:20] == -math.inf).all())
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("K", [1, 3, 17, 40])
+def test_tree_listed_pages(S, K):
+    """Lists as the selection leaves them, and with holes, ids of pages without tokens and a page twice."""
+    rng = np.random.default_rng(S * K)
+    p = Packed([1500, 30, 777], [9, 20, 1], heads=8, kv_heads=2, S=S, seed=K)
+    lists = np.full((3, 2, K), -1, np.int32)
+    for b in range(3):
+        pages = -(-p.lens[b] // S)
+        for h in range(2):
+            m = min(K, pages)
+            lists[b, h, :m] = np.sort(rng.permutation(pages)[:m])
+    rough = lists.copy()
+    for b in range(3):
+        for h in range(2):
+            rng.shuffle(rough[b, h])
+            if K >= 3:
+                rough[b, h, K // 2] = -5 if h else 100000
+                rough[b, h, 0] = rough[b, h, 1]
+    for these in (lists, rough):
+        t = Trees(p, lists=these, seed=K)
+        for half in (True, False):
+            for ws in ("full", None):
+                check_tree(p, t, *run_tree(p, t, half, workspace=ws), half, SCALE, (S, K, half, ws))
+
+
+@pytest.mark.parametrize("scale", [-SCALE, 0.0, 1.0])
+def test_tree_scales(scale):
+    p = Packed([300], [17], heads=4, kv_heads=2, seed=8)
+    t = Trees(p)
+    for half in (True, False):
+        check_tree(p, t, *run_tree(p, t, half, scale), half, scale, scale)
+
+
+# ---- insertion
+
+def one_by_one(p, past, rows):
+    """What calls of quest_append_meta leave: the cache and the metadata, token after token."""
+    k_pool, v_pool, meta, lens = p.k_pool.clone(), p.v_pool.clone(), p.meta.clone(), torch.zeros_like(p.seq_lens)
+    for b in range(p.B):
+        one = Q.Cache(k_pool, v_pool, meta, p.table[b:b + 1], lens[b:b + 1], num_heads=p.H)
+        for i in range(p.new[b]):
+            row = int(p.cu_np[b]) + i
+            row = row if rows is None else int(rows[row])
+            lens[b] = past[b] + i + 1
+            Q.quest_append_meta(one, p.k_new[row].contiguous(), p.v_new[row].contiguous(), True)
+    torch.cuda.synchronize()
+    return k_pool, v_pool, meta
+
+
+def same_bits(a, b):
+    return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("stride", [0, 24])
+def test_append_like_one_by_one(S, stride):
+    new = [1, 0, 2 * S, 3 * S + 1, S - 1, 5, 1, 70]
+    past = [0, 13, 0, S - 1, 1, S + S // 2, 2 * S, 3]
+    p = Packed([n + m for n, m in zip(new, past)], new, heads=6, kv_heads=3, S=S, seed=S, stride=stride)
+    p.k_new[::5, :, ::3] = 0.0
+    p.k_new[1::5, :, ::3] = -0.0
+    p.seq_lens.copy_(torch.tensor(past))
+    p.seq_lens.clamp_(min=1)
+    Q.quest_build_meta(p.cache)                    # entries of the tokens before (others are overwritten or not read)
+    p.seq_lens.copy_(torch.tensor(p.lens))
+    rng = np.random.default_rng(S)
+    for rows in (None, rng.permutation(p.total - 3), rng.integers(0, p.total - 3, p.total - 3)):
+        want = one_by_one(p, past, rows)
+        keep = [x.clone() for x in (p.k_pool, p.v_pool, p.meta)]
+        dev_rows = None if rows is None else torch.from_numpy(np.concatenate([rows, [-1] * 3]).astype(np.int32)).to(p.dev)
+        Q.quest_append_tokens(p.cache, p.k_new, p.v_new, p.cu, rows=dev_rows)
+        torch.cuda.synchronize()
+        for got, w, name in zip((p.k_pool, p.v_pool, p.meta), want, ("k", "v", "meta")):
+            assert same_bits(got, w), (S, name, rows is None)
+        for x, y in zip((p.k_pool, p.v_pool, p.meta), keep):
+            x.copy_(y)
+
+
+def test_append_prompts_like_build():
+    """A batch of more sequences than a wave has lanes; the metadata of whole prompts is what quest_build_meta gives."""
+    new = [int(x) for x in np.random.default_rng(1).integers(1, 90, 100)]
+    p = Packed(new, new, heads=2, kv_heads=2, seed=1, cached=False)
+    Q.quest_append_tokens(p.cache, p.k_new, p.v_new, p.cu)
+    got = p.meta.clone()
+    p.meta.zero_()
+    Q.quest_build_meta(p.cache)
+    torch.cuda.synchronize()
+    assert same_bits(got, p.meta)
+    for b in range(p.B):
+        k, v = p.cached(b, 1)
+        assert torch.equal(k, p.k_new[p.rows(b), 1].double()) and torch.equal(v, p.v_new[p.rows(b), 1].double())
+    used = torch.zeros(p.k_pool.shape[0], dtype=torch.bool, device=p.dev)
+    for b in range(p.B):
+        used[p.table[b, :-(-new[b] // p.S)].long()] = True
+    assert bool(p.k_pool[~used].isnan().all()) and bool(p.v_pool[~used].isnan().all())
