@@ -1,4 +1,11 @@
 // Attention of prompts (causal) and of trees of drafted tokens over the paged cache.  See quest_rows_core.h.
+//
+// Two kernels.  Many rows: four waves of 32 rows share the tiles of tokens, which are fetched once for 128 rows.
+// Few rows: every wave of a work-group has all 32 (or 64) rows and tiles of its own, so that four waves
+// stream tokens however few the rows are; their results are joined in LDS.
+//
+// A tile's tokens are walked in splits of `chunk` tiles where that gives the compute units more to do; rows with more
+// than one leave partial results, which merge_rows_kernel joins.
 #include <algorithm>
 
 #include "quest_common.h"
@@ -9,242 +16,351 @@ namespace quest {
 
 namespace {
 
-constexpr int kSharedWaves = 4;                       // waves of 32 rows that share the tiles of tokens
-constexpr int kSharedRows = 32 * kSharedWaves;
+constexpr int kWaves = 4;
+constexpr int kSharedRows = 32 * kWaves;
 
-// What the threads of a work-group fetch of a tile of 64 tokens: 16 tokens in each of four loads, four tokens (in
-// one page) a wave.
-constexpr int kLoads = kTileTokens / (4 * kSharedWaves);
+// A work-group's part: a unit of one KV head.  Adjacent work-groups have adjacent heads: with a multiple of eight KV heads
+// a head's units are all on one die, whose L2 then holds what its row tiles read at the same time.
+template <bool kTree, int kRows>
+struct Part {
+  Sequence s;
+  Stream<kTree> stream;
+  int hk, unit, row0, rows, past, group, first_tile, end_tile;
 
-struct Tile {
-  uint4 k[kLoads], v[kLoads];
+  // position of a row's token (of the last one's, from there on)
+  __device__ __forceinline__ int position(int row) const { return past + min(row, rows - 1) / group; }
+  __device__ __forceinline__ bool whole() const { return s.splits == 1; }   // the row tile has no other split
+
+  __device__ __forceinline__ bool find(const RowsArgs& a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
+                                       const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, int lane) {
+    hk = blockIdx.x % a.kv_heads;
+    unit = blockIdx.x / a.kv_heads;
+    if (!find_sequence<kTree, kRows, false>(s, a, cu, seq_lens, kTree && topk != nullptr, unit, lane)) return false;
+    const int index = unit - s.before, split = index / s.row_tiles;
+    group = a.group;
+    rows = s.tokens * group;
+    row0 = (s.row_tiles - 1 - (index - split * s.row_tiles)) * kRows;  // a prompt's last rows have the most work
+    past = s.seq_len - s.tokens;
+    stream.init(a, s, hk, position(row0 + kRows - 1), page_table, topk);
+    first_tile = split * s.chunk;
+    end_tile = s.chunk < stream.tiles - first_tile ? first_tile + s.chunk : stream.tiles;
+    return true;
+  }
+  __device__ __forceinline__ size_t part_row(const RowsArgs& a, int in_tile) const {
+    return ((size_t)unit * a.kv_heads + hk) * kRows + in_tile;
+  }
 };
 
+// Many rows: the next tile is on its way to registers while the waves work on the one in LDS.
 template <bool kTree, bool kExact>
-__global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
+__global__ __launch_bounds__(kWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
+  constexpr int kLoads = kTileTokens / (4 * kWaves);
   __shared__ __align__(16) char lds[2][2][kTileTokens * kRowBytes];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
-  const int hk = blockIdx.x % a.kv_heads;
-  const int split = blockIdx.x / a.kv_heads % a.splits;
-  const int slot = a.slots - 1 - (int)(blockIdx.x / a.kv_heads / a.splits);  // a prompt's last rows have the most work
-  RowTile t;
-  if (!find_tile<kSharedRows>(t, cu, a.batch, a.group, slot, lane)) return;
-  const int32_t* table = page_table + (size_t)t.b * a.max_pages;
-  const int seq_len = seq_lens[t.b];
-  const int page_mask = (1 << a.page_shift) - 1;
-
-  // this lane's row, and the tokens that the wave's and the work-group's rows attend to
-  const int row = t.row0 + wave * 32 + (lane & 31);
-  const bool there = row < t.rows;
-  const int token = there ? row / a.group : t.tokens - 1;
-  const int head = hk * a.group + (there ? row - token * a.group : 0);
-  const int past = seq_len - t.tokens;                                  // prompts: tokens before the new ones
-  const int wave_first = past + min(t.row0 + wave * 32, t.rows - 1) / a.group;
-  const int wave_last = past + min(t.row0 + wave * 32 + 31, t.rows - 1) / a.group;
-  const int group_last = past + min(t.row0 + kSharedRows - 1, t.rows - 1) / a.group;
-  // tiles: of the context, then (trees) of the drafted tokens
-  const int limit = kTree ? seq_len : group_last + 1;
-  const bool list = kTree && topk != nullptr;
-  const int32_t* pages = list ? topk + ((size_t)t.b * a.kv_heads + hk) * a.k_pages : nullptr;
-  const int seq_pages = (seq_len + page_mask) >> a.page_shift;
-  const int context_tiles =
-      list ? (int)((((int64_t)min(a.k_pages, a.max_pages) << a.page_shift) + kTileTokens - 1) / kTileTokens)
-           : (limit + kTileTokens - 1) / kTileTokens;
-  const int all_tiles = context_tiles + (kTree ? (t.tokens + kTileTokens - 1) / kTileTokens : 0);
-  const int first_tile = (int)((int64_t)all_tiles * split / a.splits);
-  const int end_tile = (int)((int64_t)all_tiles * (split + 1) / a.splits);
+  Part<kTree, kSharedRows> w;
+  if (!w.find(a, cu, seq_lens, page_table, topk, lane)) return;
+  const int row0 = w.row0 + wave * 32, row = row0 + (lane & 31);
+  const bool there = row < w.rows;
+  const int token = there ? row / a.group : 0;
+  const int head = w.hk * a.group + (there ? row - token * a.group : 0);
+  const int wave_first = w.position(row0), wave_last = w.position(row0 + 31);
 
   RowState<kExact> st;
-  st.init(a.q + (int64_t)(t.first + token) * a.q_stride + (int64_t)head * kRowBytes, there, a.q_sign, lane);
+  st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, there, a.q_sign, lane);
 
-  // The physical page (and how many of the four tokens are there) of each of a tile's loads.
-  int phys[kLoads], count[kLoads];
-  auto find_pages = [&](int tile) {
+  typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of a tile; load i is wave's place 16 i + 4 wave
+  uint64_t held = 0, held_next = 0;
+  uint4 k[kLoads], v[kLoads];
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      w.stream.load(a, w.hk, tile * kTileTokens + (i * kWaves + wave) * 4, four, i * kWaves + wave, lane, k[i], v[i]);
+    if (kTree) held_next = w.stream.held(four, lane);
+  };
+  auto find = [&](int tile) { four = w.stream.find(min(tile, w.end_tile - 1) * kTileTokens + (lane & 15) * 4); };
+  auto store = [&](int buffer) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = tile * kTileTokens + i * (4 * kSharedWaves) + wave * 4;
-      if (kTree && tile >= context_tiles) {
-        count[i] = t.tokens - (at - context_tiles * kTileTokens);
-      } else if (list) {
-        const int entry = at >> a.page_shift;
-        const int page = entry < min(a.k_pages, a.max_pages) ? pages[entry] : -1;
-        const bool valid = page >= 0 && page < seq_pages;
-        count[i] = valid ? seq_len - (page << a.page_shift) - (at & page_mask) : 0;
-        phys[i] = valid ? table[page] : 0;
-      } else {
-        count[i] = limit - at;
-        phys[i] = table[min(at, limit - 1) >> a.page_shift];
-      }
+      const int at = (i * kWaves + wave) * 4 + (lane >> 4);
+      st16(lds[buffer][0] + k_place(at, lane & 15), k[i]);
+      st16(lds[buffer][1] + v_place(at, lane & 15), v[i]);
     }
   };
-  auto load = [&](Tile& r, int tile) {
-    const int sub = lane >> 4, chunk = lane & 15;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = tile * kTileTokens + i * (4 * kSharedWaves) + wave * 4;
-      const char *k, *v;
-      if (kTree && tile >= context_tiles) {
-        const int node = min(at - context_tiles * kTileTokens + sub, t.tokens - 1);
-        const int64_t off = (int64_t)(t.first + node) * a.new_stride + (int64_t)hk * kRowBytes + chunk * 16;
-        k = a.k_new + off;
-        v = a.v_new + off;
-      } else {
-        const size_t off =
-            ((((size_t)phys[i] * a.kv_heads + hk) << a.page_shift) + (at & page_mask) + sub) * kRowBytes + chunk * 16;
-        k = a.k_pool + off;
-        v = a.v_pool + off;
-      }
-      r.k[i] = ld16(k);
-      r.v[i] = ld16(v);
-      if (sub >= count[i]) r.v[i] = make_uint4(0, 0, 0, 0);  // stale slots may hold anything
-    }
-  };
-  auto store = [&](const Tile& r, int buffer) {
-    const int chunk = lane & 15;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = i * (4 * kSharedWaves) + wave * 4 + (lane >> 4);
-      st16(lds[buffer][0] + k_place(at, chunk), r.k[i]);
-      st16(lds[buffer][1] + v_place(at, chunk), r.v[i]);
-    }
-  };
-
-  if (first_tile < end_tile) {
-    Tile next;
-    find_pages(first_tile);
-    load(next, first_tile);
-    store(next, 0);
+  if (w.first_tile < w.end_tile) {
+    find(w.first_tile);
+    load(w.first_tile);
+    find(w.first_tile + 1);
+    store(0);
     __syncthreads();
-    for (int tile = first_tile; tile < end_tile; ++tile) {
-      const int buffer = (tile - first_tile) & 1;
-      if (tile + 1 < end_tile) {
-        find_pages(tile + 1);
-        load(next, tile + 1);
+    for (int tile = w.first_tile; tile < w.end_tile; ++tile) {
+      const int buffer = (tile - w.first_tile) & 1;
+      const bool more = tile + 1 < w.end_tile;
+      held = held_next;
+      if (more) {
+        load(tile + 1);
+        find(tile + 2);
       }
-      const int t0 = tile * kTileTokens;
-      bool masked = false, skip = false;
-      uint64_t allow = ~0ull;
-      auto first_bits = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
-      if (!kTree) {
-        masked = t0 + kTileTokens - 1 > wave_first;
-        skip = t0 > wave_last;
-        if (masked) allow = first_bits(past + token + 1 - t0);
-      } else if (tile >= context_tiles) {
-        masked = true;
-        const int words = tile - context_tiles;
-        allow = words < a.mask_words ? (uint64_t)mask[(int64_t)(t.first + token) * a.mask_words + words] : 0;
-        allow &= first_bits(t.tokens - words * kTileTokens);
-      } else if (list) {
-        const int entry = (t0 + lane) >> a.page_shift;
-        const int page = entry < min(a.k_pages, a.max_pages) ? pages[entry] : -1;
-        allow = __ballot(page >= 0 && page < seq_pages &&
-                         ((int64_t)page << a.page_shift) + ((t0 + lane) & page_mask) < seq_len);
-        masked = allow != ~0ull;
-      } else {
-        masked = t0 + kTileTokens > limit;
-        allow = first_bits(limit - t0);
+      const int p0 = tile * kTileTokens;
+      if (row0 < w.rows && (kTree || p0 <= wave_last)) {
+        const bool masked = !w.stream.whole(held, p0, wave_first);
+        uint64_t allow = ~0ull;
+        if (masked) allow = w.stream.allow(held, p0, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words);
+        st.template fold<2>(lds[buffer][0], lds[buffer][1], a.scale_log2, masked, allow, lane);
       }
-      if (!skip) st.template fold<2>(lds[buffer][0], lds[buffer][1], a.scale_log2, masked, allow, lane);
-      if (tile + 1 < end_tile) store(next, buffer ^ 1);
+      if (more) store(buffer ^ 1);
       __syncthreads();
     }
   }
 
+  if (!there) return;
   const float total = st.total();
-  if (a.splits > 1) {
-    const size_t part = (((size_t)split * a.slots + slot) * a.kv_heads + hk) * kSharedRows + wave * 32 + (lane & 31);
-    if (there) {
-      st.each4(RowState<kExact>::kUnscale, lane,
-               [&](int d, float4 v) { *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d) = v; });
-      if (lane < 32) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(st.ref, total);
-    }
+  if (!w.whole()) {
+    const size_t part = w.part_row(a, wave * 32 + (lane & 31));
+    st.each4(RowState<kExact>::kUnscale, lane,
+             [&](int d, float4 o) { *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d) = o; });
+    if (lane < 32) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(st.ref, total);
     return;
   }
-  if (!there) return;
-  const size_t out_row = (size_t)(t.first + token) * (a.kv_heads * a.group) + head;
+  const size_t out_row = (size_t)(w.s.first + token) * (a.kv_heads * a.group) + head;
   const float factor = total > 0.f ? RowState<kExact>::kUnscale / total : 0.f;
-  st.each4(factor, lane, [&](int d, float4 v) { store4(a.out, a.out_is_fp16, out_row * kHeadDim + d, v); });
+  st.each4(factor, lane, [&](int d, float4 o) { store4(a.out, a.out_is_fp16, out_row * kHeadDim + d, o); });
   if (a.lse != nullptr && lane < 32)
     a.lse[out_row] = total > 0.f ? (st.ref + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
 }
 
-// The splits of each row: a wave a row, two channels a lane.
-template <int kRows>
-__global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const int32_t* __restrict__ cu) {
+// Few rows: tiles of 32 tokens, each wave its own.
+template <bool kTree, bool kExact, int kBlocks>
+__global__ __launch_bounds__(kWaves* kWave, kBlocks == 1 ? 2 : 1) void few_rows_kernel(
+    const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
+    const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
+  constexpr int kRows = 32 * kBlocks, kTokens = 32, kLoads = kTokens / 4;
+  constexpr int kStride = kHeadDim + 4;
+  constexpr int kStage = 2 * kTokens * kRowBytes, kJoin = 32 * kStride * 4;
+  __shared__ __align__(16) char lds[kWaves * (kStage > kJoin ? kStage : kJoin)];
+  __shared__ float ml[2][kWaves][32];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = lane_id();
+  Part<kTree, kRows> w;
+  if (!w.find(a, cu, seq_lens, page_table, topk, lane)) return;
+
+  RowState<kExact> st[kBlocks];
+  int token[kBlocks];
+#pragma unroll
+  for (int n = 0; n < kBlocks; ++n) {
+    const int row = w.row0 + n * 32 + (lane & 31);
+    const bool there = row < w.rows;
+    token[n] = there ? row / a.group : 0;
+    const int head = w.hk * a.group + (there ? row - token[n] * a.group : 0);
+    st[n].init(a.q + (int64_t)(w.s.first + token[n]) * a.q_stride + (int64_t)head * kRowBytes, there, a.q_sign, lane);
+  }
+  const int first_position = w.position(w.row0);
+
+  const int end = w.end_tile * 2;
+  char* stage_k = lds + wave * kStage;
+  char* stage_v = stage_k + kTokens * kRowBytes;
+  typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of the tile of 64 that has the wave's 32
+  uint64_t held = 0, held_next = 0;
+  uint4 k[kLoads], v[kLoads];
+  auto load = [&](int half) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      w.stream.load(a, w.hk, half * kTokens + i * 4, four, (half & 1) * kLoads + i, lane, k[i], v[i]);
+    if (kTree) held_next = w.stream.held(four, lane);
+  };
+  auto find = [&](int half) { four = w.stream.find((min(half, end - 1) * kTokens & ~63) + (lane & 15) * 4); };
+  int half = w.first_tile * 2 + wave;
+  if (half < end) {
+    find(half);
+    load(half);
+    find(half + kWaves);
+  }
+  for (; half < end; half += kWaves) {
+    held = held_next;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = i * 4 + (lane >> 4);
+      st16(stage_k + k_place(at, lane & 15), k[i]);
+      st16(stage_v + v_place(at, lane & 15), v[i]);
+    }
+    lds_in_order();
+    if (half + kWaves < end) {
+      load(half + kWaves);
+      find(half + 2 * kWaves);
+    }
+    const int p0 = half * kTokens & ~63;
+    const bool masked = !w.stream.whole(held, p0, first_position);
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      uint64_t allow = ~0ull;
+      if (masked)
+        allow = w.stream.allow(held, p0, w.past + token[n], mask + (int64_t)(w.s.first + token[n]) * a.mask_words, a.mask_words) >>
+                (half & 1) * 32;
+      st[n].template fold<1>(stage_k, stage_v, a.scale_log2, masked, allow, lane);
+    }
+    lds_in_order();
+  }
+
+  // Join the waves' results, 32 rows at a time: eight threads a row, 16 channels each.
+  float* join = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int n = 0; n < kBlocks; ++n) {
+    __syncthreads();
+    const float total = st[n].total();
+    float* mine = join + (wave * 32 + (lane & 31)) * kStride;
+    st[n].each4(RowState<kExact>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
+    if (lane < 32) {
+      ml[0][wave][lane] = total > 0.f ? st[n].ref : kNegBig;
+      ml[1][wave][lane] = total;
+    }
+    __syncthreads();
+    const int in_block = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * 16;
+    const int row = w.row0 + n * 32 + in_block;
+    if (row >= w.rows) continue;
+    float top = kNegBig, sum = 0.f, weight[kWaves];
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[0][i][in_block]);
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      weight[i] = __builtin_amdgcn_exp2f(ml[0][i][in_block] - top);
+      sum += weight[i] * ml[1][i][in_block];
+    }
+    float4 o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(join + (i * 32 + in_block) * kStride + d0 + 4 * j);
+        o[j].x += weight[i] * x.x, o[j].y += weight[i] * x.y, o[j].z += weight[i] * x.z, o[j].w += weight[i] * x.w;
+      }
+    }
+    if (!w.whole()) {
+      const size_t part = w.part_row(a, n * 32 + in_block);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d0 + 4 * j) = o[j];
+      if (d0 == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(top, sum);
+      continue;
+    }
+    const int tok = row / a.group;
+    const size_t out_row = (size_t)(w.s.first + tok) * (a.kv_heads * a.group) + w.hk * a.group + (row - tok * a.group);
+    const float factor = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      store4(a.out, a.out_is_fp16, out_row * kHeadDim + d0 + 4 * j,
+             make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor));
+    if (a.lse != nullptr && d0 == 0) a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
+}
+
+// The partial results of each row: a wave a row, a lane a split for the weights, then two channels a lane.
+template <bool kTree, int kRows>
+__global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const int32_t* __restrict__ cu,
+                                                         const int32_t* __restrict__ seq_lens, int list) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
   const int hk = blockIdx.x % a.kv_heads;
   const int rest = blockIdx.x / a.kv_heads;
   const int in_tile = rest % (kRows / 4) * 4 + wave;
-  const int slot = rest / (kRows / 4);
-  RowTile t;
-  if (!find_tile<kRows>(t, cu, a.batch, a.group, slot, lane)) return;
-  const int row = t.row0 + in_tile;
-  if (row >= t.rows) return;
-  const size_t part0 = ((size_t)slot * a.kv_heads + hk) * kRows + in_tile;
-  const size_t step = (size_t)a.slots * a.kv_heads * kRows;
+  const int tile = rest / (kRows / 4);
+  Sequence s;
+  if (!find_sequence<kTree, kRows, true>(s, a, cu, seq_lens, list != 0, tile, lane)) return;
+  const int row = (tile - s.before) * kRows + in_tile;
+  if (row >= s.tokens * a.group || s.splits == 1) return;  // (of one split: written already)
+  const int parts = s.splits;
+  const size_t step = (size_t)s.row_tiles * a.kv_heads * kRows;   // rows between two splits' parts
+  const size_t part0 = (((size_t)s.units_before + (s.row_tiles - 1 - (tile - s.before))) * a.kv_heads + hk) * kRows + in_tile;
   float top = kNegBig;
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part0 + s * step) * 2);
+  for (int i = lane; i < parts; i += kWave) {
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part0 + i * step) * 2);
     if (ml.y > 0.f) top = fmaxf(top, ml.x);
   }
+#pragma unroll
+  for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
   float sum = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part0 + s * step) * 2);
-    if (!(ml.y > 0.f)) continue;
-    const float w = __builtin_amdgcn_exp2f(ml.x - top);
-    const float2 v = *reinterpret_cast<const float2*>(a.part_acc + (part0 + s * step) * kHeadDim + lane * 2);
-    sum += ml.y * w;
-    o0 += v.x * w;
-    o1 += v.y * w;
+  const float* from = a.part_acc + part0 * kHeadDim + lane * 2;
+  for (int base = 0; base < parts; base += kWave) {
+    float weight = 0.f;
+    if (base + lane < parts) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part0 + (base + lane) * step) * 2);
+      weight = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+      sum += weight * ml.y;
+    }
+    const int n = min(parts - base, kWave);
+    for (int i = 0; i < n; i += 8) {  // eight on their way
+      float2 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = *reinterpret_cast<const float2*>(from + (base + min(i + j, n - 1)) * step * kHeadDim);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = i + j < n ? from_lane(weight, i + j) : 0.f;
+        o0 += v[j].x * x;
+        o1 += v[j].y * x;
+      }
+    }
   }
+#pragma unroll
+  for (int i = 1; i < kWave; i <<= 1) sum += __shfl_xor(sum, i);
   const int token = row / a.group;
-  const size_t out_row = (size_t)(t.first + token) * (a.kv_heads * a.group) + hk * a.group + (row - token * a.group);
+  const size_t out_row = (size_t)(s.first + token) * (a.kv_heads * a.group) + hk * a.group + (row - token * a.group);
   const float factor = sum > 0.f ? 1.f / sum : 0.f;
   store_out2(a.out, a.out_is_fp16, out_row * kHeadDim + lane * 2, o0 * factor, o1 * factor);
   if (a.lse != nullptr && lane == 0)
     a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
-constexpr int kMaxSplits = 64;
-
-int64_t slots_of(const quest_cache& c, int total_tokens, int rows) {
-  return (int64_t)total_tokens * group_size(c) / rows + c.batch;
+// How a call is cut up, from what the host knows.
+struct Plan {
+  int rows;                  // of a row tile: 32, 64 (few_rows_kernel), 128
+  int64_t row_tiles;         // room for them
+  int target_log2, least_chunk;
+};
+Plan plan_of(const quest_cache& c, int total_tokens, bool tree) {
+  Plan p;
+  const int64_t mean = ((int64_t)total_tokens * group_size(c) + c.batch - 1) / c.batch;
+  p.rows = mean <= 32 ? 32 : mean <= 64 ? 64 : kSharedRows;
+  p.row_tiles = (int64_t)total_tokens * group_size(c) / p.rows + c.batch;
+  p.target_log2 = p.row_tiles * kv_heads(c) >= (tree ? 4096 : 512) ? -1 : 10;
+  p.least_chunk = p.rows == kSharedRows ? 8 : 4;
+  return p;
+}
+// Units: 2^target_log2 for all heads and one for each row tile (rounding up), at most; without splits the row tiles.
+int64_t units_of(const Plan& p, const quest_cache& c) {
+  return p.row_tiles + (p.target_log2 < 0 ? 0 : (1 << p.target_log2) / kv_heads(c));
+}
+size_t bytes_of(const Plan& p, const quest_cache& c) {
+  return p.target_log2 < 0 ? 0 : (size_t)units_of(p, c) * kv_heads(c) * p.rows * (kHeadDim + 2) * sizeof(float);
 }
 
-// Splits of the tokens: as many work-groups as the compute units hold at once, two each.
-int splits_of(const quest_cache& c, int total_tokens) {
-  const int64_t groups = slots_of(c, total_tokens, kSharedRows) * kv_heads(c);
-  const int64_t tiles = ((int64_t)c.max_pages_per_seq * c.page_size + kTileTokens - 1) / kTileTokens;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, tiles, kMaxSplits}));
-}
-
-size_t split_bytes(const quest_cache& c, int total_tokens) {
-  return (size_t)slots_of(c, total_tokens, kSharedRows) * kv_heads(c) * kSharedRows * (kHeadDim + 2) * sizeof(float);
-}
-
-template <bool kTree>
-int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32_t* topk, void* workspace,
-                size_t bytes, const char* who, hipStream_t s) {
-  a.slots = (int)slots_of(c, total_tokens, kSharedRows);
-  a.splits = splits_of(c, total_tokens);
-  const size_t one = split_bytes(c, total_tokens);
-  if (workspace == nullptr) bytes = 0;
-  a.splits = (int)std::min<size_t>(a.splits, std::max<size_t>(1, bytes / one));
+template <bool kTree, bool kExact>
+int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32_t* topk, void* workspace, size_t bytes,
+                const char* who, hipStream_t s) {
+  Plan p = plan_of(c, total_tokens, kTree);
+  if (workspace == nullptr || bytes_of(p, c) > bytes) p.target_log2 = -1;
+  a.target_log2 = p.target_log2;
+  a.least_chunk = p.least_chunk;
   a.part_acc = (float*)workspace;
-  a.part_ml = a.part_acc + (size_t)a.splits * a.slots * a.kv_heads * kSharedRows * kHeadDim;
-  const dim3 grid((unsigned)(a.slots * a.splits * a.kv_heads)), block(kSharedWaves * kWave);
-  if (a.out_is_fp16)
-    hipLaunchKernelGGL((shared_rows_kernel<kTree, false>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+  a.part_ml = a.part_acc + (size_t)units_of(p, c) * a.kv_heads * p.rows * kHeadDim;
+  const dim3 grid((unsigned)(units_of(p, c) * a.kv_heads)), block(kWaves * kWave);
+  if (p.rows == 32)
+    hipLaunchKernelGGL((few_rows_kernel<kTree, kExact, 1>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+  else if (p.rows == 64)
+    hipLaunchKernelGGL((few_rows_kernel<kTree, kExact, 2>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   else
-    hipLaunchKernelGGL((shared_rows_kernel<kTree, true>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+    hipLaunchKernelGGL((shared_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   const int r = check_launch(who);
-  if (r != QUEST_OK || a.splits == 1) return r;
-  hipLaunchKernelGGL(merge_rows_kernel<kSharedRows>, dim3((unsigned)(a.slots * (kSharedRows / 4) * a.kv_heads)), dim3(256), 0, s, a,
-                     a.cu);
+  if (r != QUEST_OK || p.target_log2 < 0) return r;
+  const dim3 merge((unsigned)(p.row_tiles * (p.rows / 4) * a.kv_heads));
+  const int list = topk != nullptr;
+  if (p.rows == 32)
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, 32>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
+  else if (p.rows == 64)
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, 64>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
+  else
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kSharedRows>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
   return check_launch(who);
 }
 
@@ -272,19 +388,17 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
 
 }  // namespace
 
-size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) {
-  const int splits = splits_of(c, total_tokens);
-  return splits > 1 ? splits * split_bytes(c, total_tokens) : 0;
-}
+size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) { return bytes_of(plan_of(c, total_tokens, true), c); }
 
 bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {
-  return slots_of(c, total_tokens, kSharedRows) * (kSharedRows / 4) * kv_heads(c) <= INT32_MAX;
+  return ((int64_t)total_tokens * group_size(c) + 128 * (int64_t)c.batch) * kv_heads(c) <= INT32_MAX;
 }
 
 int launch_prompt(const quest_cache& c, const PackedTokens& p, const void* q, int64_t q_stride, float sm_scale, void* out,
                   int out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, hipStream_t s) {
   RowsArgs a = rows_args(c, p, q, q_stride, sm_scale, out, out_is_fp16, lse);
-  return launch_rows<false>(c, a, p.total, nullptr, workspace, workspace_bytes, "quest_prompt_attention", s);
+  const auto launch = out_is_fp16 ? launch_rows<false, false> : launch_rows<false, true>;
+  return launch(c, a, p.total, nullptr, workspace, workspace_bytes, "quest_prompt_attention", s);
 }
 
 int launch_tree(const quest_cache& c, const PackedTokens& p, const void* q, int64_t q_stride, const void* k_new,
@@ -298,7 +412,8 @@ int launch_tree(const quest_cache& c, const PackedTokens& p, const void* q, int6
   a.mask = mask;
   a.mask_words = mask_words;
   a.k_pages = k_pages;
-  return launch_rows<true>(c, a, p.total, topk_idx, workspace, workspace_bytes, "quest_tree_attention", s);
+  const auto launch = out_is_fp16 ? launch_rows<true, false> : launch_rows<true, true>;
+  return launch(c, a, p.total, topk_idx, workspace, workspace_bytes, "quest_tree_attention", s);
 }
 
 }  // namespace quest

@@ -4,8 +4,9 @@
 // head r % G of token r / G, so that whatever the group the keys are read once for all of them.
 // Rows are cut into tiles of kRows.  A tile walks the tokens it attends to 64 at a time with an online softmax.
 //
-// Work-groups have to know their sequence without the host knowing any length: sequence b's tiles start at slot
-// floor(cu[b] G / kRows) + b, which leaves room for ceil(n_b G / kRows) of them; slots without rows end at once.
+// The host knows no lengths, so every work-group works out the plan for itself: one sequence a lane, the row
+// tiles times token tiles of all of them give the length of a split (`chunk` token tiles) with which about
+// 2^target_log2 work-groups come out, however ragged the batch; a prefix sum finds the work-group's own sequence.
 //
 // On the matrix cores, v_mfma_f32_32x32x16_f16 throughout (lane l: c = l % 32, h = l / 32):
 //   logits   S^T = K Q^T: first operand 32 tokens, second operand 32 query rows; a lane gets of its row c the
@@ -39,14 +40,16 @@ struct RowsArgs {
   const int32_t* seq_lens;
   void* out;
   float* lse;
-  float* part_acc;          // [splits][slots][kv heads][kRows][D]
-  float* part_ml;           // [splits][slots][kv heads][kRows][2]: reference exponent, sum
+  float* part_acc;          // [units][kv heads][kRows][D]
+  float* part_ml;           // [units][kv heads][kRows][2]: reference exponent, sum
   const char* k_new;        // trees: keys and values of the drafted nodes
   const char* v_new;
   const int64_t* mask;      // trees: [rows of cu][mask_words]
   int64_t q_stride, new_stride;   // bytes between tokens
   int batch, max_pages, page_shift, kv_heads, group;
-  int slots, splits, mask_words, k_pages;
+  int mask_words, k_pages;
+  int target_log2;          // work-groups to come out, about; below 0: no splits
+  int least_chunk;          // token tiles of a split, at least
   int out_is_fp16;
   uint32_t q_sign;          // exclusive-ored onto q: sign bits where the scale is negative
   float scale_log2;         // |sm_scale| log2(e), not 0
@@ -60,31 +63,69 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t lds_short4_t;
 
-// The sequence and tile of a slot (see above); false: the slot has no rows.
-struct RowTile {
-  int b, first;        // sequence, first packed token of it
-  int tokens;          // its new tokens
-  int row0, rows;      // the tile's first row, rows of the sequence
+// The plan of one sequence, and where its units start.  A unit is a split of a row tile; sequence b's are in the order
+// split * row_tiles + row tile.
+struct Sequence {
+  int b, first, tokens, seq_len;   // first: its first packed row
+  int row_tiles, splits, chunk;
+  int before;                      // units (row tiles) of the sequences before
+  int units_before;
 };
-template <int kRows>
-__device__ __forceinline__ bool find_tile(RowTile& t, const int32_t* __restrict__ cu, int batch, int group, int slot,
-                                          int lane) {
-  int b = -1;
-  for (int base = 0; base < batch; base += kWave) {  // the last sequence that starts at or before the slot
-    const int i = base + lane;
-    const bool before = i < batch && (int64_t)cu[i < batch ? i : 0] * group / kRows + i <= slot;
-    const int n = __popcll(__ballot(before));
-    b += n;
-    if (n < kWave) break;
+// Finds the sequence of unit `want` (kByTile: of row tile `want`, counted over all sequences); false: there is none.
+template <bool kTree, int kRows, bool kByTile>
+__device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, const int32_t* __restrict__ cu,
+                                              const int32_t* __restrict__ seq_lens, bool list, int want, int lane) {
+  int first = 0, tokens = 0, seq_len = 0, row_tiles = 0, tiles = 0;
+  auto read = [&](int base) {
+    const int i = min(base + lane, a.batch - 1);
+    first = cu[i];
+    tokens = cu[i + 1] - first;
+    seq_len = seq_lens[i];
+    row_tiles = base + lane < a.batch ? (tokens * a.group + kRows - 1) / kRows : 0;
+    const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : seq_len;
+    tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
+  };
+  const int lanes = min(a.batch, kWave);  // sums over as many
+  int64_t all = 0;
+  for (int base = 0; base < a.batch; base += kWave) {
+    read(base);
+    all += (int64_t)row_tiles * tiles;
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  t.b = b;
-  t.first = cu[b];
-  t.tokens = cu[b + 1] - t.first;
-  t.rows = t.tokens * group;
-  const int tile = slot - (int)((int64_t)t.first * group / kRows) - b;
-  t.row0 = tile * kRows;
-  return t.row0 < t.rows;
+  for (int d = 1; d < lanes; d <<= 1) all += __shfl_xor(all, d);
+  all = ((int64_t)__builtin_amdgcn_readfirstlane((int)(all >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)all)) *
+        a.kv_heads;
+  const int64_t even = (all + (1ll << max(a.target_log2, 0)) - 1) >> max(a.target_log2, 0);
+  s.chunk = a.target_log2 < 0 || even > INT32_MAX ? INT32_MAX : max(a.least_chunk, (int)even);
+  int units_before = 0, tiles_before = 0;
+  for (int base = 0; base < a.batch; base += kWave) {
+    if (a.batch > kWave) read(base);
+    const int splits = tiles / s.chunk + (tiles % s.chunk != 0);
+    const int units = row_tiles * splits;
+    int u = units, t = row_tiles;   // inclusive sums
+    for (int d = 1; d < lanes; d <<= 1) {
+      const int uu = __shfl_up(u, d), tt = __shfl_up(t, d);
+      if (lane >= d) u += uu, t += tt;
+    }
+    u += units_before;
+    t += tiles_before;
+    const unsigned long long behind = __ballot((kByTile ? t : u) > want);  // (lanes without a sequence repeat the sum)
+    if (behind != 0) {
+      const int at = __builtin_ctzll(behind);
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+      s.b = base + at;
+      s.first = of(first);
+      s.tokens = of(tokens);
+      s.seq_len = of(seq_len);
+      s.row_tiles = of(row_tiles);
+      s.splits = of(splits);
+      s.units_before = of(u - units);
+      s.before = kByTile ? of(t - row_tiles) : s.units_before;
+      return true;
+    }
+    units_before = __builtin_amdgcn_readlane(u, lanes - 1);
+    tiles_before = __builtin_amdgcn_readlane(t, lanes - 1);
+  }
+  return false;
 }
 
 // Attention state of a wave's 32 rows; lane l: row l % 32.
@@ -129,6 +170,7 @@ struct RowState {
       }
     }
     if (masked) {
+      asm volatile("");  // a branch, not 32 selections in every tile
 #pragma unroll
       for (int t = 0; t < kBlocks; ++t) {
         const uint32_t bits = (uint32_t)(allow >> (32 * t)) >> ((lane >> 5) * 4);
@@ -224,6 +266,92 @@ __device__ __forceinline__ int k_place(int token, int slot) { return token * kRo
 __device__ __forceinline__ int v_place(int token, int slot) {
   return token * kRowBytes + ((slot ^ ((token & 3) << 2)) << 4);
 }
+
+// The first n of 64 bits.
+__device__ __forceinline__ uint64_t first_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+// The stream of tokens that a row tile of sequence b and KV head hk attends to.  Stream places 0, 1, .. are the
+// cached tokens in order, or those of the listed pages; (trees) from the next multiple of 64 on come the drafted nodes.
+// Four places from a multiple of 4 on lie in one page.
+template <bool kTree>
+struct Stream {
+  const int32_t* table;   // the sequence's page-table row
+  const int32_t* pages;   // its list, or null
+  int seq_len, seq_pages, listed, page_shift;
+  int limit;              // cached tokens (without a list): nothing behind them is looked at
+  int context;            // places before the drafted nodes
+  int first, nodes;       // the drafted nodes' first packed row, and how many
+  int tiles;              // of 64 places
+
+  // `last`: the last position that a row of the tile attends to (prompts).
+  __device__ __forceinline__ void init(const RowsArgs& a, const Sequence& s, int hk, int last,
+                                       const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk) {
+    table = page_table + (size_t)s.b * a.max_pages;
+    pages = kTree && topk != nullptr ? topk + ((size_t)s.b * a.kv_heads + hk) * a.k_pages : nullptr;
+    listed = min(a.k_pages, a.max_pages);
+    page_shift = a.page_shift;
+    seq_len = s.seq_len;
+    seq_pages = (seq_len + (1 << page_shift) - 1) >> page_shift;
+    limit = kTree ? seq_len : last + 1;
+    const int places = pages != nullptr ? listed << page_shift : max(limit, 0);
+    context = (places + kTileTokens - 1) & ~(kTileTokens - 1);
+    first = s.first;
+    nodes = kTree ? s.tokens : 0;
+    tiles = (context + nodes + kTileTokens - 1) / kTileTokens;
+  }
+  // What a lane knows of the four places from its `at` on: their physical page, and how many of them hold a token
+  // (any number).
+  struct Four {
+    int phys, count;
+  };
+  __device__ __forceinline__ Four find(int at) const {
+    if (kTree && at >= context) return {0, nodes - (at - context)};
+    if (pages != nullptr) {
+      const int entry = at >> page_shift;
+      const int page = entry < listed ? pages[entry] : -1;
+      if (page < 0 || page >= seq_pages) return {0, 0};
+      return {table[page], seq_len - (page << page_shift) - (at & ((1 << page_shift) - 1))};
+    }
+    return {table[min(at, limit - 1) >> page_shift], limit - at};
+  }
+  // 16 bytes of the key and of the value of place at + lane / 16, of the four that lane `from` has looked up.  A value
+  // that is not there is zero: stale slots may hold anything, and zero weights times that need not be zero.
+  __device__ __forceinline__ void load(const RowsArgs& a, int hk, int at, Four f, int from, int lane, uint4& key,
+                                       uint4& value) const {
+    const int sub = lane >> 4, chunk = (lane & 15) * 16;
+    const char *k = a.k_pool, *v = a.v_pool;
+    size_t off;
+    if (kTree && at >= context) {
+      k = a.k_new;
+      v = a.v_new;
+      off = (int64_t)(first + min(at - context + sub, nodes - 1)) * a.new_stride + (int64_t)hk * kRowBytes;
+    } else {
+      const int phys = __builtin_amdgcn_readlane(f.phys, from);
+      off = ((((size_t)phys * a.kv_heads + hk) << page_shift) + (at & ((1 << page_shift) - 1))) * kRowBytes +
+            sub * kRowBytes;
+    }
+    key = ld16(k + off + chunk);
+    value = ld16(v + off + chunk);
+    if (sub >= __builtin_amdgcn_readlane(f.count, from)) value = make_uint4(0, 0, 0, 0);
+  }
+  // Which of 64 places hold a token, lane g having looked up the g-th four of them.
+  __device__ __forceinline__ uint64_t held(Four f, int lane) const {
+    return __ballot((lane & 3) < __builtin_amdgcn_ds_bpermute(lane & ~3, f.count));
+  }
+  // Which of the 64 places from p0 (a multiple of 64) on a row attends to, of the `held` ones: those up to its
+  // position (prompts), all cached ones or those of its mask (trees).
+  __device__ __forceinline__ uint64_t allow(uint64_t held, int p0, int position, const int64_t* __restrict__ mask,
+                                            int mask_words) const {
+    if (!kTree) return first_bits(position + 1 - p0);
+    if (p0 < context) return held;
+    const int word = (p0 - context) / 64;
+    return word < mask_words ? (uint64_t)mask[word] & held : 0;
+  }
+  // Whether all rows from `position` on attend to all of those places.
+  __device__ __forceinline__ bool whole(uint64_t held, int p0, int position) const {
+    return kTree ? p0 < context && held == ~0ull : p0 + kTileTokens - 1 <= position;
+  }
+};
 
 #endif  // __HIPCC__
 
