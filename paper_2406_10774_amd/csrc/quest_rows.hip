@@ -17,7 +17,9 @@ namespace quest {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kSharedRows = 32 * kWaves;
+constexpr int kSharedWaves = 8;
+constexpr int kSharedRows = 32 * kSharedWaves;
+constexpr int kBuffers = 4;
 
 // A work-group's part: a unit of one KV head.  Adjacent work-groups have adjacent heads: with a multiple of eight KV heads
 // a head's units are all on one die, whose L2 then holds what its row tiles read at the same time.
@@ -28,7 +30,9 @@ struct Part {
   int hk, unit, row0, rows, past, group, first_tile, end_tile;
 
   // position of a row's token (of the last one's, from there on)
-  __device__ __forceinline__ int position(int row) const { return past + min(row, rows - 1) / group; }
+  __device__ __forceinline__ int position(int row) const {
+    return past + __builtin_amdgcn_readfirstlane(min(row, rows - 1) / group);
+  }
   __device__ __forceinline__ bool whole() const { return s.splits == 1; }   // the row tile has no other split
 
   __device__ __forceinline__ bool find(const RowsArgs& a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -51,13 +55,16 @@ struct Part {
   }
 };
 
-// Many rows: the next tile is on its way to registers while the waves work on the one in LDS.
+// Many rows.  Two waves on each SIMD: while one of them has matrix products to do, the other is at its softmax, by
+// turns that barriers keep: turn 2t is the first four waves' products (values of tile t - 1, logits of tile t) and
+// the other four's softmax of tile t - 1, in turn 2t + 1 they change places.  In its turn of softmax of tile t a wave
+// also puts its share of tile t + 2 into LDS; four buffers, as values of tile t - 1 are read until turn 2t + 1.
 template <bool kTree, bool kExact>
-__global__ __launch_bounds__(kWaves* kWave, 2) void shared_rows_kernel(
+__global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
-  constexpr int kLoads = kTileTokens / (4 * kWaves);
-  __shared__ __align__(16) char lds[2][2][kTileTokens * kRowBytes];
+  constexpr int kLoads = kTileTokens / (4 * kSharedWaves);
+  __shared__ __align__(16) char lds[kBuffers][2][kTileTokens * kRowBytes];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
   Part<kTree, kSharedRows> w;
@@ -66,53 +73,90 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void shared_rows_kernel(
   const bool there = row < w.rows;
   const int token = there ? row / a.group : 0;
   const int head = w.hk * a.group + (there ? row - token * a.group : 0);
-  const int wave_first = w.position(row0), wave_last = w.position(row0 + 31);
+  const int wave_first = w.position(row0);
 
   RowState<kExact> st;
   st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, there, a.q_sign, lane);
 
-  typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of a tile; load i is wave's place 16 i + 4 wave
-  uint64_t held = 0, held_next = 0;
+  typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of a tile
+  uint64_t held = 0, held1 = 0, held2 = 0, held3 = 0;   // of tiles t, t + 1, ..
   uint4 k[kLoads], v[kLoads];
+  bool token_there[kLoads];
   auto load = [&](int tile) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      w.stream.load(a, w.hk, tile * kTileTokens + (i * kWaves + wave) * 4, four, i * kWaves + wave, lane, k[i], v[i]);
-    if (kTree) held_next = w.stream.held(four, lane);
+      token_there[i] = w.stream.load(a, w.hk, tile * kTileTokens + (i * kSharedWaves + wave) * 4, four,
+                                     i * kSharedWaves + wave, lane, k[i], v[i]);
+    if (kTree) held3 = w.stream.held(four, lane);
   };
   auto find = [&](int tile) { four = w.stream.find(min(tile, w.end_tile - 1) * kTileTokens + (lane & 15) * 4); };
   auto store = [&](int buffer) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = (i * kWaves + wave) * 4 + (lane >> 4);
+      const int at = (i * kSharedWaves + wave) * 4 + (lane >> 4);
       st16(lds[buffer][0] + k_place(at, lane & 15), k[i]);
-      st16(lds[buffer][1] + v_place(at, lane & 15), v[i]);
+      st16(lds[buffer][1] + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
     }
   };
-  if (w.first_tile < w.end_tile) {
-    find(w.first_tile);
-    load(w.first_tile);
-    find(w.first_tile + 1);
+  const int first = w.first_tile, end = w.end_tile;
+  if (first < end) {
+    find(first);
+    load(first);
+    held = held3;
+    find(first + 1);
     store(0);
+    load(min(first + 1, end - 1));
+    held1 = held3;
+    find(first + 2);
+    store(1);
+    load(min(first + 2, end - 1));
+    held2 = held3;
+    find(first + 3);
     __syncthreads();
-    for (int tile = w.first_tile; tile < w.end_tile; ++tile) {
-      const int buffer = (tile - w.first_tile) & 1;
-      const bool more = tile + 1 < w.end_tile;
-      held = held_next;
-      if (more) {
-        load(tile + 1);
-        find(tile + 2);
-      }
-      const int p0 = tile * kTileTokens;
-      if (row0 < w.rows && (kTree || p0 <= wave_last)) {
-        const bool masked = !w.stream.whole(held, p0, wave_first);
-        uint64_t allow = ~0ull;
-        if (masked) allow = w.stream.allow(held, p0, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words);
-        st.template fold<2>(lds[buffer][0], lds[buffer][1], a.scale_log2, masked, allow, lane);
-      }
-      if (more) store(buffer ^ 1);
+    const bool second = wave >= kSharedWaves / 2;
+    if (second) __syncthreads();
+    auto stage = [&](int tile) {   // what a wave does for all of them in the turn of its softmax of `tile`
+      store((tile - first + 2) & (kBuffers - 1));
+      load(min(tile + 3, end - 1));
+      find(tile + 4);
+    };
+    auto turn = [] {
+      __builtin_amdgcn_sched_barrier(0);
       __syncthreads();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if (row0 < w.rows) {
+      typename RowState<kExact>::template Weights<2> p;
+      f32x16_t s[2];
+      auto softmax = [&](int tile) {
+        const int p0 = tile * kTileTokens;
+        if (!w.stream.whole(held, p0, wave_first))
+          st.hide(s, w.stream.allow(held, p0, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words), lane);
+        st.template weigh<2>(p, s, a.scale_log2);
+        held = held1, held1 = held2, held2 = held3;
+      };
+      st.template logits<2>(s, lds[0][0], lane);
+      turn();
+      stage(first);
+      softmax(first);
+      turn();
+      for (int tile = first + 1; tile < end; ++tile) {
+        st.template add<2>(p, lds[(tile - first - 1) & (kBuffers - 1)][1], lane);
+        st.template logits<2>(s, lds[(tile - first) & (kBuffers - 1)][0], lane);
+        turn();
+        stage(tile);
+        softmax(tile);
+        turn();
+      }
+      st.template add<2>(p, lds[(end - 1 - first) & (kBuffers - 1)][1], lane);
+    } else {
+      for (int tile = first; tile < end; ++tile) {
+        stage(tile);
+        turn();
+        turn();
+      }
     }
+    if (!second) __syncthreads();
   }
 
   if (!there) return;
@@ -164,10 +208,11 @@ __global__ __launch_bounds__(kWaves* kWave, kBlocks == 1 ? 2 : 1) void few_rows_
   typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of the tile of 64 that has the wave's 32
   uint64_t held = 0, held_next = 0;
   uint4 k[kLoads], v[kLoads];
+  bool token_there[kLoads];
   auto load = [&](int half) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      w.stream.load(a, w.hk, half * kTokens + i * 4, four, (half & 1) * kLoads + i, lane, k[i], v[i]);
+      token_there[i] = w.stream.load(a, w.hk, half * kTokens + i * 4, four, (half & 1) * kLoads + i, lane, k[i], v[i]);
     if (kTree) held_next = w.stream.held(four, lane);
   };
   auto find = [&](int half) { four = w.stream.find((min(half, end - 1) * kTokens & ~63) + (lane & 15) * 4); };
@@ -183,7 +228,7 @@ __global__ __launch_bounds__(kWaves* kWave, kBlocks == 1 ? 2 : 1) void few_rows_
     for (int i = 0; i < kLoads; ++i) {
       const int at = i * 4 + (lane >> 4);
       st16(stage_k + k_place(at, lane & 15), k[i]);
-      st16(stage_v + v_place(at, lane & 15), v[i]);
+      st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
     }
     lds_in_order();
     if (half + kWaves < end) {
@@ -323,7 +368,7 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree) {
   const int64_t mean = ((int64_t)total_tokens * group_size(c) + c.batch - 1) / c.batch;
   p.rows = mean <= 32 ? 32 : mean <= 64 ? 64 : kSharedRows;
   p.row_tiles = (int64_t)total_tokens * group_size(c) / p.rows + c.batch;
-  p.target_log2 = p.row_tiles * kv_heads(c) >= (tree ? 4096 : 512) ? -1 : 10;
+  p.target_log2 = p.row_tiles * kv_heads(c) >= (tree ? 4096 : 256) ? -1 : 10;
   p.least_chunk = p.rows == kSharedRows ? 8 : 4;
   return p;
 }
@@ -344,7 +389,7 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   a.least_chunk = p.least_chunk;
   a.part_acc = (float*)workspace;
   a.part_ml = a.part_acc + (size_t)units_of(p, c) * a.kv_heads * p.rows * kHeadDim;
-  const dim3 grid((unsigned)(units_of(p, c) * a.kv_heads)), block(kWaves * kWave);
+  const dim3 grid((unsigned)(units_of(p, c) * a.kv_heads)), block((p.rows == kSharedRows ? kSharedWaves : kWaves) * kWave);
   if (p.rows == 32)
     hipLaunchKernelGGL((few_rows_kernel<kTree, kExact, 1>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   else if (p.rows == 64)

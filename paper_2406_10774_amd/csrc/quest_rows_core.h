@@ -152,11 +152,9 @@ struct RowState {
     l = 0.f;
   }
 
-  // Fold a tile of 32 kBlocks tokens that lies in LDS.  masked: only the tokens of `allow` (bit t: token t of
-  // the tile; a lane's own) count.
+  // Logits of 32 kBlocks tokens that lie in LDS.
   template <int kBlocks>
-  __device__ __forceinline__ void fold(const char* k, const char* v, float scale, bool masked, uint64_t allow, int lane) {
-    f32x16_t s[kBlocks];
+  __device__ __forceinline__ void logits(f32x16_t (&s)[kBlocks], const char* k, int lane) const {
     const char* k_lane = k + (lane & 31) * kRowBytes;
     const int k_chunk = ((lane >> 5) ^ (lane & 15)) << 4;
 #pragma unroll
@@ -169,16 +167,25 @@ struct RowState {
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, key), q[i], s[t], 0, 0, 0);
       }
     }
-    if (masked) {
-      asm volatile("");  // a branch, not 32 selections in every tile
+  }
+  // Only the tokens of `allow` (bit t: token t; a lane's own) count.
+  template <int kBlocks>
+  __device__ __forceinline__ static void hide(f32x16_t (&s)[kBlocks], uint64_t allow, int lane) {
 #pragma unroll
-      for (int t = 0; t < kBlocks; ++t) {
-        const uint32_t bits = (uint32_t)(allow >> (32 * t)) >> ((lane >> 5) * 4);
+    for (int t = 0; t < kBlocks; ++t) {
+      const uint32_t bits = (uint32_t)(allow >> (32 * t)) >> ((lane >> 5) * 4);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!(bits >> (8 * (r / 4) + r % 4) & 1)) s[t][r] = -INFINITY;
-      }
+      for (int r = 0; r < 16; ++r)
+        if (!(bits >> (8 * (r / 4) + r % 4) & 1)) s[t][r] = -INFINITY;
     }
+  }
+  // The weights of 32 kBlocks tokens, as second operands of the products with their values.
+  template <int kBlocks>
+  struct Weights {
+    half8_t w[kBlocks * 2], rest[kExact ? kBlocks * 2 : 1];
+  };
+  template <int kBlocks>
+  __device__ __forceinline__ void weigh(Weights<kBlocks>& p, const f32x16_t (&s)[kBlocks], float scale) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
@@ -198,23 +205,26 @@ struct RowState {
         for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
     }
     float sum[2] = {0.f, 0.f};
-    half8_t w[kBlocks * 2], rest[kExact ? kBlocks * 2 : 1];
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], scale, -ref));
-        sum[r & 1] += p;
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], scale, -ref));
+        sum[r & 1] += x;
         if constexpr (kExact) {
-          const float scaled = p * kWeightScale;
+          const float scaled = x * kWeightScale;
           const _Float16 part = (_Float16)scaled;
-          w[2 * t + r / 8][r % 8] = part;
-          rest[2 * t + r / 8][r % 8] = (_Float16)(scaled - (float)part);
+          p.w[2 * t + r / 8][r % 8] = part;
+          p.rest[2 * t + r / 8][r % 8] = (_Float16)(scaled - (float)part);
         } else {
-          w[2 * t + r / 8][r % 8] = (_Float16)p;
+          p.w[2 * t + r / 8][r % 8] = (_Float16)x;
         }
       }
     l += sum[0] + sum[1];
+  }
+  // Add the weighted values, which lie in LDS.
+  template <int kBlocks>
+  __device__ __forceinline__ void add(const Weights<kBlocks>& p, const char* v, int lane) {
     // lane: token 4 h + (l % 16) / 4, channels 16 (l / 16 % 2) + 4 (l % 4) ..+3 of a block of 32
     const int quad = (lane >> 2) & 3;
     const char* v_lane = v + ((lane >> 5) * 4 + quad) * kRowBytes + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
@@ -227,9 +237,19 @@ struct RowState {
         const short4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(at + 8 * kRowBytes));
         const half8_t value =
             __builtin_bit_cast(half8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, w[i], acc[d], 0, 0, 0);
-        if constexpr (kExact) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, rest[i], acc[d], 0, 0, 0);
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, p.w[i], acc[d], 0, 0, 0);
+        if constexpr (kExact) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, p.rest[i], acc[d], 0, 0, 0);
       }
+  }
+  // All of it for a tile.
+  template <int kBlocks>
+  __device__ __forceinline__ void fold(const char* k, const char* v, float scale, bool masked, uint64_t allow, int lane) {
+    f32x16_t s[kBlocks];
+    logits(s, k, lane);
+    if (masked) hide(s, allow, lane);
+    Weights<kBlocks> p;
+    weigh(p, s, scale);
+    add(p, v, lane);
   }
 
   // The row's whole sum and what the accumulators have to be multiplied by.
@@ -314,25 +334,24 @@ struct Stream {
     }
     return {table[min(at, limit - 1) >> page_shift], limit - at};
   }
-  // 16 bytes of the key and of the value of place at + lane / 16, of the four that lane `from` has looked up.  A value
-  // that is not there is zero: stale slots may hold anything, and zero weights times that need not be zero.
-  __device__ __forceinline__ void load(const RowsArgs& a, int hk, int at, Four f, int from, int lane, uint4& key,
+  // 16 bytes of the key and of the value of place at + lane / 16, of the four that lane `from` has looked up.  Returns
+  // whether there is a token; if not, the value has to be zeroed when it has arrived: stale slots may hold anything, and
+  // zero weights times that need not be zero.
+  __device__ __forceinline__ bool load(const RowsArgs& a, int hk, int at, Four f, int from, int lane, uint4& key,
                                        uint4& value) const {
-    const int sub = lane >> 4, chunk = (lane & 15) * 16;
-    const char *k = a.k_pool, *v = a.v_pool;
-    size_t off;
+    const int sub = lane >> 4;
     if (kTree && at >= context) {
-      k = a.k_new;
-      v = a.v_new;
-      off = (int64_t)(first + min(at - context + sub, nodes - 1)) * a.new_stride + (int64_t)hk * kRowBytes;
+      const int64_t off = (int64_t)(first + min(at - context + sub, nodes - 1)) * a.new_stride + (int64_t)hk * kRowBytes +
+                          (lane & 15) * 16;
+      key = ld16(a.k_new + off);
+      value = ld16(a.v_new + off);
     } else {
       const int phys = __builtin_amdgcn_readlane(f.phys, from);
-      off = ((((size_t)phys * a.kv_heads + hk) << page_shift) + (at & ((1 << page_shift) - 1))) * kRowBytes +
-            sub * kRowBytes;
+      const int64_t row = (((int64_t)phys * a.kv_heads + hk) << page_shift) + (at & ((1 << page_shift) - 1));
+      key = ld16(a.k_pool + row * kRowBytes + lane * 16);   // four rows of 256 bytes
+      value = ld16(a.v_pool + row * kRowBytes + lane * 16);
     }
-    key = ld16(k + off + chunk);
-    value = ld16(v + off + chunk);
-    if (sub >= __builtin_amdgcn_readlane(f.count, from)) value = make_uint4(0, 0, 0, 0);
+    return sub < __builtin_amdgcn_readlane(f.count, from);
   }
   // Which of 64 places hold a token, lane g having looked up the g-th four of them.
   __device__ __forceinline__ uint64_t held(Four f, int lane) const {
