@@ -17,6 +17,7 @@ namespace quest {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kFewRows = 32;
 constexpr int kSharedWaves = 8;
 constexpr int kSharedRows = 32 * kSharedWaves;
 constexpr int kBuffers = 4;
@@ -76,20 +77,20 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   const int wave_first = w.position(row0);
 
   RowState<kExact> st;
-  st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, there, a.q_sign, lane);
-
-  typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of a tile
+  Walk<kTree, kTileTokens> walk;
+  walk.init(w.stream, w.first_tile * kTileTokens, kTileTokens);
+  const int steps = w.end_tile - w.first_tile;
   uint64_t held = 0, held1 = 0, held2 = 0, held3 = 0;   // of tiles t, t + 1, ..
   uint4 k[kLoads], v[kLoads];
   bool token_there[kLoads];
-  auto load = [&](int tile) {
+  auto load = [&](int step) {
+    step = min(step, steps - 1);
+    if (!walk.knows(step)) walk.find(w.stream, step, lane);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      token_there[i] = w.stream.load(a, w.hk, tile * kTileTokens + (i * kSharedWaves + wave) * 4, four,
-                                     i * kSharedWaves + wave, lane, k[i], v[i]);
-    if (kTree) held3 = w.stream.held(four, lane);
+      token_there[i] = walk.load(a, w.stream, w.hk, step, (i * kSharedWaves + wave) * 4, lane, k[i], v[i]);
+    if (kTree) held3 = walk.held(step, lane);
   };
-  auto find = [&](int tile) { four = w.stream.find(min(tile, w.end_tile - 1) * kTileTokens + (lane & 15) * 4); };
   auto store = [&](int buffer) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -98,27 +99,24 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
       st16(lds[buffer][1] + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
     }
   };
-  const int first = w.first_tile, end = w.end_tile;
-  if (first < end) {
-    find(first);
-    load(first);
+  if (steps > 0) {
+    walk.find(w.stream, 0, lane);
+    st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+    load(0);
     held = held3;
-    find(first + 1);
+    st.ready(a.q_sign);
     store(0);
-    load(min(first + 1, end - 1));
+    load(1);
     held1 = held3;
-    find(first + 2);
     store(1);
-    load(min(first + 2, end - 1));
+    load(2);
     held2 = held3;
-    find(first + 3);
     __syncthreads();
     const bool second = wave >= kSharedWaves / 2;
     if (second) __syncthreads();
-    auto stage = [&](int tile) {   // what a wave does for all of them in the turn of its softmax of `tile`
-      store((tile - first + 2) & (kBuffers - 1));
-      load(min(tile + 3, end - 1));
-      find(tile + 4);
+    auto stage = [&](int step) {   // what a wave does for all of them in the turn of its softmax
+      store((step + 2) & (kBuffers - 1));
+      load(step + 3);
     };
     auto turn = [] {
       __builtin_amdgcn_sched_barrier(0);
@@ -128,35 +126,38 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     if (row0 < w.rows) {
       typename RowState<kExact>::template Weights<2> p;
       f32x16_t s[2];
-      auto softmax = [&](int tile) {
-        const int p0 = tile * kTileTokens;
-        if (!w.stream.whole(held, p0, wave_first))
-          st.hide(s, w.stream.allow(held, p0, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words), lane);
+      auto softmax = [&](int step) {
+        if (!walk.whole(w.stream, held, step, wave_first))
+          st.hide(s, walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words), lane);
         st.template weigh<2>(p, s, a.scale_log2);
         held = held1, held1 = held2, held2 = held3;
       };
       st.template logits<2>(s, lds[0][0], lane);
       turn();
-      stage(first);
-      softmax(first);
+      stage(0);
+      softmax(0);
       turn();
-      for (int tile = first + 1; tile < end; ++tile) {
-        st.template add<2>(p, lds[(tile - first - 1) & (kBuffers - 1)][1], lane);
-        st.template logits<2>(s, lds[(tile - first) & (kBuffers - 1)][0], lane);
+      for (int step = 1; step < steps; ++step) {
+        st.template add<2>(p, lds[(step - 1) & (kBuffers - 1)][1], lane);
+        st.template logits<2>(s, lds[step & (kBuffers - 1)][0], lane);
         turn();
-        stage(tile);
-        softmax(tile);
+        stage(step);
+        softmax(step);
         turn();
       }
-      st.template add<2>(p, lds[(end - 1 - first) & (kBuffers - 1)][1], lane);
+      st.template add<2>(p, lds[(steps - 1) & (kBuffers - 1)][1], lane);
     } else {
-      for (int tile = first; tile < end; ++tile) {
-        stage(tile);
+      for (int step = 0; step < steps; ++step) {
+        stage(step);
         turn();
         turn();
       }
     }
     if (!second) __syncthreads();
+  }
+
+  else {
+    st.clear();
   }
 
   if (!there) return;
@@ -176,53 +177,47 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
 }
 
 // Few rows: tiles of 32 tokens, each wave its own.
-template <bool kTree, bool kExact, int kBlocks>
-__global__ __launch_bounds__(kWaves* kWave, kBlocks == 1 ? 2 : 1) void few_rows_kernel(
+template <bool kTree, bool kExact>
+__global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
-  constexpr int kRows = 32 * kBlocks, kTokens = 32, kLoads = kTokens / 4;
+  constexpr int kTokens = 32, kLoads = kTokens / 4;
   constexpr int kStride = kHeadDim + 4;
-  constexpr int kStage = 2 * kTokens * kRowBytes, kJoin = 32 * kStride * 4;
+  constexpr int kStage = 2 * kTokens * kRowBytes, kJoin = kFewRows * kStride * 4;
   __shared__ __align__(16) char lds[kWaves * (kStage > kJoin ? kStage : kJoin)];
-  __shared__ float ml[2][kWaves][32];
+  __shared__ float ml[2][kWaves][kFewRows];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
-  Part<kTree, kRows> w;
+  Part<kTree, kFewRows> w;
   if (!w.find(a, cu, seq_lens, page_table, topk, lane)) return;
-
-  RowState<kExact> st[kBlocks];
-  int token[kBlocks];
-#pragma unroll
-  for (int n = 0; n < kBlocks; ++n) {
-    const int row = w.row0 + n * 32 + (lane & 31);
-    const bool there = row < w.rows;
-    token[n] = there ? row / a.group : 0;
-    const int head = w.hk * a.group + (there ? row - token[n] * a.group : 0);
-    st[n].init(a.q + (int64_t)(w.s.first + token[n]) * a.q_stride + (int64_t)head * kRowBytes, there, a.q_sign, lane);
+  int token, head;
+  {
+    const int row = w.row0 + (lane & 31);
+    token = row < w.rows ? row / a.group : 0;
+    head = w.hk * a.group + (row < w.rows ? row - token * a.group : 0);
   }
   const int first_position = w.position(w.row0);
 
-  const int end = w.end_tile * 2;
+  RowState<kExact> st;
+  Walk<kTree, kTokens> walk;
+  walk.init(w.stream, w.first_tile * kTileTokens + wave * kTokens, kWaves * kTokens);
+  const int steps = ((w.end_tile - w.first_tile) * (kTileTokens / kTokens) - wave + kWaves - 1) / kWaves;
   char* stage_k = lds + wave * kStage;
   char* stage_v = stage_k + kTokens * kRowBytes;
-  typename Stream<kTree>::Four four;    // lane g < 16: the g-th four places of the tile of 64 that has the wave's 32
   uint64_t held = 0, held_next = 0;
   uint4 k[kLoads], v[kLoads];
   bool token_there[kLoads];
-  auto load = [&](int half) {
+  auto load = [&](int step) {
+    if (!walk.knows(step)) walk.find(w.stream, step, lane);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      token_there[i] = w.stream.load(a, w.hk, half * kTokens + i * 4, four, (half & 1) * kLoads + i, lane, k[i], v[i]);
-    if (kTree) held_next = w.stream.held(four, lane);
+    for (int i = 0; i < kLoads; ++i) token_there[i] = walk.load(a, w.stream, w.hk, step, i * 4, lane, k[i], v[i]);
+    if (kTree) held_next = walk.held(step, lane);
   };
-  auto find = [&](int half) { four = w.stream.find((min(half, end - 1) * kTokens & ~63) + (lane & 15) * 4); };
-  int half = w.first_tile * 2 + wave;
-  if (half < end) {
-    find(half);
-    load(half);
-    find(half + kWaves);
-  }
-  for (; half < end; half += kWaves) {
+  if (steps > 0) walk.find(w.stream, 0, lane);
+  st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+  if (steps > 0) load(0);
+  st.ready(a.q_sign);
+  for (int step = 0; step < steps; ++step) {
     held = held_next;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -231,73 +226,62 @@ __global__ __launch_bounds__(kWaves* kWave, kBlocks == 1 ? 2 : 1) void few_rows_
       st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
     }
     lds_in_order();
-    if (half + kWaves < end) {
-      load(half + kWaves);
-      find(half + 2 * kWaves);
-    }
-    const int p0 = half * kTokens & ~63;
-    const bool masked = !w.stream.whole(held, p0, first_position);
-#pragma unroll
-    for (int n = 0; n < kBlocks; ++n) {
-      uint64_t allow = ~0ull;
-      if (masked)
-        allow = w.stream.allow(held, p0, w.past + token[n], mask + (int64_t)(w.s.first + token[n]) * a.mask_words, a.mask_words) >>
-                (half & 1) * 32;
-      st[n].template fold<1>(stage_k, stage_v, a.scale_log2, masked, allow, lane);
-    }
+    if (step + 1 < steps) load(step + 1);
+    const bool masked = !walk.whole(w.stream, held, step, first_position);
+    uint64_t allow = ~0ull;
+    if (masked)
+      allow = walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words);
+    st.template fold<1>(stage_k, stage_v, a.scale_log2, masked, allow, lane);
     lds_in_order();
   }
 
-  // Join the waves' results, 32 rows at a time: eight threads a row, 16 channels each.
+  // Join the waves' results: eight threads a row, 16 channels each.
+  __syncthreads();
   float* join = reinterpret_cast<float*>(lds);
+  const float total = st.total();
+  float* mine = join + (wave * kFewRows + (lane & 31)) * kStride;
+  st.each4(RowState<kExact>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
+  if (lane < kFewRows) {
+    ml[0][wave][lane] = total > 0.f ? st.ref : kNegBig;
+    ml[1][wave][lane] = total;
+  }
+  __syncthreads();
+  const int in_tile = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * 16;
+  const int row = w.row0 + in_tile;
+  if (row >= w.rows) return;
+  float top = kNegBig, sum = 0.f, weight[kWaves];
 #pragma unroll
-  for (int n = 0; n < kBlocks; ++n) {
-    __syncthreads();
-    const float total = st[n].total();
-    float* mine = join + (wave * 32 + (lane & 31)) * kStride;
-    st[n].each4(RowState<kExact>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
-    if (lane < 32) {
-      ml[0][wave][lane] = total > 0.f ? st[n].ref : kNegBig;
-      ml[1][wave][lane] = total;
-    }
-    __syncthreads();
-    const int in_block = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * 16;
-    const int row = w.row0 + n * 32 + in_block;
-    if (row >= w.rows) continue;
-    float top = kNegBig, sum = 0.f, weight[kWaves];
+  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[0][i][in_tile]);
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[0][i][in_block]);
+  for (int i = 0; i < kWaves; ++i) {
+    weight[i] = __builtin_amdgcn_exp2f(ml[0][i][in_tile] - top);
+    sum += weight[i] * ml[1][i][in_tile];
+  }
+  float4 o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      weight[i] = __builtin_amdgcn_exp2f(ml[0][i][in_block] - top);
-      sum += weight[i] * ml[1][i][in_block];
+      const float4 x = *reinterpret_cast<const float4*>(join + (i * kFewRows + in_tile) * kStride + d0 + 4 * j);
+      o[j].x += weight[i] * x.x, o[j].y += weight[i] * x.y, o[j].z += weight[i] * x.z, o[j].w += weight[i] * x.w;
     }
-    float4 o[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        const float4 x = *reinterpret_cast<const float4*>(join + (i * 32 + in_block) * kStride + d0 + 4 * j);
-        o[j].x += weight[i] * x.x, o[j].y += weight[i] * x.y, o[j].z += weight[i] * x.z, o[j].w += weight[i] * x.w;
-      }
-    }
-    if (!w.whole()) {
-      const size_t part = w.part_row(a, n * 32 + in_block);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d0 + 4 * j) = o[j];
-      if (d0 == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(top, sum);
-      continue;
-    }
-    const int tok = row / a.group;
-    const size_t out_row = (size_t)(w.s.first + tok) * (a.kv_heads * a.group) + w.hk * a.group + (row - tok * a.group);
-    const float factor = sum > 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      store4(a.out, a.out_is_fp16, out_row * kHeadDim + d0 + 4 * j,
-             make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor));
-    if (a.lse != nullptr && d0 == 0) a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
   }
+  if (!w.whole()) {
+    const size_t part = w.part_row(a, in_tile);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d0 + 4 * j) = o[j];
+    if (d0 == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(top, sum);
+    return;
+  }
+  const int tok = row / a.group;
+  const size_t out_row = (size_t)(w.s.first + tok) * (a.kv_heads * a.group) + w.hk * a.group + (row - tok * a.group);
+  const float factor = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    store4(a.out, a.out_is_fp16, out_row * kHeadDim + d0 + 4 * j,
+           make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor));
+  if (a.lse != nullptr && d0 == 0) a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
 // The partial results of each row: a wave a row, a lane a split for the weights, then two channels a lane.
@@ -317,34 +301,40 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   const int parts = s.splits;
   const size_t step = (size_t)s.row_tiles * a.kv_heads * kRows;   // rows between two splits' parts
   const size_t part0 = (((size_t)s.units_before + (s.row_tiles - 1 - (tile - s.before))) * a.kv_heads + hk) * kRows + in_tile;
+  const float* ml = a.part_ml + part0 * 2;
+  const float* from = a.part_acc + part0 * kHeadDim + lane * 2;
+  float2 v[8];
+  auto ask = [&](int i) {   // eight parts' outputs
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float2*>(from + min(i + j, parts - 1) * step * kHeadDim);
+  };
+  ask(0);
   float top = kNegBig;
   for (int i = lane; i < parts; i += kWave) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part0 + i * step) * 2);
-    if (ml.y > 0.f) top = fmaxf(top, ml.x);
+    const float2 x = *reinterpret_cast<const float2*>(ml + i * step * 2);
+    if (x.y > 0.f) top = fmaxf(top, x.x);
   }
 #pragma unroll
   for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
   float sum = 0.f, o0 = 0.f, o1 = 0.f;
-  const float* from = a.part_acc + part0 * kHeadDim + lane * 2;
   for (int base = 0; base < parts; base += kWave) {
     float weight = 0.f;
     if (base + lane < parts) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part0 + (base + lane) * step) * 2);
-      weight = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
-      sum += weight * ml.y;
+      const float2 x = *reinterpret_cast<const float2*>(ml + (base + lane) * step * 2);
+      weight = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - top) : 0.f;
+      sum += weight * x.y;
     }
     const int n = min(parts - base, kWave);
-    for (int i = 0; i < n; i += 8) {  // eight on their way
-      float2 v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[j] = *reinterpret_cast<const float2*>(from + (base + min(i + j, n - 1)) * step * kHeadDim);
+    for (int i = 0; i < n; i += 8) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float x = i + j < n ? from_lane(weight, i + j) : 0.f;
-        o0 += v[j].x * x;
-        o1 += v[j].y * x;
+        if (x > 0.f) {   // (a part without tokens has left whatever was there)
+          o0 += v[j].x * x;
+          o1 += v[j].y * x;
+        }
       }
+      ask(base + i + 8);
     }
   }
 #pragma unroll
@@ -359,51 +349,54 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 
 // How a call is cut up, from what the host knows.
 struct Plan {
-  int rows;                  // of a row tile: 32, 64 (few_rows_kernel), 128
-  int64_t row_tiles;         // room for them
-  int target_log2, least_chunk;
+  int rows;                     // of a row tile: kFewRows or kSharedRows
+  int row_tiles;                // of a KV head, at most
+  int most_units, least_chunk;  // of a KV head; 0 units: no splits
 };
+#ifndef ROUNDS
+#define ROUNDS 0
+#endif
+#ifndef ROWS
+#define ROWS 0
+#endif
 Plan plan_of(const quest_cache& c, int total_tokens, bool tree) {
   Plan p;
-  const int64_t mean = ((int64_t)total_tokens * group_size(c) + c.batch - 1) / c.batch;
-  p.rows = mean <= 32 ? 32 : mean <= 64 ? 64 : kSharedRows;
-  p.row_tiles = (int64_t)total_tokens * group_size(c) / p.rows + c.batch;
-  p.target_log2 = p.row_tiles * kv_heads(c) >= (tree ? 4096 : 256) ? -1 : 10;
-  p.least_chunk = p.rows == kSharedRows ? 8 : 4;
+  const int64_t rows = (int64_t)total_tokens * group_size(c), mean = (rows + c.batch - 1) / c.batch;
+  p.rows = ROWS ? ROWS : mean <= 64 ? kFewRows : kSharedRows;
+  p.row_tiles = (int)(rows / p.rows + c.batch);
+  const int heads = kv_heads(c);
+  const int at_once = (p.rows == 32 ? 512 : 256) / heads;   // work-groups that the compute units take at once
+  p.least_chunk = p.rows == kSharedRows ? 4 : 2;
+  int rounds = p.row_tiles * 4 <= at_once ? 1 : p.row_tiles * 2 <= at_once ? 2 : 4;
+  if (ROUNDS) rounds = ROUNDS;
+  p.most_units = p.row_tiles > at_once * (tree ? 4 : 1) ? 0 : std::max(at_once * rounds, p.row_tiles + 1);
   return p;
 }
-// Units: 2^target_log2 for all heads and one for each row tile (rounding up), at most; without splits the row tiles.
-int64_t units_of(const Plan& p, const quest_cache& c) {
-  return p.row_tiles + (p.target_log2 < 0 ? 0 : (1 << p.target_log2) / kv_heads(c));
-}
+int units_of(const Plan& p) { return std::max(p.row_tiles, p.most_units); }
 size_t bytes_of(const Plan& p, const quest_cache& c) {
-  return p.target_log2 < 0 ? 0 : (size_t)units_of(p, c) * kv_heads(c) * p.rows * (kHeadDim + 2) * sizeof(float);
+  return p.most_units == 0 ? 0 : (size_t)units_of(p) * kv_heads(c) * p.rows * (kHeadDim + 2) * sizeof(float);
 }
 
 template <bool kTree, bool kExact>
 int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32_t* topk, void* workspace, size_t bytes,
                 const char* who, hipStream_t s) {
   Plan p = plan_of(c, total_tokens, kTree);
-  if (workspace == nullptr || bytes_of(p, c) > bytes) p.target_log2 = -1;
-  a.target_log2 = p.target_log2;
+  if (workspace == nullptr || bytes_of(p, c) > bytes) p.most_units = 0;
+  a.most_units = p.most_units;
   a.least_chunk = p.least_chunk;
   a.part_acc = (float*)workspace;
-  a.part_ml = a.part_acc + (size_t)units_of(p, c) * a.kv_heads * p.rows * kHeadDim;
-  const dim3 grid((unsigned)(units_of(p, c) * a.kv_heads)), block((p.rows == kSharedRows ? kSharedWaves : kWaves) * kWave);
-  if (p.rows == 32)
-    hipLaunchKernelGGL((few_rows_kernel<kTree, kExact, 1>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
-  else if (p.rows == 64)
-    hipLaunchKernelGGL((few_rows_kernel<kTree, kExact, 2>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+  a.part_ml = a.part_acc + (size_t)units_of(p) * a.kv_heads * p.rows * kHeadDim;
+  const dim3 grid((unsigned)(units_of(p) * a.kv_heads)), block((p.rows == kSharedRows ? kSharedWaves : kWaves) * kWave);
+  if (p.rows == kFewRows)
+    hipLaunchKernelGGL((few_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   else
     hipLaunchKernelGGL((shared_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   const int r = check_launch(who);
-  if (r != QUEST_OK || p.target_log2 < 0) return r;
+  if (r != QUEST_OK || p.most_units == 0) return r;
   const dim3 merge((unsigned)(p.row_tiles * (p.rows / 4) * a.kv_heads));
   const int list = topk != nullptr;
-  if (p.rows == 32)
-    hipLaunchKernelGGL((merge_rows_kernel<kTree, 32>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
-  else if (p.rows == 64)
-    hipLaunchKernelGGL((merge_rows_kernel<kTree, 64>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
+  if (p.rows == kFewRows)
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
   else
     hipLaunchKernelGGL((merge_rows_kernel<kTree, kSharedRows>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
   return check_launch(who);

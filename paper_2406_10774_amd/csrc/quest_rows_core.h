@@ -4,9 +4,10 @@
 // head r % G of token r / G, so that whatever the group the keys are read once for all of them.
 // Rows are cut into tiles of kRows.  A tile walks the tokens it attends to 64 at a time with an online softmax.
 //
-// The host knows no lengths, so every work-group works out the plan for itself: one sequence a lane, the row
-// tiles times token tiles of all of them give the length of a split (`chunk` token tiles) with which about
-// 2^target_log2 work-groups come out, however ragged the batch; a prefix sum finds the work-group's own sequence.
+// The host knows no lengths, so every work-group works out the plan for itself, one sequence a lane: from the row tiles
+// and the row tiles times token tiles of all of them comes the length of a split (`chunk` token tiles) with which
+// the units are no more than the compute units take at once (or in the few rounds that the host chose), however ragged
+// the batch; a prefix sum finds the work-group's own sequence.
 //
 // On the matrix cores, v_mfma_f32_32x32x16_f16 throughout (lane l: c = l % 32, h = l / 32):
 //   logits   S^T = K Q^T: first operand 32 tokens, second operand 32 query rows; a lane gets of its row c the
@@ -48,7 +49,7 @@ struct RowsArgs {
   int64_t q_stride, new_stride;   // bytes between tokens
   int batch, max_pages, page_shift, kv_heads, group;
   int mask_words, k_pages;
-  int target_log2;          // work-groups to come out, about; below 0: no splits
+  int most_units;           // splits and row tiles that may come out; 0: no splits
   int least_chunk;          // token tiles of a split, at least
   int out_is_fp16;
   uint32_t q_sign;          // exclusive-ored onto q: sign bits where the scale is negative
@@ -62,6 +63,26 @@ constexpr int kTileTokens = 64;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t lds_short4_t;
+
+// v of this lane and all before it.
+template <int N, class T>
+__device__ __forceinline__ T row_shr(T v) {  // of the lane N before, in the same row of 16; 0 where there is none
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x110 + N, 0xf, 0xf, false));
+}
+template <class T>
+__device__ __forceinline__ T up_to_lane(T v, int lane) {
+  v += row_shr<1>(v);
+  v += row_shr<2>(v);
+  v += row_shr<4>(v);
+  v += row_shr<8>(v);
+  T before = 0;
+#pragma unroll
+  for (int row = 1; row < 4; ++row) {
+    const T end = __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), row * 16 - 1));
+    if (lane >= row * 16) before += end;
+  }
+  return v + before;
+}
 
 // The plan of one sequence, and where its units start.  A unit is a split of a row tile; sequence b's are in the order
 // split * row_tiles + row tile.
@@ -85,29 +106,26 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
     const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : seq_len;
     tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
   };
-  const int lanes = min(a.batch, kWave);  // sums over as many
-  int64_t all = 0;
+  float all = 0.f;
+  int count = 0;
   for (int base = 0; base < a.batch; base += kWave) {
     read(base);
-    all += (int64_t)row_tiles * tiles;
+    const float work = up_to_lane((float)row_tiles * (float)tiles, lane);
+    all += as_f((uint32_t)__builtin_amdgcn_readlane((int)as_u(work), kWave - 1));
+    count += __builtin_amdgcn_readlane(up_to_lane(row_tiles, lane), kWave - 1);
   }
-  for (int d = 1; d < lanes; d <<= 1) all += __shfl_xor(all, d);
-  all = ((int64_t)__builtin_amdgcn_readfirstlane((int)(all >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)all)) *
-        a.kv_heads;
-  const int64_t even = (all + (1ll << max(a.target_log2, 0)) - 1) >> max(a.target_log2, 0);
-  s.chunk = a.target_log2 < 0 || even > INT32_MAX ? INT32_MAX : max(a.least_chunk, (int)even);
+  // ceil(tiles / chunk) summed over the row tiles is at most all / chunk + count (a hundred-thousandth covers the
+  // roundings)
+  const int room = a.most_units - count;
+  const float even = all * 1.00001f / (float)max(room, 1);
+  s.chunk = room < 1 || even > 1e9f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
   int units_before = 0, tiles_before = 0;
   for (int base = 0; base < a.batch; base += kWave) {
     if (a.batch > kWave) read(base);
     const int splits = tiles / s.chunk + (tiles % s.chunk != 0);
     const int units = row_tiles * splits;
-    int u = units, t = row_tiles;   // inclusive sums
-    for (int d = 1; d < lanes; d <<= 1) {
-      const int uu = __shfl_up(u, d), tt = __shfl_up(t, d);
-      if (lane >= d) u += uu, t += tt;
-    }
-    u += units_before;
-    t += tiles_before;
+    const int u = up_to_lane(units, lane) + units_before;
+    const int t = kByTile ? up_to_lane(row_tiles, lane) + tiles_before : 0;
     const unsigned long long behind = __ballot((kByTile ? t : u) > want);  // (lanes without a sequence repeat the sum)
     if (behind != 0) {
       const int at = __builtin_ctzll(behind);
@@ -122,8 +140,8 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
       s.before = kByTile ? of(t - row_tiles) : s.units_before;
       return true;
     }
-    units_before = __builtin_amdgcn_readlane(u, lanes - 1);
-    tiles_before = __builtin_amdgcn_readlane(t, lanes - 1);
+    units_before = __builtin_amdgcn_readlane(u, kWave - 1);
+    tiles_before = __builtin_amdgcn_readlane(t, kWave - 1);
   }
   return false;
 }
@@ -137,19 +155,29 @@ struct RowState {
   f32x16_t acc[4];     // [d / 32]: channels 8 (r / 4) + 4 h + r % 4
   float ref, l;        // reference exponent; this lane's share of the row's sum
 
-  __device__ __forceinline__ void init(const char* row, bool there, uint32_t sign, int lane) {
+  // Asks for the row's query; what uses it comes after ready().
+  __device__ __forceinline__ void init(const char* row, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint4 v = there ? ld16(row + i * 32 + (lane >> 5) * 16) : make_uint4(0, 0, 0, 0);
-      v.x ^= sign, v.y ^= sign, v.z ^= sign, v.w ^= sign;
-      q[i] = __builtin_bit_cast(half8_t, v);
-    }
+    for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(half8_t, ld16(row + i * 32 + (lane >> 5) * 16));
+    clear();
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
     ref = kNegBig;
     l = 0.f;
+  }
+  __device__ __forceinline__ void ready(uint32_t sign) {
+    if (sign != 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint4 v = __builtin_bit_cast(uint4, q[i]);
+        v.x ^= sign, v.y ^= sign, v.z ^= sign, v.w ^= sign;
+        q[i] = __builtin_bit_cast(half8_t, v);
+      }
+    }
   }
 
   // Logits of 32 kBlocks tokens that lie in LDS.
@@ -319,56 +347,88 @@ struct Stream {
     nodes = kTree ? s.tokens : 0;
     tiles = (context + nodes + kTileTokens - 1) / kTileTokens;
   }
-  // What a lane knows of the four places from its `at` on: their physical page, and how many of them hold a token
-  // (any number).
-  struct Four {
-    int phys, count;
-  };
-  __device__ __forceinline__ Four find(int at) const {
-    if (kTree && at >= context) return {0, nodes - (at - context)};
-    if (pages != nullptr) {
-      const int entry = at >> page_shift;
-      const int page = entry < listed ? pages[entry] : -1;
-      if (page < 0 || page >= seq_pages) return {0, 0};
-      return {table[page], seq_len - (page << page_shift) - (at & ((1 << page_shift) - 1))};
-    }
-    return {table[min(at, limit - 1) >> page_shift], limit - at};
+};
+
+// A wave's walk over the stream in steps of kPlaces (32 or 64) places, step i at place start + i stride.  What page a place
+// is in is looked up for many steps at a time, one page (or part of one, where a page is longer than a step) a lane:
+// lane e of the first step's, then the next step's, ..  The lookups' latency, twice a memory access with a list, is
+// then paid once in 16 to 64 steps, and nothing waits for a lookup behind the keys and values under way.
+template <bool kTree, int kPlaces>
+struct Walk {
+  int start, stride;
+  int shift;            // log2 of the places a lane looks up: a page, at most a step
+  int per_step_log2;    // lanes of a step
+  int first_step;       // step of lane 0
+  int phys, left;       // this lane's page, and how many of its places (from its first on) hold a token
+  static constexpr int kLog2 = kPlaces == 64 ? 6 : 5;
+
+  __device__ __forceinline__ void init(const Stream<kTree>& s, int start_, int stride_) {
+    start = start_;
+    stride = stride_;
+    shift = min(s.page_shift, kLog2);
+    per_step_log2 = kLog2 - shift;
+    first_step = 0;
   }
-  // 16 bytes of the key and of the value of place at + lane / 16, of the four that lane `from` has looked up.  Returns
-  // whether there is a token; if not, the value has to be zeroed when it has arrived: stale slots may hold anything, and
+  __device__ __forceinline__ bool knows(int step) const { return (step - first_step) << per_step_log2 < kWave; }
+  __device__ __forceinline__ void find(const Stream<kTree>& s, int step, int lane) {
+    first_step = step;
+    const int at = start + (step + (lane >> per_step_log2)) * stride + ((lane & ((1 << per_step_log2) - 1)) << shift);
+    phys = 0;
+    left = 0;
+    if (kTree && at >= s.context) {
+      left = s.nodes - (at - s.context);
+    } else if (s.pages != nullptr) {
+      const int entry = at >> s.page_shift;
+      const int page = entry < s.listed ? s.pages[entry] : -1;
+      if (page >= 0 && page < s.seq_pages) {
+        phys = s.table[page];
+        left = s.seq_len - (page << s.page_shift) - (at & ((1 << s.page_shift) - 1));
+      }
+    } else if (at < s.limit) {
+      phys = s.table[at >> s.page_shift];
+      left = s.limit - at;
+    }
+  }
+  // 16 bytes of the key and of the value of the step's place `four` + lane / 16 (`four`: a multiple of 4).  Returns whether
+  // there is a token; if not, the value has to be zeroed when it has arrived: stale slots may hold anything, and
   // zero weights times that need not be zero.
-  __device__ __forceinline__ bool load(const RowsArgs& a, int hk, int at, Four f, int from, int lane, uint4& key,
-                                       uint4& value) const {
-    const int sub = lane >> 4;
-    if (kTree && at >= context) {
-      const int64_t off = (int64_t)(first + min(at - context + sub, nodes - 1)) * a.new_stride + (int64_t)hk * kRowBytes +
-                          (lane & 15) * 16;
+  __device__ __forceinline__ bool load(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int four, int lane,
+                                       uint4& key, uint4& value) const {
+    const int sub = lane >> 4, at = start + step * stride + four;
+    const int from = ((step - first_step) << per_step_log2) + (four >> shift);
+    if (kTree && at >= s.context) {
+      const int64_t off = (int64_t)(s.first + min(at - s.context + sub, s.nodes - 1)) * a.new_stride +
+                          (int64_t)hk * kRowBytes + (lane & 15) * 16;
       key = ld16(a.k_new + off);
       value = ld16(a.v_new + off);
     } else {
-      const int phys = __builtin_amdgcn_readlane(f.phys, from);
-      const int64_t row = (((int64_t)phys * a.kv_heads + hk) << page_shift) + (at & ((1 << page_shift) - 1));
+      const int page = __builtin_amdgcn_readlane(phys, from);
+      const int64_t row = (((int64_t)page * a.kv_heads + hk) << s.page_shift) + (at & ((1 << s.page_shift) - 1));
       key = ld16(a.k_pool + row * kRowBytes + lane * 16);   // four rows of 256 bytes
       value = ld16(a.v_pool + row * kRowBytes + lane * 16);
     }
-    return sub < __builtin_amdgcn_readlane(f.count, from);
+    return (four & ((1 << shift) - 1)) + sub < __builtin_amdgcn_readlane(left, from);
   }
-  // Which of 64 places hold a token, lane g having looked up the g-th four of them.
-  __device__ __forceinline__ uint64_t held(Four f, int lane) const {
-    return __ballot((lane & 3) < __builtin_amdgcn_ds_bpermute(lane & ~3, f.count));
+  // Which of the step's places hold a token.
+  __device__ __forceinline__ uint64_t held(int step, int lane) const {
+    const int place = lane & (kPlaces - 1);
+    const int from = ((step - first_step) << per_step_log2) + (place >> shift);
+    const uint64_t all = __ballot((place & ((1 << shift) - 1)) < __builtin_amdgcn_ds_bpermute(from * 4, left));
+    return kPlaces == 64 ? all : all & 0xffffffffull;
   }
-  // Which of the 64 places from p0 (a multiple of 64) on a row attends to, of the `held` ones: those up to its
-  // position (prompts), all cached ones or those of its mask (trees).
-  __device__ __forceinline__ uint64_t allow(uint64_t held, int p0, int position, const int64_t* __restrict__ mask,
-                                            int mask_words) const {
-    if (!kTree) return first_bits(position + 1 - p0);
-    if (p0 < context) return held;
-    const int word = (p0 - context) / 64;
-    return word < mask_words ? (uint64_t)mask[word] & held : 0;
+  // Which of them a row attends to: those up to its position (prompts), all cached ones or those of its mask (trees).
+  __device__ __forceinline__ uint64_t allow(const Stream<kTree>& s, uint64_t held, int step, int position,
+                                            const int64_t* __restrict__ mask, int mask_words) const {
+    const int at = start + step * stride;
+    if (!kTree) return first_bits(position + 1 - at);
+    if (at < s.context) return held;
+    const int node = at - s.context;
+    return (node >> 6) < mask_words ? ((uint64_t)mask[node >> 6] >> (node & 63)) & held : 0;
   }
-  // Whether all rows from `position` on attend to all of those places.
-  __device__ __forceinline__ bool whole(uint64_t held, int p0, int position) const {
-    return kTree ? p0 < context && held == ~0ull : p0 + kTileTokens - 1 <= position;
+  // Whether all rows from `position` on attend to all of them.
+  __device__ __forceinline__ bool whole(const Stream<kTree>& s, uint64_t held, int step, int position) const {
+    const int at = start + step * stride;
+    return kTree ? at < s.context && held == (kPlaces == 64 ? ~0ull : 0xffffffffull) : at + kPlaces - 1 <= position;
   }
 };
 
