@@ -239,13 +239,14 @@ def quest_decode_step_static(cache: Cache, k_new, v_new, k_pool_write, q, k_page
 
 def _row_stride(t, other=None):
     """Elements between the rows of t, and of `other`, whose heads have to lie next to each other."""
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-    for x in (t,) if other is None else (t, other):
-        if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or x.shape != t.shape \
-                or (x.shape[0] > 1 and x.stride(0) != stride):
-            raise QuestError(-2, f"packed rows of shape {tuple(x.shape)} and strides {x.stride()}: heads have to lie "
-                                 "next to each other, and keys as values do")
-    return stride
+    shape, stride = t.shape, t.stride()
+    rows, heads, dim = shape
+    if (stride[2] == 1 and (stride[1] == dim or heads == 1)
+            and (other is None or other.shape == shape and other.stride() == stride)):
+        return stride[0] if rows > 1 else heads * dim
+    what = "" if other is None else f", {tuple(other.shape)} and {other.stride()}"
+    raise QuestError(-2, f"packed rows of shape {tuple(shape)} and strides {stride}{what}: heads have to lie next to "
+                         "each other, and keys as values do")
 
 
 def quest_append_tokens(cache: Cache, k_new, v_new, cu_tokens, rows=None, stream=None):

@@ -34,7 +34,7 @@ struct Part {
   __device__ __forceinline__ int position(int row) const {
     return past + __builtin_amdgcn_readfirstlane(min(row, rows - 1) / group);
   }
-  __device__ __forceinline__ bool whole() const { return s.splits == 1; }   // the row tile has no other split
+  __device__ __forceinline__ bool whole() const { return stream.tiles <= s.chunk; }   // the row tile has no other split
 
   __device__ __forceinline__ bool find(const RowsArgs& a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
                                        const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, int lane) {
@@ -49,7 +49,7 @@ struct Part {
     stream.init(a, s, hk, position(row0 + kRows - 1), page_table, topk);
     first_tile = split * s.chunk;
     end_tile = s.chunk < stream.tiles - first_tile ? first_tile + s.chunk : stream.tiles;
-    return true;
+    return first_tile < end_tile;   // (a prompt's first rows have fewer splits than its last)
   }
   __device__ __forceinline__ size_t part_row(const RowsArgs& a, int in_tile) const {
     return ((size_t)unit * a.kv_heads + hk) * kRows + in_tile;
@@ -81,42 +81,44 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   walk.init(w.stream, w.first_tile * kTileTokens, kTileTokens);
   const int steps = w.end_tile - w.first_tile;
   uint64_t held = 0, held1 = 0, held2 = 0, held3 = 0;   // of tiles t, t + 1, ..
-  uint4 k[kLoads], v[kLoads];
-  bool token_there[kLoads];
-  auto load = [&](int step) {
+  struct Part64 {
+    uint4 k[kLoads], v[kLoads];
+    bool there[kLoads];
+  } next;
+  auto load = [&](Part64& r, int step) {
     step = min(step, steps - 1);
     if (!walk.knows(step)) walk.find(w.stream, step, lane);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      token_there[i] = walk.load(a, w.stream, w.hk, step, (i * kSharedWaves + wave) * 4, lane, k[i], v[i]);
-    if (kTree) held3 = walk.held(step, lane);
+      r.there[i] = walk.load(a, w.stream, w.hk, step, (i * kSharedWaves + wave) * 4, lane, r.k[i], r.v[i]);
+    return kTree ? walk.held(step, lane) : 0;
   };
-  auto store = [&](int buffer) {
+  auto store = [&](const Part64& r, int buffer) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int at = (i * kSharedWaves + wave) * 4 + (lane >> 4);
-      st16(lds[buffer][0] + k_place(at, lane & 15), k[i]);
-      st16(lds[buffer][1] + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
+      st16(lds[buffer][0] + k_place(at, lane & 15), r.k[i]);
+      st16(lds[buffer][1] + v_place(at, lane & 15), r.there[i] ? r.v[i] : make_uint4(0, 0, 0, 0));
     }
   };
-  if (steps > 0) {
+  {
     walk.find(w.stream, 0, lane);
     st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
-    load(0);
-    held = held3;
-    st.ready(a.q_sign);
-    store(0);
-    load(1);
-    held1 = held3;
-    store(1);
-    load(2);
-    held2 = held3;
+    {
+      Part64 one, two;   // all on their way at once
+      held = load(one, 0);
+      held1 = load(two, 1);
+      held2 = load(next, 2);
+      st.ready(a.q_sign);
+      store(one, 0);
+      store(two, 1);
+    }
     __syncthreads();
     const bool second = wave >= kSharedWaves / 2;
     if (second) __syncthreads();
     auto stage = [&](int step) {   // what a wave does for all of them in the turn of its softmax
-      store((step + 2) & (kBuffers - 1));
-      load(step + 3);
+      store(next, (step + 2) & (kBuffers - 1));
+      held3 = load(next, step + 3);
     };
     auto turn = [] {
       __builtin_amdgcn_sched_barrier(0);
@@ -156,9 +158,6 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     if (!second) __syncthreads();
   }
 
-  else {
-    st.clear();
-  }
 
   if (!there) return;
   const float total = st.total();
@@ -284,92 +283,102 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   if (a.lse != nullptr && d0 == 0) a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
-// The partial results of each row: a wave a row, a lane a split for the weights, then two channels a lane.
-template <bool kTree, int kRows>
+// The partial results: a wave has some rows, one after the other, a lane a split for the weights, then two channels a
+// lane.  A row's outputs are asked for with its weights (the first eight), and the next row's before they are used.
+template <bool kTree, int kRows, int kMergeRows>
 __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const int32_t* __restrict__ cu,
-                                                         const int32_t* __restrict__ seq_lens, int list) {
+                                                         const int32_t* __restrict__ seq_lens,
+                                                         const int32_t* __restrict__ topk) {
+  constexpr int kEach = kMergeRows / 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
   const int hk = blockIdx.x % a.kv_heads;
   const int rest = blockIdx.x / a.kv_heads;
-  const int in_tile = rest % (kRows / 4) * 4 + wave;
-  const int tile = rest / (kRows / 4);
+  const int tile = rest / (kRows / kMergeRows);
+  const int in_tile = rest % (kRows / kMergeRows) * kMergeRows + wave * kEach;
   Sequence s;
-  if (!find_sequence<kTree, kRows, true>(s, a, cu, seq_lens, list != 0, tile, lane)) return;
-  const int row = (tile - s.before) * kRows + in_tile;
-  if (row >= s.tokens * a.group || s.splits == 1) return;  // (of one split: written already)
-  const int parts = s.splits;
+  if (!find_sequence<kTree, kRows, true>(s, a, cu, seq_lens, topk != nullptr, tile, lane)) return;
+  const int row0 = (tile - s.before) * kRows, rows = s.tokens * a.group;
+  if (s.splits == 1 || row0 + in_tile >= rows) return;
+  Stream<kTree> stream;
+  stream.init(a, s, hk, s.seq_len - s.tokens + (min(row0 + kRows, rows) - 1) / a.group, nullptr, topk);
+  const int parts = (stream.tiles + s.chunk - 1) / s.chunk;
+  if (parts == 1) return;  // written already
   const size_t step = (size_t)s.row_tiles * a.kv_heads * kRows;   // rows between two splits' parts
   const size_t part0 = (((size_t)s.units_before + (s.row_tiles - 1 - (tile - s.before))) * a.kv_heads + hk) * kRows + in_tile;
   const float* ml = a.part_ml + part0 * 2;
   const float* from = a.part_acc + part0 * kHeadDim + lane * 2;
-  float2 v[8];
-  auto ask = [&](int i) {   // eight parts' outputs
+  float2 v[8], mine;
+  auto ask = [&](int r, int i) {   // eight parts' outputs of row r
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float2*>(from + min(i + j, parts - 1) * step * kHeadDim);
+    for (int j = 0; j < 8; ++j)
+      v[j] = *reinterpret_cast<const float2*>(from + (min(i + j, parts - 1) * step + r) * kHeadDim);
   };
-  ask(0);
-  float top = kNegBig;
-  for (int i = lane; i < parts; i += kWave) {
-    const float2 x = *reinterpret_cast<const float2*>(ml + i * step * 2);
-    if (x.y > 0.f) top = fmaxf(top, x.x);
-  }
-#pragma unroll
-  for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-  float sum = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int base = 0; base < parts; base += kWave) {
-    float weight = 0.f;
-    if (base + lane < parts) {
-      const float2 x = *reinterpret_cast<const float2*>(ml + (base + lane) * step * 2);
-      weight = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - top) : 0.f;
-      sum += weight * x.y;
+  auto ask_weight = [&](int r, int i) {
+    return *reinterpret_cast<const float2*>(ml + (min(i + lane, parts - 1) * step + r) * 2);
+  };
+  const int n_rows = min(kEach, rows - row0 - in_tile);
+  mine = ask_weight(0, 0);
+  ask(0, 0);
+  for (int r = 0; r < n_rows; ++r) {
+    float top = lane < parts && mine.y > 0.f ? mine.x : kNegBig;
+    for (int i = kWave; i < parts; i += kWave) {
+      const float2 x = ask_weight(r, i);
+      if (i + lane < parts && x.y > 0.f) top = fmaxf(top, x.x);
     }
-    const int n = min(parts - base, kWave);
-    for (int i = 0; i < n; i += 8) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = i + j < n ? from_lane(weight, i + j) : 0.f;
-        if (x > 0.f) {   // (a part without tokens has left whatever was there)
+    for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+    float sum = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int base = 0; base < parts; base += kWave) {
+      if (base > 0) mine = ask_weight(r, base);
+      const float weight = base + lane < parts && mine.y > 0.f ? __builtin_amdgcn_exp2f(mine.x - top) : 0.f;
+      sum += weight * mine.y;
+      const int n = min(parts - base, kWave);
+      if (base + n == parts) mine = ask_weight(min(r + 1, n_rows - 1), 0);
+      for (int i = 0; i < n; i += 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = i + j < n ? from_lane(weight, i + j) : 0.f;
           o0 += v[j].x * x;
           o1 += v[j].y * x;
         }
+        if (i + 8 < n || base + n < parts)
+          ask(r, base + i + 8);
+        else
+          ask(min(r + 1, n_rows - 1), 0);
       }
-      ask(base + i + 8);
     }
-  }
 #pragma unroll
-  for (int i = 1; i < kWave; i <<= 1) sum += __shfl_xor(sum, i);
-  const int token = row / a.group;
-  const size_t out_row = (size_t)(s.first + token) * (a.kv_heads * a.group) + hk * a.group + (row - token * a.group);
-  const float factor = sum > 0.f ? 1.f / sum : 0.f;
-  store_out2(a.out, a.out_is_fp16, out_row * kHeadDim + lane * 2, o0 * factor, o1 * factor);
-  if (a.lse != nullptr && lane == 0)
-    a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    for (int i = 1; i < kWave; i <<= 1) sum += __shfl_xor(sum, i);
+    const int row = row0 + in_tile + r, token = row / a.group;
+    const size_t out_row = (size_t)(s.first + token) * (a.kv_heads * a.group) + hk * a.group + (row - token * a.group);
+    const float factor = sum > 0.f ? 1.f / sum : 0.f;
+    store_out2(a.out, a.out_is_fp16, out_row * kHeadDim + lane * 2, o0 * factor, o1 * factor);
+    if (a.lse != nullptr && lane == 0)
+      a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
 }
 
 // How a call is cut up, from what the host knows.
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
   int row_tiles;                // of a KV head, at most
-  int most_units, least_chunk;  // of a KV head; 0 units: no splits
+  int most_units, good_units, least_chunk;  // of a KV head; 0 units: no splits
 };
-#ifndef ROUNDS
-#define ROUNDS 0
-#endif
-#ifndef ROWS
-#define ROWS 0
-#endif
 Plan plan_of(const quest_cache& c, int total_tokens, bool tree) {
   Plan p;
   const int64_t rows = (int64_t)total_tokens * group_size(c), mean = (rows + c.batch - 1) / c.batch;
-  p.rows = ROWS ? ROWS : mean <= 64 ? kFewRows : kSharedRows;
+  const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + (tree ? total_tokens / c.batch : 0);
+  p.rows = mean <= 64 || places <= 1536 ? kFewRows : kSharedRows;
+  const bool few = p.rows == kFewRows;
   p.row_tiles = (int)(rows / p.rows + c.batch);
-  const int heads = kv_heads(c);
-  const int at_once = (p.rows == 32 ? 512 : 256) / heads;   // work-groups that the compute units take at once
-  p.least_chunk = p.rows == kSharedRows ? 4 : 2;
-  int rounds = p.row_tiles * 4 <= at_once ? 1 : p.row_tiles * 2 <= at_once ? 2 : 4;
-  if (ROUNDS) rounds = ROUNDS;
-  p.most_units = p.row_tiles > at_once * (tree ? 4 : 1) ? 0 : std::max(at_once * rounds, p.row_tiles + 1);
+  const int at_once = std::max(1, (few ? 512 : 256) / kv_heads(c));  // work-groups that the compute units take at once
+  const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
+  const int rounds = !tree ? (likely * 8 <= at_once ? 1 : 2) : likely * 4 <= at_once ? 1 : few ? 2 : 4;
+  p.least_chunk = few ? 2 : 8;
+  p.good_units = std::max(at_once * rounds, p.row_tiles + 1);
+  p.most_units = tree ? p.good_units : 2 * p.good_units;
+  if (4 * p.row_tiles > at_once * (tree ? 16 : 3) || places <= 8 * kTileTokens) p.most_units = 0;
   return p;
 }
 int units_of(const Plan& p) { return std::max(p.row_tiles, p.most_units); }
@@ -383,6 +392,7 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   Plan p = plan_of(c, total_tokens, kTree);
   if (workspace == nullptr || bytes_of(p, c) > bytes) p.most_units = 0;
   a.most_units = p.most_units;
+  a.good_units = p.good_units;
   a.least_chunk = p.least_chunk;
   a.part_acc = (float*)workspace;
   a.part_ml = a.part_acc + (size_t)units_of(p) * a.kv_heads * p.rows * kHeadDim;
@@ -393,12 +403,16 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
     hipLaunchKernelGGL((shared_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   const int r = check_launch(who);
   if (r != QUEST_OK || p.most_units == 0) return r;
-  const dim3 merge((unsigned)(p.row_tiles * (p.rows / 4) * a.kv_heads));
-  const int list = topk != nullptr;
+  const unsigned tiles = (unsigned)(p.row_tiles * a.kv_heads);
   if (p.rows == kFewRows)
-    hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 4>), dim3(tiles * (kFewRows / 4)), dim3(256), 0, s, a, a.cu,
+                       a.seq_lens, topk);
+  else if (tiles <= 32)
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kSharedRows, 4>), dim3(tiles * (kSharedRows / 4)), dim3(256), 0, s, a,
+                       a.cu, a.seq_lens, topk);
   else
-    hipLaunchKernelGGL((merge_rows_kernel<kTree, kSharedRows>), merge, dim3(256), 0, s, a, a.cu, a.seq_lens, list);
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kSharedRows, 16>), dim3(tiles * (kSharedRows / 16)), dim3(256), 0, s, a,
+                       a.cu, a.seq_lens, topk);
   return check_launch(who);
 }
 
@@ -426,7 +440,9 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
 
 }  // namespace
 
-size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) { return bytes_of(plan_of(c, total_tokens, true), c); }
+size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) {
+  return std::max(bytes_of(plan_of(c, total_tokens, true), c), bytes_of(plan_of(c, total_tokens, false), c));
+}
 
 bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {
   return ((int64_t)total_tokens * group_size(c) + 128 * (int64_t)c.batch) * kv_heads(c) <= INT32_MAX;

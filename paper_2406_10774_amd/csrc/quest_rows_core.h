@@ -49,7 +49,8 @@ struct RowsArgs {
   int64_t q_stride, new_stride;   // bytes between tokens
   int batch, max_pages, page_shift, kv_heads, group;
   int mask_words, k_pages;
-  int most_units;           // splits and row tiles that may come out; 0: no splits
+  int most_units;           // units of a KV head that there is room for; 0: no splits
+  int good_units;           // and that have something to do, about
   int least_chunk;          // token tiles of a split, at least
   int out_is_fp16;
   uint32_t q_sign;          // exclusive-ored onto q: sign bits where the scale is negative
@@ -106,19 +107,23 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
     const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : seq_len;
     tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
   };
-  float all = 0.f;
+  // A prompt's row tile j before the last attends to j kRows / G tokens less than the last.
+  const float less = kTree ? 0.f : 0.5f * kRows / (kTileTokens * a.group);
+  float all = 0.f, work = 0.f;
   int count = 0;
+  auto whole = [](auto v) { return __builtin_bit_cast(decltype(v), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1)); };
   for (int base = 0; base < a.batch; base += kWave) {
     read(base);
-    const float work = up_to_lane((float)row_tiles * (float)tiles, lane);
-    all += as_f((uint32_t)__builtin_amdgcn_readlane((int)as_u(work), kWave - 1));
-    count += __builtin_amdgcn_readlane(up_to_lane(row_tiles, lane), kWave - 1);
+    const float most = (float)row_tiles * (float)tiles;
+    all += whole(up_to_lane(most, lane));
+    if (!kTree) work += whole(up_to_lane(most - less * (float)row_tiles * (float)(row_tiles - 1), lane));
+    count += whole(up_to_lane(row_tiles, lane));
   }
+  if (kTree) work = all;
   // ceil(tiles / chunk) summed over the row tiles is at most all / chunk + count (a hundred-thousandth covers the
   // roundings)
-  const int room = a.most_units - count;
-  const float even = all * 1.00001f / (float)max(room, 1);
-  s.chunk = room < 1 || even > 1e9f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
+  const float even = fmaxf(all / (float)max(a.most_units - count, 1), work / (float)max(a.good_units - count, 1)) * 1.00001f;
+  s.chunk = a.most_units <= count || even > 1e9f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
   int units_before = 0, tiles_before = 0;
   for (int base = 0; base < a.batch; base += kWave) {
     if (a.batch > kWave) read(base);
