@@ -59,7 +59,8 @@ struct Part {
 // Many rows.  Two waves on each SIMD: while one of them has matrix products to do, the other is at its softmax, by
 // turns that barriers keep: turn 2t is the first four waves' products (values of tile t - 1, logits of tile t) and
 // the other four's softmax of tile t - 1, in turn 2t + 1 they change places.  In its turn of softmax of tile t a wave
-// also puts its share of tile t + 2 into LDS; four buffers, as values of tile t - 1 are read until turn 2t + 1.
+// also asks for its share of tile t + 2, straight into LDS; it waits for that at the end of its next products, a turn
+// before anyone reads it.  Four buffers: values of tile t - 2 are read until turn 2t - 1, its place is written from 2t + 1.
 template <bool kTree, bool kExact>
 __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -80,84 +81,69 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   Walk<kTree, kTileTokens> walk;
   walk.init(w.stream, w.first_tile * kTileTokens, kTileTokens);
   const int steps = w.end_tile - w.first_tile;
-  uint64_t held = 0, held1 = 0, held2 = 0, held3 = 0;   // of tiles t, t + 1, ..
-  struct Part64 {
-    uint4 k[kLoads], v[kLoads];
-    bool there[kLoads];
-  } next;
-  auto load = [&](Part64& r, int step) {
-    step = min(step, steps - 1);
+  uint64_t held = 0, held1 = 0, held2 = 0;   // of tiles t, t + 1, ..
+  auto keys = [&](int step) { return lds[step & (kBuffers - 1)][0]; };
+  auto values = [&](int step) { return lds[step & (kBuffers - 1)][1]; };
+  // a wave's share of a tile: four tokens in each of kLoads pieces
+  auto fetch = [&](int step) -> uint64_t {
+    if (step >= steps) return 0;
     if (!walk.knows(step)) walk.find(w.stream, step, lane);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      r.there[i] = walk.load(a, w.stream, w.hk, step, (i * kSharedWaves + wave) * 4, lane, r.k[i], r.v[i]);
+      walk.fetch(a, w.stream, w.hk, step, (i * kSharedWaves + wave) * 4, lane, lds_address(keys(step)),
+                 lds_address(values(step)));
     return kTree ? walk.held(step, lane) : 0;
   };
-  auto store = [&](const Part64& r, int buffer) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = (i * kSharedWaves + wave) * 4 + (lane >> 4);
-      st16(lds[buffer][0] + k_place(at, lane & 15), r.k[i]);
-      st16(lds[buffer][1] + v_place(at, lane & 15), r.there[i] ? r.v[i] : make_uint4(0, 0, 0, 0));
-    }
-  };
-  {
-    walk.find(w.stream, 0, lane);
-    st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
-    {
-      Part64 one, two;   // all on their way at once
-      held = load(one, 0);
-      held1 = load(two, 1);
-      held2 = load(next, 2);
-      st.ready(a.q_sign);
-      store(one, 0);
-      store(two, 1);
-    }
+  walk.find(w.stream, 0, lane);
+  st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+  held = fetch(0);
+  held1 = fetch(1);
+  st.ready(a.q_sign);
+  dma_arrived<0>();
+  __syncthreads();
+  const bool second = wave >= kSharedWaves / 2;
+  if (second) __syncthreads();
+  auto turn = [] {
+    __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
-    const bool second = wave >= kSharedWaves / 2;
-    if (second) __syncthreads();
-    auto stage = [&](int step) {   // what a wave does for all of them in the turn of its softmax
-      store(next, (step + 2) & (kBuffers - 1));
-      held3 = load(next, step + 3);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (row0 < w.rows) {
+    typename RowState<kExact>::template Weights<2> p;
+    f32x16_t s[2];
+    auto softmax = [&](int step) {
+      if (!walk.whole(w.stream, held, step, wave_first))
+        st.hide(s, walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words), lane);
+      st.template weigh<2>(p, s, a.scale_log2);
+      held = held1, held1 = held2;
     };
-    auto turn = [] {
-      __builtin_amdgcn_sched_barrier(0);
-      __syncthreads();
-      __builtin_amdgcn_sched_barrier(0);
+    auto rest = [&](int step) {
+      dma_arrived<0>();
+      __builtin_amdgcn_s_setprio(0);
+      turn();
+      held2 = fetch(step + 2);
+      softmax(step);
+      __builtin_amdgcn_s_setprio(1);   // products first where both waves could issue (1 % of the time)
+      turn();
     };
-    if (row0 < w.rows) {
-      typename RowState<kExact>::template Weights<2> p;
-      f32x16_t s[2];
-      auto softmax = [&](int step) {
-        if (!walk.whole(w.stream, held, step, wave_first))
-          st.hide(s, walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words), lane);
-        st.template weigh<2>(p, s, a.scale_log2);
-        held = held1, held1 = held2, held2 = held3;
-      };
-      st.template logits<2>(s, lds[0][0], lane);
-      turn();
-      stage(0);
-      softmax(0);
-      turn();
-      for (int step = 1; step < steps; ++step) {
-        st.template add<2>(p, lds[(step - 1) & (kBuffers - 1)][1], lane);
-        st.template logits<2>(s, lds[step & (kBuffers - 1)][0], lane);
-        turn();
-        stage(step);
-        softmax(step);
-        turn();
-      }
-      st.template add<2>(p, lds[(steps - 1) & (kBuffers - 1)][1], lane);
-    } else {
-      for (int step = 0; step < steps; ++step) {
-        stage(step);
-        turn();
-        turn();
-      }
+    st.template logits<2>(s, keys(0), lane);
+    rest(0);
+    for (int step = 1; step < steps; ++step) {
+      st.template add<2>(p, values(step - 1), lane);
+      st.template logits<2>(s, keys(step), lane);
+      rest(step);
     }
-    if (!second) __syncthreads();
+    st.template add<2>(p, values(steps - 1), lane);
+  } else {
+    for (int step = 0; step < steps; ++step) {
+      dma_arrived<0>();
+      turn();
+      held2 = fetch(step + 2);
+      held = held1, held1 = held2;
+      turn();
+    }
   }
-
+  if (!second) __syncthreads();
 
   if (!there) return;
   const float total = st.total();

@@ -320,6 +320,27 @@ __device__ __forceinline__ int v_place(int token, int slot) {
   return token * kRowBytes + ((slot ^ ((token & 3) << 2)) << 4);
 }
 
+// 16 bytes a lane from memory to LDS at `to` + 16 lane, without registers in between: from a wave's address and a
+// lane's offset, or a lane's address.  The compiler does not count these: dma_arrived<n> waits until at
+// most the last n (and what was loaded since) are under way.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+__device__ __forceinline__ void dma16(uint32_t to, const char* base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma16(uint32_t to, const char* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void dma_arrived() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // The first n of 64 bits.
 __device__ __forceinline__ uint64_t first_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
@@ -413,6 +434,38 @@ struct Walk {
       value = ld16(a.v_pool + row * kRowBytes + lane * 16);
     }
     return (four & ((1 << shift) - 1)) + sub < __builtin_amdgcn_readlane(left, from);
+  }
+  // The same straight into LDS, where k_place and v_place would put it (`k_lds`, `v_lds`: the tile's addresses): a lane
+  // fetches the chunk that belongs at its own place.  Rows that are not there get a row that is (the first of the
+  // sequence): any finite value will do under a weight of zero.  To be waited for with dma_arrived.
+  __device__ __forceinline__ void fetch(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int four, int lane,
+                                        uint32_t k_lds, uint32_t v_lds) const {
+    const int sub = lane >> 4, at = start + step * stride + four;
+    const int from = ((step - first_step) << per_step_log2) + (four >> shift);
+    const int there = __builtin_amdgcn_readlane(left, from) - (four & ((1 << shift) - 1));
+    const uint32_t k_chunk = ((lane & 15) ^ ((four + sub) & 15)) << 4, v_chunk = ((lane & 15) ^ (sub << 2)) << 4;
+    k_lds += four * kRowBytes;
+    v_lds += four * kRowBytes;
+    const bool drafts = kTree && at >= s.context;
+    const int page = __builtin_amdgcn_readlane(phys, from);
+    const int64_t row = (((int64_t)page * a.kv_heads + hk) << s.page_shift) + (at & ((1 << s.page_shift) - 1));
+    if (!drafts && there >= 4) {
+      dma16(k_lds, a.k_pool + row * kRowBytes, sub * kRowBytes + k_chunk);
+      dma16(v_lds, a.v_pool + row * kRowBytes, sub * kRowBytes + v_chunk);
+      return;
+    }
+    const char *k = a.k_pool, *v = a.v_pool;
+    int64_t off = (row + sub) * kRowBytes;
+    if (drafts || (kTree && sub >= there)) {
+      k = a.k_new;
+      v = a.v_new;
+      const int node = drafts ? min(at - s.context + sub, s.nodes - 1) : 0;
+      off = (int64_t)(s.first + node) * a.new_stride + (int64_t)hk * kRowBytes;
+    } else if (sub >= there) {
+      off = (((int64_t)s.table[0] * a.kv_heads + hk) << s.page_shift) * kRowBytes;
+    }
+    dma16(k_lds, k + off + k_chunk);
+    dma16(v_lds, v + off + v_chunk);
   }
   // Which of the step's places hold a token.
   __device__ __forceinline__ uint64_t held(int step, int lane) const {
