@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   const int head = w.hk * a.group + (there ? row - token * a.group : 0);
   const int wave_first = w.position(row0);
 
-  RowState<kExact> st;
+  RowState<kExact, true> st;
   Walk<kTree, kTileTokens> walk;
   walk.init(w.stream, w.first_tile * kTileTokens, kTileTokens);
   const int steps = w.end_tile - w.first_tile;
@@ -109,12 +109,12 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     __builtin_amdgcn_sched_barrier(0);
   };
   if (row0 < w.rows) {
-    typename RowState<kExact>::template Weights<2> p;
+    typename RowState<kExact, true>::template Weights<2> p;
     f32x16_t s[2];
     auto softmax = [&](int step) {
       if (!walk.whole(w.stream, held, step, wave_first))
         st.hide(s, walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words), lane);
-      st.template weigh<2>(p, s, a.scale_log2);
+      st.template weigh<2>(p, s, a);
       held = held1, held1 = held2;
     };
     auto rest = [&](int step) {
@@ -149,16 +149,16 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   const float total = st.total();
   if (!w.whole()) {
     const size_t part = w.part_row(a, wave * 32 + (lane & 31));
-    st.each4(RowState<kExact>::kUnscale, lane,
+    st.each4(RowState<kExact, true>::kUnscale, lane,
              [&](int d, float4 o) { *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d) = o; });
-    if (lane < 32) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(st.ref, total);
+    if (lane < 32) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(st.base, total);
     return;
   }
   const size_t out_row = (size_t)(w.s.first + token) * (a.kv_heads * a.group) + head;
-  const float factor = total > 0.f ? RowState<kExact>::kUnscale / total : 0.f;
+  const float factor = total > 0.f ? RowState<kExact, true>::kUnscale / total : 0.f;
   st.each4(factor, lane, [&](int d, float4 o) { store4(a.out, a.out_is_fp16, out_row * kHeadDim + d, o); });
   if (a.lse != nullptr && lane < 32)
-    a.lse[out_row] = total > 0.f ? (st.ref + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+    a.lse[out_row] = st.lse(st.base, total, a.scale);
 }
 
 // Few rows: tiles of 32 tokens, each wave its own.
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   }
   const int first_position = w.position(w.row0);
 
-  RowState<kExact> st;
+  RowState<kExact, false> st;
   Walk<kTree, kTokens> walk;
   walk.init(w.stream, w.first_tile * kTileTokens + wave * kTokens, kWaves * kTokens);
   const int steps = ((w.end_tile - w.first_tile) * (kTileTokens / kTokens) - wave + kWaves - 1) / kWaves;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     uint64_t allow = ~0ull;
     if (masked)
       allow = walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words);
-    st.template fold<1>(stage_k, stage_v, a.scale_log2, masked, allow, lane);
+    st.template fold<1>(stage_k, stage_v, a, masked, allow, lane);
     lds_in_order();
   }
 
@@ -225,9 +225,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   float* join = reinterpret_cast<float*>(lds);
   const float total = st.total();
   float* mine = join + (wave * kFewRows + (lane & 31)) * kStride;
-  st.each4(RowState<kExact>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
+  st.each4(RowState<kExact, false>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
   if (lane < kFewRows) {
-    ml[0][wave][lane] = total > 0.f ? st.ref : kNegBig;
+    ml[0][wave][lane] = total > 0.f ? st.base : kNegBig;
     ml[1][wave][lane] = total;
   }
   __syncthreads();
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[0][i][in_tile]);
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
-    weight[i] = __builtin_amdgcn_exp2f(ml[0][i][in_tile] - top);
+    weight[i] = __builtin_amdgcn_exp2f((ml[0][i][in_tile] - top) * a.scale);
     sum += weight[i] * ml[1][i][in_tile];
   }
   float4 o[4];
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   for (int j = 0; j < 4; ++j)
     store4(a.out, a.out_is_fp16, out_row * kHeadDim + d0 + 4 * j,
            make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor));
-  if (a.lse != nullptr && d0 == 0) a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  if (a.lse != nullptr && d0 == 0) a.lse[out_row] = st.lse(top, sum, a.scale);
 }
 
 // The partial results: a wave has some rows, one after the other, a lane a split for the weights, then two channels a
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
     float sum = 0.f, o0 = 0.f, o1 = 0.f;
     for (int base = 0; base < parts; base += kWave) {
       if (base > 0) mine = ask_weight(r, base);
-      const float weight = base + lane < parts && mine.y > 0.f ? __builtin_amdgcn_exp2f(mine.x - top) : 0.f;
+      const float weight = base + lane < parts && mine.y > 0.f ? __builtin_amdgcn_exp2f((mine.x - top) * a.scale) : 0.f;
       sum += weight * mine.y;
       const int n = min(parts - base, kWave);
       if (base + n == parts) mine = ask_weight(min(r + 1, n_rows - 1), 0);
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
     const float factor = sum > 0.f ? 1.f / sum : 0.f;
     store_out2(a.out, a.out_is_fp16, out_row * kHeadDim + lane * 2, o0 * factor, o1 * factor);
     if (a.lse != nullptr && lane == 0)
-      a.lse[out_row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+      a.lse[out_row] = RowState<false, false>::lse(top, sum, a.scale);
   }
 }
 
@@ -420,7 +420,9 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
   a.group = group_size(c);
   a.out_is_fp16 = out_is_fp16;
   a.q_sign = sm_scale < 0.f ? 0x80008000u : 0u;
-  a.scale_log2 = std::max(std::abs(sm_scale) * kLog2e, 1e-30f);  // scale 0: all weights alike
+  a.scale = std::max(std::abs(sm_scale) * kLog2e, 1e-30f);  // scale 0: all weights alike
+  a.below = (out_is_fp16 ? RowState<false, false>::kBelow : RowState<true, false>::kBelow) / a.scale;
+  a.limit = (out_is_fp16 ? RowState<false, false>::kMove : RowState<true, false>::kMove) / a.scale;
   return a;
 }
 

@@ -42,7 +42,7 @@ struct RowsArgs {
   void* out;
   float* lse;
   float* part_acc;          // [units][kv heads][kRows][D]
-  float* part_ml;           // [units][kv heads][kRows][2]: reference exponent, sum
+  float* part_ml;           // [units][kv heads][kRows][2]: reference (logit before the scale), sum
   const char* k_new;        // trees: keys and values of the drafted nodes
   const char* v_new;
   const int64_t* mask;      // trees: [rows of cu][mask_words]
@@ -54,7 +54,8 @@ struct RowsArgs {
   int least_chunk;          // token tiles of a split, at least
   int out_is_fp16;
   uint32_t q_sign;          // exclusive-ored onto q: sign bits where the scale is negative
-  float scale_log2;         // |sm_scale| log2(e), not 0
+  float scale;              // |sm_scale| log2(e), not 0
+  float below, limit;       // RowState's kBelow and kMove in logits before the scale
 };
 
 constexpr int kTileTokens = 64;
@@ -151,27 +152,31 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
   return false;
 }
 
-// Attention state of a wave's 32 rows; lane l: row l % 32.
-template <bool kExact>
+// Attention state of a wave's 32 rows; lane l: row l % 32.  Weights are 2^(scale (s - base)), s the logit before the scale
+// and base close below the largest one: the difference first, which is exact near it, so that logits of any size keep
+// their order.  kShifted: the products that make the logits start at -base, which costs 16 registers and no instruction.
+template <bool kExact, bool kShifted>
 struct RowState {
-  static constexpr float kBelow = kExact ? 0.f : 7.f;    // the reference lies this far below the largest logit
-  static constexpr float kMove = kExact ? 1.f : 15.f;    // and moves when a logit is this far above it (log2)
+  static constexpr float kBelow = kExact ? 0.f : 7.f;    // the base lies this far below the largest logit (log2)
+  static constexpr float kMove = kExact ? 1.f : 15.f;    // and moves when a logit is this far above it
   half8_t q[8];        // channels 16 i + 8 h ..+7
   f32x16_t acc[4];     // [d / 32]: channels 8 (r / 4) + 4 h + r % 4
-  float ref, l;        // reference exponent; this lane's share of the row's sum
+  f32x16_t start;      // kShifted: -base
+  float base, limit;   // moves when s - base is above; -3e38 while no token has counted
+  float l;             // this lane's share of the row's sum
 
   // Asks for the row's query; what uses it comes after ready().
   __device__ __forceinline__ void init(const char* row, int lane) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(half8_t, ld16(row + i * 32 + (lane >> 5) * 16));
-    clear();
-  }
-  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
-    ref = kNegBig;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) start[r] = 0.f;
+    base = 0.f;
+    limit = -3e38f;
     l = 0.f;
   }
   __device__ __forceinline__ void ready(uint32_t sign) {
@@ -185,15 +190,19 @@ struct RowState {
     }
   }
 
-  // Logits of 32 kBlocks tokens that lie in LDS.
+  // Logits (kShifted: minus the base) of 32 kBlocks tokens that lie in LDS.
   template <int kBlocks>
   __device__ __forceinline__ void logits(f32x16_t (&s)[kBlocks], const char* k, int lane) const {
     const char* k_lane = k + (lane & 31) * kRowBytes;
     const int k_chunk = ((lane >> 5) ^ (lane & 15)) << 4;
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t) {
+      if constexpr (kShifted) {
+        s[t] = start;
+      } else {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+        for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint4 key = ld16(k_lane + t * (32 * kRowBytes) + (k_chunk ^ (i << 5)));
@@ -218,31 +227,41 @@ struct RowState {
     half8_t w[kBlocks * 2], rest[kExact ? kBlocks * 2 : 1];
   };
   template <int kBlocks>
-  __device__ __forceinline__ void weigh(Weights<kBlocks>& p, const f32x16_t (&s)[kBlocks], float scale) {
+  __device__ __forceinline__ void weigh(Weights<kBlocks>& p, f32x16_t (&s)[kBlocks], const RowsArgs& a) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
     const LanePair p2 = pair_across32(as_u(top));
-    top = fmaxf(as_f(p2.first), as_f(p2.second)) * scale;
-    const bool move = top > ref + kMove;
+    top = fmaxf(as_f(p2.first), as_f(p2.second));
+    if (!kShifted) top -= base;
+    const bool move = top > limit;
     if (__ballot(move)) {
-      const float to = move ? top - kBelow : ref;
-      const float alpha = __builtin_amdgcn_exp2f(ref - to);
-      ref = to;
+      const float by = move ? top - a.below : 0.f;
+      const float alpha = limit < -1e38f ? 0.f : __builtin_amdgcn_exp2f(-by * a.scale);
+      base += by;
+      limit = move ? a.limit : limit;
       l *= alpha;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
+      if constexpr (kShifted) {
+#pragma unroll
+        for (int t = 0; t < kBlocks; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[t][r] -= by;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) start[r] = -base;
+      }
     }
     float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], scale, -ref));
+        const float x = __builtin_amdgcn_exp2f((kShifted ? s[t][r] : s[t][r] - base) * a.scale);
         sum[r & 1] += x;
         if constexpr (kExact) {
           const float scaled = x * kWeightScale;
@@ -276,12 +295,12 @@ struct RowState {
   }
   // All of it for a tile.
   template <int kBlocks>
-  __device__ __forceinline__ void fold(const char* k, const char* v, float scale, bool masked, uint64_t allow, int lane) {
+  __device__ __forceinline__ void fold(const char* k, const char* v, const RowsArgs& a, bool masked, uint64_t allow, int lane) {
     f32x16_t s[kBlocks];
     logits(s, k, lane);
     if (masked) hide(s, allow, lane);
     Weights<kBlocks> p;
-    weigh(p, s, scale);
+    weigh(p, s, a);
     add(p, v, lane);
   }
 
@@ -289,6 +308,10 @@ struct RowState {
   __device__ __forceinline__ float total() const {
     const LanePair s = pair_across32(as_u(l));
     return as_f(s.first) + as_f(s.second);
+  }
+  // log sum exp of a row, of its base and sum.
+  __device__ __forceinline__ static float lse(float base, float total, float scale) {
+    return total > 0.f ? __builtin_fmaf(base, scale, __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
   }
   static constexpr float kUnscale = kExact ? 1.f / kWeightScale : 1.f;
 

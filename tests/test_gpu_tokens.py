@@ -163,6 +163,35 @@ def test_tree_scales(scale):
         check_tree(p, t, *run_tree(p, t, half, scale), half, scale, scale)
 
 
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("n,ctx", [(7, 900), (300, 900)])
+def test_largest_logits(n, ctx, half):
+    """Queries and keys near fp16's largest: logits of 1e11 and gaps between them of 1e9, far beyond what the sums of
+    128 channels round (2^-24 * 128 of 6e11, 5e6).  Each row's weight is on one key: the visible one of the largest factor."""
+    p = Packed([ctx + n], [n], heads=4, kv_heads=2, seed=n)
+    total = ctx + n
+    sign = (torch.rand(2, D, device=p.dev) < 0.5).half() * 2 - 1
+    order = torch.argsort(torch.rand(total, device=p.dev))
+    factor = (30000 + 25 * order.float()).half()           # fp16 has steps of 16 and 32 there: runs of equal keys
+    t = torch.arange(total, device=p.dev)
+    phys = p.table[0].long()[t // p.S]
+    p.k_pool[phys, :, t % p.S] = factor[:, None, None] * sign
+    p.q[:n] = (60000 * sign.repeat_interleave(2, 0))[None].half()
+    p.v_pool[phys, :, t % p.S] = factor[:, None, None] / 30000   # equal keys, equal values
+    for row in run_prompt(p, half, scale=1.0), run_prompt(p, half, scale=1.0, workspace=None):
+        out, lse = row
+        visible = torch.cummax(factor.float(), 0).values[ctx:]
+        assert bool((out[:n].float() == (visible.half() / 30000).float()[:, None, None]).all()), float(out[:n].max())
+        want = visible.double() * 60000 * 128
+        assert bool(((lse[:n].double() - want[:, None]).abs() <= 2.0 ** -16 * want[:, None]).all())
+    p.k_new[:n] = factor[ctx:, None, None] * sign
+    p.v_new[:n] = factor[ctx:, None, None] / 30000
+    p.seq_lens.fill_(ctx)
+    trees = Trees(p, kind=lambda rng, n, words: np.tril(np.ones((n, n), bool)))
+    out, lse = run_tree(p, trees, half, scale=1.0)
+    assert bool((out[:n].float() == (visible.half() / 30000).float()[:, None, None]).all())
+
+
 # ---- insertion
 
 def one_by_one(p, past, rows):
