@@ -329,11 +329,12 @@ int quest_append_tokens(const quest_cache* cache, const void* k_new, const void*
                         const int32_t* rows, const int32_t* cu_tokens, int32_t total_tokens, void* stream);
 
 /* Bytes of device workspace for quest_prompt_attention and quest_tree_attention on this cache
- * with at most total_tokens packed tokens (it grows and falls with total_tokens; 0: none is used).
- * Pure host function.  The workspace holds partial results of calls that walk the
- * tokens in several splits.  It need not be initialised and keeps nothing between calls; calls that
- * share a workspace must not overlap in time.  A smaller workspace, or NULL, is accepted: fewer splits,
- * slower, results equal within rounding. */
+ * with up to total_tokens packed tokens; it does not fall as total_tokens grows (0: none is used).
+ * Pure host function.  The workspace holds the partial results of calls that walk the
+ * tokens in several splits: about 35 MB, or 145 MB where sequences may have more than 64 rows (new
+ * tokens times query heads of a KV head).  It need not be initialised
+ * and keeps nothing between calls; calls that share a workspace must not overlap in time.
+ * A smaller workspace, or NULL, is accepted: fewer splits, slower, results equal within rounding. */
 int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens, size_t* out_bytes);
 
 /* Causal attention of packed queries over the cache: the last n_b of the seq_lens[b] cached tokens

@@ -351,32 +351,38 @@ struct Plan {
   int row_tiles;                // of a KV head, at most
   int most_units, good_units, least_chunk;  // of a KV head; 0 units: no splits
 };
-Plan plan_of(const quest_cache& c, int total_tokens, bool tree) {
+// Work-groups of a KV head that the compute units take at once: two few_rows_kernel each, or one shared_rows_kernel.
+int at_once(int rows, const quest_cache& c) { return std::max(1, (rows == kFewRows ? 512 : 256) / kv_heads(c)); }
+// k_pages: listed pages (0: all).
+Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   Plan p;
   const int64_t rows = (int64_t)total_tokens * group_size(c), mean = (rows + c.batch - 1) / c.batch;
-  const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + (tree ? total_tokens / c.batch : 0);
+  const int64_t pages = k_pages > 0 ? std::min(k_pages, c.max_pages_per_seq) : c.max_pages_per_seq;
+  const int64_t places = pages * c.page_size + (tree ? total_tokens / c.batch : 0);   // that a row may attend to
   p.rows = mean <= 64 || places <= 1536 ? kFewRows : kSharedRows;
   const bool few = p.rows == kFewRows;
+  const int once = at_once(p.rows, c);
   p.row_tiles = (int)(rows / p.rows + c.batch);
-  const int at_once = std::max(1, (few ? 512 : 256) / kv_heads(c));  // work-groups that the compute units take at once
   const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
-  const int rounds = !tree ? (likely * 8 <= at_once ? 1 : 2) : likely * 4 <= at_once ? 1 : few ? 2 : 4;
+  const int rounds = !tree ? (likely * 8 <= once ? 1 : 2) : likely * 4 <= once ? 1 : few ? 2 : 4;
   p.least_chunk = few ? 2 : 8;
-  p.good_units = std::max(at_once * rounds, p.row_tiles + 1);
+  p.good_units = std::max(once * rounds, p.row_tiles + 1);
   p.most_units = tree ? p.good_units : 2 * p.good_units;
-  if (4 * p.row_tiles > at_once * (tree ? 16 : 3) || places <= 8 * kTileTokens) p.most_units = 0;
+  if (4 * p.row_tiles > once * (tree ? 16 : 3) || places <= 8 * kTileTokens) p.most_units = 0;
   return p;
 }
 int units_of(const Plan& p) { return std::max(p.row_tiles, p.most_units); }
-size_t bytes_of(const Plan& p, const quest_cache& c) {
-  return p.most_units == 0 ? 0 : (size_t)units_of(p) * kv_heads(c) * p.rows * (kHeadDim + 2) * sizeof(float);
-}
+size_t unit_bytes(int rows, const quest_cache& c) { return (size_t)kv_heads(c) * rows * (kHeadDim + 2) * sizeof(float); }
 
 template <bool kTree, bool kExact>
 int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32_t* topk, void* workspace, size_t bytes,
                 const char* who, hipStream_t s) {
-  Plan p = plan_of(c, total_tokens, kTree);
-  if (workspace == nullptr || bytes_of(p, c) > bytes) p.most_units = 0;
+  Plan p = plan_of(c, total_tokens, kTree, topk != nullptr ? a.k_pages : 0);
+  const size_t room = workspace != nullptr ? bytes / unit_bytes(p.rows, c) : 0;
+  if (room < (size_t)units_of(p)) {  // as far as it goes
+    p.most_units = room > (size_t)p.row_tiles ? (int)room : 0;
+    p.good_units = std::min(p.good_units, p.most_units);
+  }
   a.most_units = p.most_units;
   a.good_units = p.good_units;
   a.least_chunk = p.least_chunk;
@@ -428,8 +434,17 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
 
 }  // namespace
 
+// Enough for calls with any number of tokens up to this one: four rounds of units, and one more, of the largest
+// row tiles that they may have.
 size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) {
-  return std::max(bytes_of(plan_of(c, total_tokens, true), c), bytes_of(plan_of(c, total_tokens, false), c));
+  size_t most = 0;
+  for (const bool tree : {false, true}) {
+    const Plan p = plan_of(c, total_tokens, tree, 0);
+    const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + (tree ? total_tokens : 0);
+    if (places > 8 * kTileTokens && total_tokens > 0)
+      most = std::max(most, (4 * (size_t)at_once(p.rows, c) + 2) * unit_bytes(p.rows, c));
+  }
+  return most;
 }
 
 bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {

@@ -11,17 +11,18 @@ D = 128
 
 class Packed:
     """Sequences of lens[b] cached tokens and new[b] packed ones, pages in random order; slots without a token and packed
-    rows behind the last sequence are NaN.  stride: elements between packed rows beyond their heads."""
+    rows behind the last sequence are NaN.  stride: elements between packed rows beyond their heads.  room: tokens that a
+    page-table row has room for (kernels are chosen by it)."""
 
     def __init__(self, lens, new, heads=4, kv_heads=2, S=16, seed=0, stride=0, spare_rows=3, cached=True, device="cuda:0",
-                 spread=1.0):
+                 spread=1.0, room=0):
         rng = np.random.default_rng(seed)
         gen = torch.Generator(device=device)
         gen.manual_seed(seed)
         self.lens, self.new, self.H, self.Hkv, self.G, self.S = list(lens), list(new), heads, kv_heads, heads // kv_heads, S
         self.B, self.dev = len(lens), device
         pages = [-(-n // S) for n in lens]
-        width = max(pages) + 2
+        width = max(max(pages) + 2, room // S)
         N = sum(pages) + 3
         ids = rng.permutation(N)
         self.table_np = np.full((self.B, width), ids[-1], np.int32)      # rows' ends: a page that nobody has

@@ -11,6 +11,7 @@ from packed_util import D, Packed, Trees, check_prompt, check_tree
 
 pytestmark = pytest.mark.gpu
 SCALE = 1 / math.sqrt(D)
+ROOMS = [0, 8192]      # page-table rows that end with the sequence, and long ones: other kernels and splits
 
 
 def run_prompt(p, half, scale=SCALE, workspace="full"):
@@ -30,25 +31,28 @@ def run_tree(p, t, half, scale=SCALE, workspace="full"):
 
 
 @pytest.mark.parametrize("half", [True, False])
-@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 515])
-def test_whole_prompts(n, half):
-    p = Packed([n], [n], heads=3, kv_heads=3, seed=n)
+@pytest.mark.parametrize("room", ROOMS)
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257, 515, 1100])
+def test_whole_prompts(n, room, half):
+    p = Packed([n], [n], heads=3, kv_heads=3, seed=n, room=room)
     for ws in ("full", None):
         check_prompt(p, *run_prompt(p, half, workspace=ws), half, SCALE, (n, ws))
 
 
+@pytest.mark.parametrize("room", ROOMS)
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 4), (4, 1), (6, 2), (10, 2), (16, 2), (18, 1), (40, 1)])
-def test_prompt_groups_ragged(heads, kv_heads):
+def test_prompt_groups_ragged(heads, kv_heads, room):
     """Sequences of different lengths, one without new tokens, parts of prompts behind cached tokens."""
-    p = Packed([150, 40, 333, 1, 70], [150, 0, 37, 1, 65], heads=heads, kv_heads=kv_heads, seed=heads)
+    p = Packed([150, 40, 333, 1, 70], [150, 0, 37, 1, 65], heads=heads, kv_heads=kv_heads, seed=heads, room=room)
     for half in (True, False):
         check_prompt(p, *run_prompt(p, half), half, SCALE, (heads, kv_heads, half))
 
 
+@pytest.mark.parametrize("room", ROOMS)
 @pytest.mark.parametrize("S", [8, 16, 32, 64])
-def test_prompt_page_sizes_and_strides(S):
+def test_prompt_page_sizes_and_strides(S, room):
     for stride in (0, 8, 3 * D):
-        p = Packed([301, 64, 7], [301, 20, 7], heads=8, kv_heads=2, S=S, seed=S, stride=stride)
+        p = Packed([301, 64, 7, 1210], [301, 20, 7, 100], heads=8, kv_heads=2, S=S, seed=S, stride=stride, room=room)
         check_prompt(p, *run_prompt(p, True), True, SCALE, (S, stride))
 
 
@@ -63,21 +67,25 @@ def test_prompt_parts_behind_long_contexts(new, past):
 
 @pytest.mark.parametrize("scale", [SCALE, -SCALE, 0.0, 1.0])
 def test_prompt_scales(scale):
-    p = Packed([190], [190], heads=2, kv_heads=2, seed=5, spread=2.0)
-    for half in (True, False):
-        check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
+    for room in ROOMS:
+        p = Packed([190], [190], heads=2, kv_heads=2, seed=5, spread=2.0, room=room)
+        for half in (True, False):
+            check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
 
 
-def test_prompt_of_more_sequences_than_lanes():
-    new = [int(x) for x in np.random.default_rng(0).integers(0, 40, 150)]
+@pytest.mark.parametrize("most,heads", [(40, 4), (60, 12)])
+def test_prompt_of_more_sequences_than_lanes(most, heads):
+    new = [int(x) for x in np.random.default_rng(0).integers(0, most, 150)]
     lens = [n + (7 * i) % 50 + 1 for i, n in enumerate(new)]
-    p = Packed(lens, new, heads=4, kv_heads=1, seed=6)
+    lens[77] += 3000
+    p = Packed(lens, new, heads=heads, kv_heads=1, seed=6)
     check_prompt(p, *run_prompt(p, True), True, SCALE)
 
 
-def test_prompt_rising_logits():
+@pytest.mark.parametrize("room", ROOMS)
+def test_prompt_rising_logits(room):
     """The running maximum moves in every tile: logits grow along the sequence, then fall."""
-    p = Packed([700], [700], heads=2, kv_heads=1, seed=7)
+    p = Packed([700], [700], heads=2, kv_heads=1, seed=7, room=room)
     t = torch.arange(700, device=p.dev)
     phys = p.table[0].long()[t // p.S]
     ramp = (torch.where(t < 400, t, 800 - t).float() * 0.25)[:, None, None].half()
@@ -88,17 +96,20 @@ def test_prompt_rising_logits():
 
 
 @pytest.mark.parametrize("half", [True, False])
-@pytest.mark.parametrize("n,ctx", [(1, 0), (1, 1), (1, 700), (5, 64), (8, 1000), (31, 65), (33, 129), (64, 300), (65, 300), (130, 77)])
-def test_trees(n, ctx, half):
-    p = Packed([ctx, ctx // 2], [n, max(1, n // 3)], heads=4, kv_heads=2, seed=n + ctx, stride=16)
+@pytest.mark.parametrize("room", ROOMS)
+@pytest.mark.parametrize("n,ctx", [(1, 0), (1, 1), (1, 700), (5, 64), (8, 1000), (31, 65), (33, 129), (64, 300), (65, 300), (130, 77),
+                                   (140, 3000), (3, 3000)])
+def test_trees(n, ctx, room, half):
+    p = Packed([ctx, ctx // 2], [n, max(1, n // 3)], heads=4, kv_heads=2, seed=n + ctx, stride=16, room=room)
     t = Trees(p, seed=n)
     for ws in ("full", None):
         check_tree(p, t, *run_tree(p, t, half, workspace=ws), half, SCALE, (n, ctx, ws))
 
 
-@pytest.mark.parametrize("heads,kv_heads,S", [(1, 1, 16), (8, 1, 8), (6, 2, 32), (64, 2, 64), (20, 4, 16)])
-def test_tree_groups_and_pages(heads, kv_heads, S):
-    p = Packed([900, 0, 64, 1203], [12, 3, 0, 40], heads=heads, kv_heads=kv_heads, S=S, seed=S)
+@pytest.mark.parametrize("room", ROOMS)
+@pytest.mark.parametrize("heads,kv_heads,S", [(1, 1, 16), (8, 1, 8), (6, 2, 32), (64, 2, 64), (20, 4, 16), (24, 1, 8), (32, 2, 32)])
+def test_tree_groups_and_pages(heads, kv_heads, S, room):
+    p = Packed([900, 0, 64, 1203], [12, 3, 0, 40], heads=heads, kv_heads=kv_heads, S=S, seed=S, room=room)
     t = Trees(p, seed=S, words=2)
     for half in (True, False):
         check_tree(p, t, *run_tree(p, t, half), half, SCALE, (heads, kv_heads, S, half))
@@ -119,14 +130,15 @@ def anything(rng, n, words):
 @pytest.mark.parametrize("kind", [nothing, everything, anything])
 def test_tree_masks(kind):
     """Also rows that see no drafted node, and, without a context, nothing at all: out 0, lse -inf."""
-    p = Packed([0, 50, 128], [20, 70, 64], heads=4, kv_heads=2, seed=3)
-    t = Trees(p, kind=kind, words=3)
-    for half in (True, False):
-        for ws in ("full", None):
-            out, lse = run_tree(p, t, half, workspace=ws)
-            check_tree(p, t, out, lse, half, SCALE, (kind.__name__, half))
-            if kind is nothing:
-                assert bool((out[:20] == 0).all()) and bool((lse[:20] == -math.inf).all())
+    for room in ROOMS:
+        p = Packed([0, 50, 128], [20, 70, 64], heads=4, kv_heads=2, seed=3, room=room)
+        t = Trees(p, kind=kind, words=3)
+        for half in (True, False):
+            for ws in ("full", None):
+                out, lse = run_tree(p, t, half, workspace=ws)
+                check_tree(p, t, out, lse, half, SCALE, (kind.__name__, half, room))
+                if kind is nothing:
+                    assert bool((out[:20] == 0).all()) and bool((lse[:20] == -math.inf).all())
 
 
 @pytest.mark.parametrize("S", [8, 16, 32, 64])
@@ -134,7 +146,7 @@ def test_tree_masks(kind):
 def test_tree_listed_pages(S, K):
     """Lists as the selection leaves them, and with holes, ids of pages without tokens and a page twice."""
     rng = np.random.default_rng(S * K)
-    p = Packed([1500, 30, 777], [9, 20, 1], heads=8, kv_heads=2, S=S, seed=K)
+    p = Packed([1500, 30, 777], [9, 20, 1], heads=8, kv_heads=2, S=S, seed=K)   # (40 pages of 64: more than a row has)
     lists = np.full((3, 2, K), -1, np.int32)
     for b in range(3):
         pages = -(-p.lens[b] // S)
@@ -153,6 +165,50 @@ def test_tree_listed_pages(S, K):
         for half in (True, False):
             for ws in ("full", None):
                 check_tree(p, t, *run_tree(p, t, half, workspace=ws), half, SCALE, (S, K, half, ws))
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+def test_tree_many_rows_listed_pages(S):
+    """Row tiles of 256 rows over lists that do not fit the small kernel, holes and missing pages among them."""
+    rng = np.random.default_rng(S)
+    p = Packed([5000, 70, 4100], [50, 33, 60], heads=16, kv_heads=2, S=S, seed=S)
+    K = 2600 // S
+    lists = rng.integers(-3, 5100 // S, (3, 2, K))
+    t = Trees(p, lists=lists, seed=1)
+    for half in (True, False):
+        for ws in ("full", None):
+            check_tree(p, t, *run_tree(p, t, half, workspace=ws), half, SCALE, (S, half, ws))
+
+
+def test_tree_of_more_sequences_than_lanes():
+    """Splits planned over three groups of 64 sequences, one of them long."""
+    rng = np.random.default_rng(9)
+    new = [int(x) for x in rng.integers(0, 9, 140)]
+    lens = [int(x) for x in rng.integers(0, 200, 140)]
+    lens[100] = 20000
+    for room in ROOMS:
+        p = Packed(lens, new, heads=2, kv_heads=1, seed=9, room=room)
+        t = Trees(p)
+        check_tree(p, t, *run_tree(p, t, True), True, SCALE, room)
+
+
+def test_smaller_workspaces():
+    """Any size is used as far as it goes; nothing is written behind it."""
+    p = Packed([6000, 3500], [3, 2], heads=8, kv_heads=2, seed=4)
+    t = Trees(p)
+    many = Packed([6000, 3500], [60, 100], heads=8, kv_heads=2, seed=4)
+    for x, call in ((p, "tree"), (p, "prompt"), (many, "prompt")):
+        full = Q.quest_tokens_workspace_bytes(x.cache, x.total)
+        for size in (16, 1 << 20, 5 << 20, full // 2, full):
+            ws = torch.full((size // 4 + 64,), 5.0, device=x.dev)
+            out, lse = x.results(False)
+            if call == "tree":
+                Q.quest_tree_attention(x.cache, x.q, x.k_new, x.v_new, x.cu, t.mask, SCALE, out, lse=lse, workspace=ws[:size // 4])
+                check_tree(x, t, out, lse, False, SCALE, size)
+            else:
+                Q.quest_prompt_attention(x.cache, x.q, x.cu, SCALE, out, lse=lse, workspace=ws[:size // 4])
+                check_prompt(x, out, lse, False, SCALE, size)
+            assert bool((ws[size // 4:] == 5).all())
 
 
 @pytest.mark.parametrize("scale", [-SCALE, 0.0, 1.0])
