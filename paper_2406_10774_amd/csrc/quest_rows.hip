@@ -145,20 +145,49 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   }
   if (!second) __syncthreads();
 
-  if (!there) return;
+  // Results: through LDS, so that 16 lanes write a row's 256 bytes together.  Two buffers that nobody reads any more have 8 KiB
+  // for every wave; k_place spreads the lanes over the banks.
+  if (row0 >= w.rows) return;
   const float total = st.total();
+  char* mine = lds[(steps + wave / 4) & (kBuffers - 1)][0] + wave % 4 * (32 * kRowBytes);
+  const int r = lane & 31;
+  auto write_rows = [&](char* to, int index, size_t row_bytes) {   // index: of the lane's row
+    lds_in_order();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = i * 4 + (lane >> 4);
+      const size_t row = (uint32_t)__builtin_amdgcn_ds_bpermute(at * 4, index);
+      const uint4 v = ld16(mine + k_place(at, lane & 15));
+      if (row0 + at < w.rows) st16(to + row * row_bytes + (lane & 15) * 16, v);
+    }
+    lds_in_order();
+  };
+  auto write_floats = [&](float factor, float* to, int index) {   // 64 channels, then the others
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      st.each4(factor, lane, [&](int d, float4 o) {
+        if (d / 64 == half) *reinterpret_cast<float4*>(mine + k_place(r, d % 64 / 4)) = o;
+      });
+      write_rows((char*)to + half * 256, index, kHeadDim * sizeof(float));
+    }
+  };
   if (!w.whole()) {
-    const size_t part = w.part_row(a, wave * 32 + (lane & 31));
-    st.each4(RowState<kExact, true>::kUnscale, lane,
-             [&](int d, float4 o) { *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d) = o; });
-    if (lane < 32) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(st.base, total);
+    const size_t part = w.part_row(a, wave * 32);
+    write_floats(st.kUnscale, a.part_acc + part * kHeadDim, r);
+    if (lane < 32 && there) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(st.base, total);
     return;
   }
-  const size_t out_row = (size_t)(w.s.first + token) * (a.kv_heads * a.group) + head;
-  const float factor = total > 0.f ? RowState<kExact, true>::kUnscale / total : 0.f;
-  st.each4(factor, lane, [&](int d, float4 o) { store4(a.out, a.out_is_fp16, out_row * kHeadDim + d, o); });
-  if (a.lse != nullptr && lane < 32)
-    a.lse[out_row] = st.lse(st.base, total, a.scale);
+  const int out_row = (w.s.first + token) * (a.kv_heads * a.group) + head;
+  const float factor = total > 0.f ? st.kUnscale / total : 0.f;
+  if constexpr (kExact) {
+    write_floats(factor, (float*)a.out, out_row);
+  } else {
+    st.each4(factor, lane, [&](int d, float4 o) {
+      store4(mine + k_place(r, d / 8) + d % 8 * 2, 1, 0, o);
+    });
+    write_rows((char*)a.out, out_row, kHeadDim * 2);
+  }
+  if (a.lse != nullptr && lane < 32 && there) a.lse[out_row] = st.lse(st.base, total, a.scale);
 }
 
 // Few rows: tiles of 32 tokens, each wave its own.
