@@ -354,7 +354,8 @@ int quest_prompt_attention(const quest_cache* cache, const void* q, int64_t q_st
  * seq_lens[b] cached tokens (0 is allowed here) and to those drafted nodes j of its own sequence whose
  * bit is set in its mask: bit j % 64 of tree_mask[row][j / 64] (device, [total_tokens][mask_words], n_b <= 64 *
  * mask_words; bits from n_b on are ignored).  A tree sets the bits of a node's ancestors and its
- * own; any mask will do.  Keys and values of the nodes are rows of k_new and v_new: cache and
+ * own; any mask will do.  (Keys and values of all n_b nodes have to be finite, also of those that no
+ * mask names.)  Keys and values of the nodes are rows of k_new and v_new: cache and
  * metadata are not touched, so that rejected nodes leave no trace; quest_append_tokens
  * puts the accepted ones in.  A node that attends to nothing gets out 0 and lse -infinity.
  * topk_idx (nullable): [batch][KV heads][k_pages] as in quest_sparse_decode: of the cache only the listed pages'

@@ -413,6 +413,10 @@ int quest_tree_attention(const quest_cache* cache, const void* q, int64_t q_stri
     set_error("%s: tree_mask must not be NULL", who);
     return QUEST_ERR_NULL;
   }
+  if ((uintptr_t)tree_mask % 8 != 0) {
+    set_error("%s: tree_mask must lie on 8 bytes", who);
+    return QUEST_ERR_SHAPE;
+  }
   if (mask_words < 1 || (topk_idx != nullptr && k_pages < 1)) {
     set_error("%s: mask_words, and k_pages with a page list, must be >= 1 (got %d, %d)", who, mask_words, k_pages);
     return QUEST_ERR_SHAPE;

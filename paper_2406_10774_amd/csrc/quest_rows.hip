@@ -182,9 +182,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   if constexpr (kExact) {
     write_floats(factor, (float*)a.out, out_row);
   } else {
-    st.each4(factor, lane, [&](int d, float4 o) {
-      store4(mine + k_place(r, d / 8) + d % 8 * 2, 1, 0, o);
-    });
+    st.each4(factor, lane, [&](int d, float4 o) { store_halves(mine + k_place(r, d / 8) + d % 8 * 2, o); });
     write_rows((char*)a.out, out_row, kHeadDim * 2);
   }
   if (a.lse != nullptr && lane < 32 && there) a.lse[out_row] = st.lse(st.base, total, a.scale);
@@ -292,9 +290,14 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   const size_t out_row = (size_t)(w.s.first + tok) * (a.kv_heads * a.group) + w.hk * a.group + (row - tok * a.group);
   const float factor = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    store4(a.out, a.out_is_fp16, out_row * kHeadDim + d0 + 4 * j,
-           make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor));
+  for (int j = 0; j < 4; ++j) {
+    const float4 v = make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor);
+    const size_t at = out_row * kHeadDim + d0 + 4 * j;
+    if constexpr (kExact)
+      *reinterpret_cast<float4*>((float*)a.out + at) = v;
+    else
+      store_halves((_Float16*)a.out + at, v);
+  }
   if (a.lse != nullptr && d0 == 0) a.lse[out_row] = st.lse(top, sum, a.scale);
 }
 
@@ -368,7 +371,11 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
     const int row = row0 + in_tile + r, token = row / a.group;
     const size_t out_row = (size_t)(s.first + token) * (a.kv_heads * a.group) + hk * a.group + (row - token * a.group);
     const float factor = sum > 0.f ? 1.f / sum : 0.f;
-    store_out2(a.out, a.out_is_fp16, out_row * kHeadDim + lane * 2, o0 * factor, o1 * factor);
+    const size_t at = out_row * kHeadDim + lane * 2;
+    if (a.out_is_fp16)
+      *reinterpret_cast<half2_t*>((_Float16*)a.out + at) = half2_t{half_of(o0 * factor), half_of(o1 * factor)};
+    else
+      *reinterpret_cast<float2*>((float*)a.out + at) = make_float2(o0 * factor, o1 * factor);
     if (a.lse != nullptr && lane == 0)
       a.lse[out_row] = RowState<false, false>::lse(top, sum, a.scale);
   }

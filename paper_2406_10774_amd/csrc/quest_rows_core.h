@@ -327,14 +327,14 @@ struct RowState {
   }
 };
 
-__device__ __forceinline__ void store4(void* out, int out_is_fp16, size_t idx, float4 v) {
-  if (out_is_fp16) {
-    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-    const h4 h = {(_Float16)v.x, (_Float16)v.y, (_Float16)v.z, (_Float16)v.w};
-    *reinterpret_cast<h4*>(reinterpret_cast<_Float16*>(out) + idx) = h;
-  } else {
-    *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + idx) = v;
-  }
+// An fp16 output.  It is a mean of fp16 values, but weights rounded to fp16 may add up to 2^-11 more than their sum: what
+// that carries past the largest fp16 is put back.
+__device__ __forceinline__ _Float16 half_of(float x) {
+  return (_Float16)(fabsf(x) < 65552.f ? __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f) : x);
+}
+__device__ __forceinline__ void store_halves(void* to, float4 v) {
+  typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<h4*>(to) = h4{half_of(v.x), half_of(v.y), half_of(v.z), half_of(v.w)};
 }
 
 // Where the 16-byte chunk `slot` of a token's key (value) lies in its LDS tile.

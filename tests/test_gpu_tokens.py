@@ -219,6 +219,46 @@ def test_tree_scales(scale):
         check_tree(p, t, *run_tree(p, t, half, scale), half, scale, scale)
 
 
+def test_without_lse():
+    for new in (3, 80):
+        p = Packed([2000, 9], [new, 9], heads=6, kv_heads=2, seed=new, room=4096)
+        t = Trees(p)
+        for ws in (p.workspace(), None):
+            for with_lse in (True, False):
+                out, lse = p.results(True)
+                Q.quest_prompt_attention(p.cache, p.q, p.cu, SCALE, out, lse=lse if with_lse else None, workspace=ws)
+                tree, tree_lse = p.results(True)
+                Q.quest_tree_attention(p.cache, p.q, p.k_new, p.v_new, p.cu, t.mask, SCALE, tree, workspace=ws,
+                                       lse=tree_lse if with_lse else None)
+                if with_lse:
+                    want = out, tree
+                else:
+                    assert torch.equal(out, want[0]) and torch.equal(tree, want[1])
+                    assert bool((lse == 77).all()) and bool((tree_lse == 77).all())
+
+
+@pytest.mark.parametrize("room", ROOMS)
+def test_more_query_heads_than_a_row_tile(room):
+    p = Packed([70, 900], [3, 2], heads=600, kv_heads=2, seed=1, room=room)
+    t = Trees(p)
+    check_prompt(p, *run_prompt(p, True), True, SCALE, room)
+    check_tree(p, t, *run_tree(p, t, False), False, SCALE, room)
+
+
+@pytest.mark.parametrize("room", ROOMS)
+def test_largest_values(room):
+    """Values at fp16's largest: their mean is that, whatever the weights' roundings, in one piece and in splits."""
+    p = Packed([2500, 300], [20, 300], heads=8, kv_heads=2, seed=11, room=room)
+    p.v_pool[...] = torch.where(p.v_pool.isnan(), p.v_pool, 65504.0)
+    p.v_new[:320] = 65504.0
+    t = Trees(p)
+    for ws in ("full", None):
+        for out, _ in (run_prompt(p, True, workspace=ws), run_tree(p, t, True, workspace=ws)):
+            assert bool(((out[:320].float() - 65504).abs() <= 65504 * 2.0 ** -10).all())    # finite, within a step and a half
+        for out, _ in (run_prompt(p, False, workspace=ws), run_tree(p, t, False, workspace=ws)):
+            assert bool(((out[:320] - 65504).abs() <= 65504 * 2.0 ** -18).all())
+
+
 @pytest.mark.parametrize("half", [True, False])
 @pytest.mark.parametrize("n,ctx", [(7, 900), (300, 900)])
 def test_largest_logits(n, ctx, half):

@@ -37,7 +37,7 @@ def call(name, cache=None, **kw):
 @pytest.mark.parametrize("cache,status", [
     (dict(head_dim=64), -3), (dict(page_size=24), -3), (dict(batch=0), -2), (dict(num_heads=70000), -2),
     (dict(page_table=None), -1), (dict(seq_lens=None), -1), (dict(k_pool=None), -1), (dict(v_pool=None), -1),
-    (dict(num_kv_heads=5), -2), (dict(max_pages_per_seq=0), -2)])
+    (dict(num_kv_heads=5), -2), (dict(max_pages_per_seq=0), -2), (dict(max_pages_per_seq=2 ** 27 - 1), -2)])
 def test_bad_caches(name, cache, status):
     assert call(name, cache) == status
     assert name.encode() in binding.load().quest_last_error()
@@ -62,6 +62,7 @@ REFUSED = [
     ("quest_tree_attention", dict(mask=None), -1), ("quest_tree_attention", dict(words=0), -2),
     ("quest_tree_attention", dict(topk=P, k_pages=0), -2), ("quest_tree_attention", dict(new_stride=1000), -2),
     ("quest_tree_attention", dict(q_stride=0), -2), ("quest_tree_attention", dict(out=P + 2), -2),
+    ("quest_tree_attention", dict(mask=P + 4), -2),
 ]
 
 
@@ -103,12 +104,78 @@ def test_workspace_bytes():
     assert lib.quest_tokens_workspace_bytes(None, 4, ctypes.byref(out)) == -1
 
 
-def test_binding_refuses_rows_it_cannot_describe():
-    """Heads apart, keys and values with different strides: before the library is asked."""
-    x = torch.zeros(6, 16, 128, dtype=torch.float16)
-    for k, v in ((x[:, ::2], x[:, ::2]), (x[:, :8], x[::2][:, :8]), (x[:, :8], torch.zeros(6, 8, 128, dtype=torch.float16)),
-                 (x.transpose(1, 2)[:, :, :8], x.transpose(1, 2)[:, :, :8])):
+def test_workspace_bytes_do_not_fall():
+    """Enough for every smaller number of tokens as well; nothing for rows of a page table that nothing is split in."""
+    lib, out = binding.load(), ctypes.c_size_t(7)
+    for kw in (dict(), dict(num_kv_heads=32), dict(batch=1, num_heads=1, num_kv_heads=1), dict(batch=500), dict(max_pages_per_seq=90)):
+        c, last = make_cache(**kw), 0
+        for total in (0, 1, 5, 33, 100, 1000, 30000, 1000000):
+            assert lib.quest_tokens_workspace_bytes(ctypes.byref(c), total, ctypes.byref(out)) == 0
+            assert last <= out.value <= 160 << 20
+            last = out.value
+    c = make_cache(max_pages_per_seq=20)
+    assert lib.quest_tokens_workspace_bytes(ctypes.byref(c), 100, ctypes.byref(out)) == 0 and out.value == 0
+
+
+class Caller:
+    """Tensors of a valid call, on the CPU (refused, or of no rows: nothing is read)."""
+
+    def __init__(self, rows=6):
+        self.pool = torch.zeros(3, 8, 16, 128, dtype=torch.float16)
+        self.meta = torch.zeros(8, 3, 2, 128, dtype=torch.float16)
+        self.cu, lens = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+        self.cache = binding.Cache(self.pool, self.pool, self.meta, torch.zeros(2, 4, dtype=torch.int32), lens, num_heads=16)
+        self.q, self.kv = torch.zeros(rows, 16, 128, dtype=torch.float16), torch.zeros(rows, 8, 128, dtype=torch.float16)
+        self.mask, self.out = torch.zeros(rows, 1, dtype=torch.int64), torch.zeros(rows, 16, 128)
+        self.lse, self.lists = torch.zeros(rows, 16), torch.zeros(2, 8, 5, dtype=torch.int32)
+
+    def append(self, **kw):
+        a = dict(k_new=self.kv, v_new=self.kv, cu_tokens=self.cu, rows=None, stream=0) | kw
+        binding.quest_append_tokens(self.cache, **a)
+
+    def prompt(self, **kw):
+        a = dict(q=self.q, cu_tokens=self.cu, sm_scale=1.0, out=self.out, lse=self.lse, stream=0) | kw
+        binding.quest_prompt_attention(self.cache, **a)
+
+    def tree(self, **kw):
+        a = dict(q=self.q, k_new=self.kv, v_new=self.kv, cu_tokens=self.cu, tree_mask=self.mask, sm_scale=1.0, out=self.out,
+                 topk_idx=self.lists, lse=self.lse, stream=0) | kw
+        binding.quest_tree_attention(self.cache, **a)
+
+
+def test_binding_refuses_what_it_cannot_describe():
+    """Types, gaps, too few rows or heads: before the library is asked."""
+    c = Caller()
+    wide = torch.zeros(6, 16, 128, dtype=torch.float16)
+    for k, v in ((wide[:, ::2], wide[:, ::2]), (wide[:, :8], c.kv), (wide, wide), (c.kv.float(), c.kv.float()),
+                 (c.kv, c.kv[:5]), (c.kv, c.kv.bfloat16()), (c.kv[:, :4], c.kv[:, :4]),
+                 (c.kv.transpose(1, 2).contiguous().transpose(1, 2), c.kv.transpose(1, 2).contiguous().transpose(1, 2))):
+        for call in (c.append, c.tree):
+            with pytest.raises(binding.QuestError):
+                call(k_new=k, v_new=v)
+    bad = [dict(cu_tokens=c.cu[:2]), dict(cu_tokens=c.cu.long())]
+    for kw in bad + [dict(rows=c.cu.long()), dict(rows=torch.zeros(8, dtype=torch.int32)[::2])]:
         with pytest.raises(binding.QuestError):
-            binding._row_stride(k, v)
-    assert binding._row_stride(x[:, 4:12], x[:, :8]) == 16 * 128
-    assert binding._row_stride(x[:1, :8]) == 8 * 128
+            c.append(**kw)
+    bad += [dict(q=c.q[:, :8]), dict(q=c.q.float()), dict(out=c.out[:5]), dict(out=c.out.bfloat16()), dict(out=c.out.double()),
+            dict(out=torch.zeros(6, 17, 128)[:, :16]), dict(out=torch.zeros(16, 6, 128).transpose(0, 1)), dict(out=c.out[:, :8].contiguous()), dict(lse=c.lse[:4]), dict(lse=c.lse.half()),
+            dict(lse=torch.zeros(6, 15))]
+    for kw in bad:
+        for call in (c.prompt, c.tree):
+            with pytest.raises(binding.QuestError):
+                call(**kw)
+    for kw in (dict(tree_mask=c.mask.int()), dict(tree_mask=c.mask[:5]), dict(tree_mask=torch.zeros(6, 2, dtype=torch.int64)[:, :1]),
+               dict(topk_idx=c.lists.long()), dict(topk_idx=c.lists[:1]), dict(topk_idx=c.lists[:, :, ::2]),
+               dict(k_new=c.kv[:5], v_new=c.kv[:5])):
+        with pytest.raises(binding.QuestError):
+            c.tree(**kw)
+
+
+def test_binding_takes_strided_rows():
+    """Parts of a fused projection; no rows at all are no work, so these return without a GPU."""
+    c = Caller(rows=0)
+    c.append(), c.prompt(), c.tree(), c.tree(topk_idx=None, lse=None), c.prompt(lse=None)
+    fused = torch.zeros(7, 32, 128, dtype=torch.float16)
+    assert binding._rows_of((7, 16, 128), fused[:, :16], 16) == 32 * 128
+    assert binding._rows_of((7, 8, 128), fused[:, 16:24], 8, fused[:, 24:]) == 32 * 128
+    assert binding._rows_of((1, 16, 128), fused[3:4, :16], 16) == 16 * 128
