@@ -324,46 +324,46 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   if (parts == 1) return;  // written already
   const size_t step = (size_t)s.row_tiles * a.kv_heads * kRows;   // rows between two splits' parts
   const size_t part0 = (((size_t)s.units_before + (s.row_tiles - 1 - (tile - s.before))) * a.kv_heads + hk) * kRows + in_tile;
-  const float* ml = a.part_ml + part0 * 2;
-  const float* from = a.part_acc + part0 * kHeadDim + lane * 2;
-  float2 v[8], mine;
-  auto ask = [&](int r, int i) {   // eight parts' outputs of row r
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      v[j] = *reinterpret_cast<const float2*>(from + (min(i + j, parts - 1) * step + r) * kHeadDim);
-  };
-  auto ask_weight = [&](int r, int i) {
-    return *reinterpret_cast<const float2*>(ml + (min(i + lane, parts - 1) * step + r) * 2);
-  };
   const int n_rows = min(kEach, rows - row0 - in_tile);
-  mine = ask_weight(0, 0);
-  ask(0, 0);
+#pragma unroll 1
   for (int r = 0; r < n_rows; ++r) {
-    float top = lane < parts && mine.y > 0.f ? mine.x : kNegBig;
-    for (int i = kWave; i < parts; i += kWave) {
-      const float2 x = ask_weight(r, i);
-      if (i + lane < parts && x.y > 0.f) top = fmaxf(top, x.x);
+    const float2* from = reinterpret_cast<const float2*>(a.part_acc + (part0 + r) * kHeadDim) + lane;
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + part0 + r;
+    float2 v[8];
+    auto ask = [&](int n) {   // the next n parts' outputs
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = *from;
+        if (j < n - 1) from += step * (kHeadDim / 2);
+      }
+    };
+    ask(parts);
+    float top = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll 1
+    for (int base = 0; base < parts; base += kWave) {
+      const float2 x = ml[min(base + lane, parts - 1) * step];
+      if (x.y > 0.f) top = fmaxf(top, x.x);
     }
 #pragma unroll
     for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-    float sum = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll 1
     for (int base = 0; base < parts; base += kWave) {
-      if (base > 0) mine = ask_weight(r, base);
-      const float weight = base + lane < parts && mine.y > 0.f ? __builtin_amdgcn_exp2f((mine.x - top) * a.scale) : 0.f;
-      sum += weight * mine.y;
+      const float2 x = ml[min(base + lane, parts - 1) * step];
+      const float weight = base + lane < parts && x.y > 0.f ? __builtin_amdgcn_exp2f((x.x - top) * a.scale) : 0.f;
+      sum += weight * x.y;
       const int n = min(parts - base, kWave);
-      if (base + n == parts) mine = ask_weight(min(r + 1, n_rows - 1), 0);
+#pragma unroll 1
       for (int i = 0; i < n; i += 8) {
+        float2 now[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) now[j] = v[j];
+        if (base + i + 8 < parts) ask(parts - base - i - 8);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float x = i + j < n ? from_lane(weight, i + j) : 0.f;
-          o0 += v[j].x * x;
-          o1 += v[j].y * x;
+          const float w = i + j < n ? from_lane(weight, i + j) : 0.f;
+          o0 += now[j].x * w;
+          o1 += now[j].y * w;
         }
-        if (i + 8 < n || base + n < parts)
-          ask(r, base + i + 8);
-        else
-          ask(min(r + 1, n_rows - 1), 0);
       }
     }
 #pragma unroll
@@ -376,8 +376,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
       *reinterpret_cast<half2_t*>((_Float16*)a.out + at) = half2_t{half_of(o0 * factor), half_of(o1 * factor)};
     else
       *reinterpret_cast<float2*>((float*)a.out + at) = make_float2(o0 * factor, o1 * factor);
-    if (a.lse != nullptr && lane == 0)
-      a.lse[out_row] = RowState<false, false>::lse(top, sum, a.scale);
+    if (a.lse != nullptr && lane == 0) a.lse[out_row] = RowState<false, false>::lse(top, sum, a.scale);
   }
 }
 
