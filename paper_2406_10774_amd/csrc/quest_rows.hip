@@ -1,11 +1,15 @@
 // Attention of prompts (causal) and of trees of drafted tokens over the paged cache.  See quest_rows_core.h.
 //
-// Two kernels.  Many rows: four waves of 32 rows share the tiles of tokens, which are fetched once for 128 rows.
-// Few rows: every wave of a work-group has all 32 (or 64) rows and tiles of its own, so that four waves
-// stream tokens however few the rows are; their results are joined in LDS.
-//
-// A tile's tokens are walked in splits of `chunk` tiles where that gives the compute units more to do; rows with more
-// than one leave partial results, which merge_rows_kernel joins.
+// Two kernels, chosen by the rows that a sequence has on average and by the tokens that a row may attend to (plan_of):
+//   many rows (shared_rows_kernel)  eight waves of 32 rows share the tiles of tokens, fetched once for 256 rows.  Bound by
+//            the matrix cores and by power: 32k tokens of 32 query / 8 KV heads 8.2 to 8.5 ms, 1040 to 1070 TFLOP/s (a large
+//            library product 1310), at 1.9 GHz; with zeros for data the clock stays at 2.4 GHz and it is 7.0.
+//   few rows (few_rows_kernel)      every wave of a work-group has all 32 rows and tiles of its own, so that four waves
+//            stream tokens however few the rows are; their results are joined in LDS.  Bound by memory, or by the chain
+//            of loads before the first tile: 26 drafts at 32k tokens of 32 heads 105 us, 5.1 TB/s.
+// A row tile's tokens are walked in splits where that gives the compute units more to do; a row tile with more than one
+// leaves partial results, which merge_rows_kernel joins (a launch of its own: 4 to 7 us, and up to 64 splits are
+// joined by as many work-groups as there are rows, not by the last one to arrive).
 #include <algorithm>
 
 #include "quest_common.h"
@@ -16,11 +20,11 @@ namespace quest {
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;                            // few_rows_kernel
 constexpr int kFewRows = 32;
-constexpr int kSharedWaves = 8;
+constexpr int kSharedWaves = 8;                      // shared_rows_kernel
 constexpr int kSharedRows = 32 * kSharedWaves;
-constexpr int kBuffers = 4;
+constexpr int kBuffers = 4;                          // tiles of tokens in LDS
 
 // A work-group's part: a unit of one KV head.  Adjacent work-groups have adjacent heads: with a multiple of eight KV heads
 // a head's units are all on one die, whose L2 then holds what its row tiles read at the same time.
@@ -61,6 +65,12 @@ struct Part {
 // the other four's softmax of tile t - 1, in turn 2t + 1 they change places.  In its turn of softmax of tile t a wave
 // also asks for its share of tile t + 2, straight into LDS; it waits for that at the end of its next products, a turn
 // before anyone reads it.  Four buffers: values of tile t - 2 are read until turn 2t - 1, its place is written from 2t + 1.
+//
+// A turn takes about 1900 cycles: the products 1450 (32 of 32 cycles; 32 KiB from LDS for each wave), the softmax 1000 and
+// the fetch 300 to 700.  32k tokens of 32 / 8 heads took 12.2 ms with all waves in the same turn, 8.5 with the tiles through
+// registers (this: 8.2), 9.7 in work-groups of 128 rows and no turns, two on a compute unit, and 9.9 with one
+// wave of 64 rows on each SIMD and the softmax between its own products.  Reading keys or values of the next turn
+// ahead changed it by less than 1 %.
 template <bool kTree, bool kExact>
 __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -188,7 +198,9 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   if (a.lse != nullptr && lane < 32 && there) a.lse[out_row] = st.lse(st.base, total, a.scale);
 }
 
-// Few rows: tiles of 32 tokens, each wave its own.
+// Few rows: tiles of 32 tokens, each wave its own; 16 KiB on the way to each wave's registers, 128 KiB for a compute unit.
+// With 64 rows a wave (one work-group on a compute unit instead of two) 64 rows took as long as two tiles of 32: 61 us and 58
+// at 65k tokens of 8 heads.
 template <bool kTree, bool kExact>
 __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -381,6 +393,15 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 }
 
 // How a call is cut up, from what the host knows.
+//   Kernel: the small one up to 64 rows a sequence on average (64 rows at 65k tokens of 8 heads: 56 us and 63; 128 rows:
+//   89 and 67), and where no row can attend to more than 1536 tokens (1500 tokens of 32 / 8 heads: 51 us and 66; 2000: 80
+//   and 57).
+//   Splits: so many that the work-groups fill the compute units once; an even share then ends at the same time
+//   everywhere (26 drafts at 32k tokens: 105 us, with twice as many 110, four times 122).  Where there are row tiles for
+//   more than a quarter of that (prompts: an eighth) their unequal ends weigh more than a start does, and the share
+//   is cut into rounds: two, and four for many rows of trees (sixteen ragged trees of 1 to 2 tiles: 1830 us in one
+//   round, 1290 in two, 1040 in four).  None where the row tiles alone fill the compute units (prompts: to three
+//   quarters; 2000 tokens of 32 / 8 heads: 57 us, 77 with), or rows have at most eight tiles of tokens.
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
   int row_tiles;                // of a KV head, at most
@@ -483,7 +504,7 @@ size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) {
 }
 
 bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {
-  return ((int64_t)total_tokens * group_size(c) + 128 * (int64_t)c.batch) * kv_heads(c) <= INT32_MAX;
+  return ((int64_t)total_tokens * group_size(c) + 2 * kSharedRows * (int64_t)c.batch) * kv_heads(c) <= INT32_MAX;
 }
 
 int launch_prompt(const quest_cache& c, const PackedTokens& p, const void* q, int64_t q_stride, float sm_scale, void* out,

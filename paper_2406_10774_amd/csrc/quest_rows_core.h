@@ -20,10 +20,11 @@
 // value with 4 (token % 4): the lanes of a read spread over all banks.
 //
 // Weights go to the product in fp16.  For fp16 outputs one rounding of each weight, 2^-11 of it, which is what the
-// output's own rounding costs; the reference exponent is put 7 below the largest logit (log2) seen when it last
-// moved and moves when a weight would pass 2^15, so weights keep all bits down to 2^-21 of the largest and are not
-// lost down to 2^-32.  For fp32 outputs a weight is two fp16 numbers, 2^14 times its value rounded and what that leaves: 22
-// bits of it.  Sums, maxima and accumulators are fp32.
+// output's own rounding costs (error against 64 bits, 2-norm: 1.3 times that of one rounding at the end); the base is
+// put so that the largest logit's weight is 2^7 and moves when a weight would pass 2^15, so weights keep all bits down
+// to 2^-21 of the largest and are not lost down to 2^-31.  For fp32 outputs a weight is two fp16 numbers, 2^14 times its
+// value rounded and what that leaves, 22 bits of it: error 4e-7, three times below fp32 products one after the other.
+// Sums, maxima and accumulators are fp32.
 #pragma once
 
 #include <type_traits>
