@@ -398,9 +398,9 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 //   and 57).
 //   Splits: so many that the work-groups fill the compute units once; an even share then ends at the same time
 //   everywhere (26 drafts at 32k tokens: 105 us, with twice as many 110, four times 122).  Where there are row tiles for
-//   more than a quarter of that (prompts: an eighth) their unequal ends weigh more than a start does, and the share
+//   more than half of that (many rows of trees: a quarter) their unequal ends weigh more than a start does, and the share
 //   is cut into rounds: two, and four for many rows of trees (sixteen ragged trees of 1 to 2 tiles: 1830 us in one
-//   round, 1290 in two, 1040 in four).  None where the row tiles alone fill the compute units (prompts: to three
+//   round, 1245 in two, 1000 in four).  None where the row tiles alone fill the compute units (prompts: to three
 //   quarters; 2000 tokens of 32 / 8 heads: 57 us, 77 with), or rows have at most eight tiles of tokens.
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
@@ -420,7 +420,7 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   const int once = at_once(p.rows, c);
   p.row_tiles = (int)(rows / p.rows + c.batch);
   const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
-  const int rounds = !tree ? (likely * 8 <= once ? 1 : 2) : likely * 4 <= once ? 1 : few ? 2 : 4;
+    const int rounds = likely * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
   p.least_chunk = few ? 2 : 8;
   p.good_units = std::max(once * rounds, p.row_tiles + 1);
   p.most_units = tree ? p.good_units : 2 * p.good_units;

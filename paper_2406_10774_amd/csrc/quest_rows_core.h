@@ -122,10 +122,26 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
     count += whole(up_to_lane(row_tiles, lane));
   }
   if (kTree) work = all;
-  // ceil(tiles / chunk) summed over the row tiles is at most all / chunk + count (a hundred-thousandth covers the
-  // roundings)
+  // The chunk: with this one the units, ceil(tiles / chunk) summed over the row tiles, are at most all / chunk + count, so
+  // no more than there is room for (a hundred-thousandth covers the roundings) ..
   const float even = fmaxf(all / (float)max(a.most_units - count, 1), work / (float)max(a.good_units - count, 1)) * 1.00001f;
   s.chunk = a.most_units <= count || even > 1e9f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
+  if (s.chunk != INT32_MAX && a.batch <= kWave) {
+    // .. and that is more than needed, as a last split is half a chunk on average: the smallest with which they are
+    // still no more than wanted, within 3 %.
+    const int usual = kTree ? tiles : tiles - (int)(less * (float)max(row_tiles - 1, 0));
+    int low = max(a.least_chunk, (int)(work / (float)a.good_units)), high = s.chunk;   // high: few enough
+    while (high - low > high >> 5) {
+      const int chunk = (low + high) >> 1;
+      const int units = row_tiles * ((usual + chunk - 1) / chunk), most = row_tiles * ((tiles + chunk - 1) / chunk);
+      const bool fits = whole(up_to_lane(units, lane)) <= a.good_units && (kTree || whole(up_to_lane(most, lane)) <= a.most_units);
+      if (fits)
+        high = chunk;
+      else
+        low = chunk + 1;
+    }
+    s.chunk = high;
+  }
   int units_before = 0, tiles_before = 0;
   for (int base = 0; base < a.batch; base += kWave) {
     if (a.batch > kWave) read(base);
