@@ -151,7 +151,8 @@ class Cache:
             k_pool=k_pool.data_ptr(), v_pool=v_pool.data_ptr() if v_pool is not None else None,
             meta=meta.data_ptr(), page_table=page_table.data_ptr(), seq_lens=seq_lens.data_ptr(),
             num_kv_heads=0 if H == Hkv else Hkv)
-        self.heads, self.kv_heads, self.batch = H, Hkv, page_table.shape[0]
+        self.heads, self.kv_heads, self.batch, self.head_dim = H, Hkv, page_table.shape[0], D
+        self.device = k_pool.get_device()
 
     @property
     def ref(self):
@@ -238,7 +239,7 @@ def quest_decode_step_static(cache: Cache, k_new, v_new, k_pool_write, q, k_page
 
 # ---- many tokens a sequence.  Packed tensors are [rows][heads][head_dim] with any stride between rows.
 
-# (What is checked here costs about 2 us a call, a part of them a tensor's shape and strides.)
+# (What is checked here costs 2 to 3 us a call, a part of them a tensor's shape, strides and device.)
 
 _types = None
 
@@ -251,41 +252,53 @@ def _types_of_torch():
     return _types
 
 
-def _rows_of(shape, t, heads, other=None):
+def _rows_of(cache, shape, t, heads, other=None):
     """Elements between the rows of t (its shape, t), and of `other`: fp16 rows whose heads lie next to each other."""
-    stride = t.stride()
-    if (t.dtype is _half and len(shape) == 3 and shape[1] == heads and stride[2] == 1 and (stride[1] == shape[2] or heads == 1)
-            and (other is None or other.dtype is _half and other.stride() == stride and other.shape == shape)):
-        return stride[0] if shape[0] > 1 else heads * shape[2]
-    what = "" if other is None else f", {tuple(other.shape)} and {other.stride()} ({other.dtype})"
-    raise QuestError(-2, f"packed rows of shape {tuple(shape)} and strides {stride} ({t.dtype}){what}: they have to be fp16 "
-                         f"[rows][{heads}][head_dim], heads next to each other, keys as values")
+    stride, dim, device = t.stride(), cache.head_dim, cache.device
+    if (t.dtype is _half and len(shape) == 3 and shape[1] == heads and shape[2] == dim and stride[2] == 1
+            and (stride[1] == dim or heads == 1) and t.get_device() == device
+            and (other is None or other.dtype is _half and other.stride() == stride and other.shape == shape
+                 and other.get_device() == device)):
+        return stride[0] if shape[0] > 1 else heads * dim
+    what = "" if other is None else f", {tuple(other.shape)} and {other.stride()} ({other.dtype}, {other.device})"
+    raise QuestError(-2, f"packed rows of shape {tuple(shape)} and strides {stride} ({t.dtype}, {t.device}){what}: they have to "
+                         f"be fp16 [rows][{heads}][{dim}] on the cache's device, heads next to each other, keys as values")
 
 
-def _plain(t, dtype, least, what):
-    """Refuses a tensor of another type, with gaps, or with fewer elements."""
-    if t.dtype is not dtype or t.numel() < least or not t.is_contiguous():
-        raise QuestError(-2, f"{what} of shape {tuple(t.shape)}, strides {t.stride()} ({t.dtype}): has to be {dtype}, "
-                             f"contiguous, of at least {least} elements")
+def _plain(cache, t, dtype, least, what):
+    """Refuses a tensor of another type or device, with gaps, or with fewer elements."""
+    if t.dtype is not dtype or t.numel() < least or not t.is_contiguous() or t.get_device() != cache.device:
+        raise QuestError(-2, f"{what} of shape {tuple(t.shape)}, strides {t.stride()} ({t.dtype}, {t.device}): has to be {dtype}, "
+                             f"contiguous, of at least {least} elements, on the cache's device")
 
 
-def _outputs(out, lse, rows, heads, dim):
-    _plain(out, _half if out.dtype is _half else _types[0], rows * heads * dim, "out")
+def _outputs(cache, out, lse, workspace, rows):
+    _plain(cache, out, _half if out.dtype is _half else _types[0], rows * cache.heads * cache.head_dim, "out")
     if lse is not None:
-        _plain(lse, _types[0], rows * heads, "lse")
+        _plain(cache, lse, _types[0], rows * cache.heads, "lse")
+    if workspace is not None:
+        _plain(cache, workspace, workspace.dtype, 0, "workspace")
+
+
+def _stream_of(cache, stream):
+    """The stream, or the current one; the cache's device has to be the current one."""
+    device = cache.device
+    if device >= 0 and _current_device() != device:
+        raise QuestError(-2, f"the cache lies on device {device}, which is not the current one")
+    return _stream(stream)
 
 
 def quest_append_tokens(cache: Cache, k_new, v_new, cu_tokens, rows=None, stream=None):
     _, i32, _ = _types or _types_of_torch()
     shape = k_new.shape
-    stride = _rows_of(shape, k_new, cache.kv_heads, v_new)
+    stride = _rows_of(cache, shape, k_new, cache.kv_heads, v_new)
     total = shape[0]
     if rows is not None:
-        _plain(rows, i32, 0, "rows")
+        _plain(cache, rows, i32, 0, "rows")
         total = rows.numel()
-    _plain(cu_tokens, i32, cache.batch + 1, "cu_tokens")
+    _plain(cache, cu_tokens, i32, cache.batch + 1, "cu_tokens")
     _check(load().quest_append_tokens(cache.ref, k_new.data_ptr(), v_new.data_ptr(), stride, _ptr(rows),
-                                      cu_tokens.data_ptr(), total, _stream(stream)))
+                                      cu_tokens.data_ptr(), total, _stream_of(cache, stream)))
 
 
 def quest_tokens_workspace_bytes(cache: Cache, total_tokens: int) -> int:
@@ -297,13 +310,13 @@ def quest_tokens_workspace_bytes(cache: Cache, total_tokens: int) -> int:
 def quest_prompt_attention(cache: Cache, q, cu_tokens, sm_scale, out, lse=None, workspace=None, stream=None):
     _, i32, _ = _types or _types_of_torch()
     shape, heads = q.shape, cache.heads
-    stride = _rows_of(shape, q, heads)
+    stride = _rows_of(cache, shape, q, heads)
     total = shape[0]
-    _plain(cu_tokens, i32, cache.batch + 1, "cu_tokens")
-    _outputs(out, lse, total, heads, shape[2])
+    _plain(cache, cu_tokens, i32, cache.batch + 1, "cu_tokens")
+    _outputs(cache, out, lse, workspace, total)
     _check(load().quest_prompt_attention(
         cache.ref, q.data_ptr(), stride, cu_tokens.data_ptr(), total, float(sm_scale), out.data_ptr(),
-        out.dtype is _half, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+        out.dtype is _half, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream_of(cache, stream)))
 
 
 def quest_tree_attention(cache: Cache, q, k_new, v_new, cu_tokens, tree_mask, sm_scale, out, topk_idx=None, lse=None,
@@ -311,18 +324,18 @@ def quest_tree_attention(cache: Cache, q, k_new, v_new, cu_tokens, tree_mask, sm
     """tree_mask: int64 [rows][words]; topk_idx: int32 [batch][KV heads][k_pages], or None for all pages."""
     _, i32, i64 = _types or _types_of_torch()
     shape, heads, new_shape = q.shape, cache.heads, k_new.shape
-    q_stride = _rows_of(shape, q, heads)
-    new_stride = _rows_of(new_shape, k_new, cache.kv_heads, v_new)
+    q_stride = _rows_of(cache, shape, q, heads)
+    new_stride = _rows_of(cache, new_shape, k_new, cache.kv_heads, v_new)
     total, (mask_rows, words), k_pages = shape[0], tree_mask.shape, 0
     if new_shape[0] < total or mask_rows < total:
         raise QuestError(-2, f"{new_shape[0]} rows of keys and values and {mask_rows} of masks for {total} of queries")
-    _plain(tree_mask, i64, 0, "tree_mask")
-    _plain(cu_tokens, i32, cache.batch + 1, "cu_tokens")
+    _plain(cache, tree_mask, i64, 0, "tree_mask")
+    _plain(cache, cu_tokens, i32, cache.batch + 1, "cu_tokens")
     if topk_idx is not None:
         k_pages = topk_idx.shape[2]
-        _plain(topk_idx, i32, cache.batch * cache.kv_heads * k_pages, "topk_idx")
-    _outputs(out, lse, total, heads, shape[2])
+        _plain(cache, topk_idx, i32, cache.batch * cache.kv_heads * k_pages, "topk_idx")
+    _outputs(cache, out, lse, workspace, total)
     _check(load().quest_tree_attention(
         cache.ref, q.data_ptr(), q_stride, k_new.data_ptr(), v_new.data_ptr(), new_stride, cu_tokens.data_ptr(),
         total, tree_mask.data_ptr(), words, _ptr(topk_idx), k_pages, float(sm_scale), out.data_ptr(),
-        out.dtype is _half, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+        out.dtype is _half, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream_of(cache, stream)))

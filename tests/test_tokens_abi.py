@@ -37,7 +37,8 @@ def call(name, cache=None, **kw):
 @pytest.mark.parametrize("cache,status", [
     (dict(head_dim=64), -3), (dict(page_size=24), -3), (dict(batch=0), -2), (dict(num_heads=70000), -2),
     (dict(page_table=None), -1), (dict(seq_lens=None), -1), (dict(k_pool=None), -1), (dict(v_pool=None), -1),
-    (dict(num_kv_heads=5), -2), (dict(max_pages_per_seq=0), -2), (dict(max_pages_per_seq=2 ** 27 - 1), -2)])
+    (dict(num_kv_heads=5), -2), (dict(max_pages_per_seq=0), -2), (dict(max_pages_per_seq=2 ** 27 - 1), -2),
+    (dict(max_pages_per_seq=2 ** 27 - 1024), -2)])
 def test_bad_caches(name, cache, status):
     assert call(name, cache) == status
     assert name.encode() in binding.load().quest_last_error()
@@ -176,6 +177,28 @@ def test_binding_takes_strided_rows():
     c = Caller(rows=0)
     c.append(), c.prompt(), c.tree(), c.tree(topk_idx=None, lse=None), c.prompt(lse=None)
     fused = torch.zeros(7, 32, 128, dtype=torch.float16)
-    assert binding._rows_of((7, 16, 128), fused[:, :16], 16) == 32 * 128
-    assert binding._rows_of((7, 8, 128), fused[:, 16:24], 8, fused[:, 24:]) == 32 * 128
-    assert binding._rows_of((1, 16, 128), fused[3:4, :16], 16) == 16 * 128
+    assert binding._rows_of(c.cache, (7, 16, 128), fused[:, :16], 16) == 32 * 128
+    assert binding._rows_of(c.cache, (7, 8, 128), fused[:, 16:24], 8, fused[:, 24:]) == 32 * 128
+    assert binding._rows_of(c.cache, (1, 16, 128), fused[3:4, :16], 16) == 16 * 128
+
+
+def test_binding_refuses_other_devices_and_head_sizes(monkeypatch):
+    """The caller's tensors lie on the CPU here: the cache says that it lies elsewhere, or that the current device is
+    another."""
+    c = Caller()
+    narrow = torch.zeros(6, 8, 256, dtype=torch.float16)[:, :, :64]
+    for call in (c.append, c.tree):
+        with pytest.raises(binding.QuestError):
+            call(k_new=narrow, v_new=narrow)
+    one = binding.Cache(c.pool[:, :1], c.pool[:, :1], c.meta, c.cache.page_table, c.cache.seq_lens)
+    with pytest.raises(binding.QuestError):   # 64 channels, 128 apart
+        binding.quest_prompt_attention(one, c.q[:, :1, :64], c.cu, 1.0, torch.zeros(6, 1, 64), stream=0)
+    c.cache.device = 0
+    for call in (c.append, c.prompt, c.tree):
+        with pytest.raises(binding.QuestError, match="on the cache's device"):
+            call()
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    with pytest.raises(binding.QuestError, match="not the current one"):
+        binding._stream_of(c.cache, 5)
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    assert binding._stream_of(c.cache, 5) == 5
