@@ -345,6 +345,8 @@ int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens,
  * out [total_tokens][num_heads][head_dim] and lse [total_tokens][num_heads] dense.  fp32 logits, softmax and
  * sums; out is fp32 or fp16 as in quest_sparse_decode.  With fp16 out the softmax weights are
  * rounded to fp16 before they meet the values, with fp32 out they keep 22 bits.
+ * Values of all seq_lens[b] tokens have to be finite, also for queries that stand before them (a later token has the
+ * weight 0, and 0 times infinity is not 0); slots behind the last token may hold anything.
  * Results must not overlap what the call reads. */
 int quest_prompt_attention(const quest_cache* cache, const void* q, int64_t q_stride, const int32_t* cu_tokens,
                            int32_t total_tokens, float sm_scale, void* out, int32_t out_is_fp16, float* lse,

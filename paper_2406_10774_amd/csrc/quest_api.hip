@@ -111,7 +111,8 @@ int check_packed(const quest_cache* c, const int32_t* cu, int32_t total, const c
     set_error("%s: total_tokens must be >= 0 and total_tokens * num_heads fit a launch (got %d)", who, total);
     return QUEST_ERR_SHAPE;
   }
-  if ((int64_t)c->max_pages_per_seq * c->page_size + total > INT32_MAX - 128) {  // places of a row and its new tokens
+  // places of a row and its new tokens, and the look-ahead of 64 steps of 128 places
+  if ((int64_t)c->max_pages_per_seq * c->page_size + total > INT32_MAX - (1 << 14)) {
     set_error("%s: max_pages_per_seq * page_size and total_tokens exceed the int32 range", who);
     return QUEST_ERR_SHAPE;
   }

@@ -420,7 +420,7 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   const int once = at_once(p.rows, c);
   p.row_tiles = (int)(rows / p.rows + c.batch);
   const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
-    const int rounds = likely * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
+  const int rounds = likely * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
   p.least_chunk = few ? 2 : 8;
   p.good_units = std::max(once * rounds, p.row_tiles + 1);
   p.most_units = tree ? p.good_units : 2 * p.good_units;

@@ -328,7 +328,7 @@ struct RowState {
   }
   // log sum exp of a row, of its base and sum.
   __device__ __forceinline__ static float lse(float base, float total, float scale) {
-    return total > 0.f ? __builtin_fmaf(base, scale, __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+    return total == 0.f ? -INFINITY : __builtin_fmaf(base, scale, __builtin_amdgcn_logf(total)) * kLn2;  // (NaN stays)
   }
   static constexpr float kUnscale = kExact ? 1.f / kWeightScale : 1.f;
 

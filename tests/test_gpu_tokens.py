@@ -288,6 +288,24 @@ def test_largest_logits(n, ctx, half):
     assert bool((out[:n].float() == (visible.half() / 30000).float()[:, None, None]).all())
 
 
+@pytest.mark.parametrize("room", ROOMS)
+def test_nan_queries(room):
+    """A query that is not a number spoils its own row, sum and all, and no other."""
+    p = Packed([2500, 300], [20, 300], heads=8, kv_heads=2, seed=12, room=room)
+    t = Trees(p)
+    runs = [lambda half=half, ws=ws, run=run: run(half, ws) for half in (True, False) for ws in ("full", None)
+            for run in (lambda half, ws: run_prompt(p, half, workspace=ws), lambda half, ws: run_tree(p, t, half, workspace=ws))]
+    before = [run() for run in runs]
+    bad = torch.zeros(p.total, 8, dtype=torch.bool, device=p.dev)
+    for row, h in ((3, 1), (19, 7), (20, 0), (250, 5)):
+        bad[row, h] = True
+    p.q[bad, 17] = math.nan
+    for run, (out0, lse0) in zip(runs, before):
+        out, lse = run()
+        assert bool(out[bad].isnan().all()) and bool(lse[bad].isnan().all())
+        assert torch.equal(out[~bad], out0[~bad]) and torch.equal(lse[~bad], lse0[~bad])
+
+
 # ---- insertion
 
 def one_by_one(p, past, rows):
