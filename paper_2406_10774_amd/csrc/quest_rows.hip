@@ -45,15 +45,24 @@ struct Part {
     hk = blockIdx.x % a.kv_heads;
     unit = blockIdx.x / a.kv_heads;
     if (!find_sequence<kTree, kRows, false>(s, a, cu, seq_lens, kTree && topk != nullptr, unit, lane)) return false;
-    const int index = unit - s.before, split = index / s.row_tiles;
+    const int index = unit - s.before, slot = index / s.places<kTree>();
+    int split = slot, behind = index - slot * s.places<kTree>();   // the row tile, counted from the last one
+    if (s.paired<kTree>()) {
+      const int splits = s.splits_of<kRows>(s.row_tiles - 1 - behind, a.group);
+      if (slot >= splits) {
+        split = slot - splits;
+        if (2 * behind + 1 == s.row_tiles) return false;   // the one in the middle has its place alone
+        behind = s.row_tiles - 1 - behind;
+      }
+    }
     group = a.group;
     rows = s.tokens * group;
-    row0 = (s.row_tiles - 1 - (index - split * s.row_tiles)) * kRows;  // a prompt's last rows have the most work
+    row0 = (s.row_tiles - 1 - behind) * kRows;  // a prompt's last rows have the most work
     past = s.seq_len - s.tokens;
     stream.init(a, s, hk, position(row0 + kRows - 1), page_table, topk);
     first_tile = split * s.chunk;
     end_tile = s.chunk < stream.tiles - first_tile ? first_tile + s.chunk : stream.tiles;
-    return first_tile < end_tile;   // (a prompt's first rows have fewer splits than its last)
+    return first_tile < end_tile;   // (a pair may need fewer slots)
   }
   __device__ __forceinline__ size_t part_row(const RowsArgs& a, int in_tile) const {
     return ((size_t)unit * a.kv_heads + hk) * kRows + in_tile;
@@ -329,13 +338,18 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   Sequence s;
   if (!find_sequence<kTree, kRows, true>(s, a, cu, seq_lens, topk != nullptr, tile, lane)) return;
   const int row0 = (tile - s.before) * kRows, rows = s.tokens * a.group;
-  if (s.splits == 1 || row0 + in_tile >= rows) return;
+  if (s.slots == 1 || row0 + in_tile >= rows) return;
   Stream<kTree> stream;
   stream.init(a, s, hk, s.seq_len - s.tokens + (min(row0 + kRows, rows) - 1) / a.group, nullptr, topk);
   const int parts = (stream.tiles + s.chunk - 1) / s.chunk;
   if (parts == 1) return;  // written already
-  const size_t step = (size_t)s.row_tiles * a.kv_heads * kRows;   // rows between two splits' parts
-  const size_t part0 = (((size_t)s.units_before + (s.row_tiles - 1 - (tile - s.before))) * a.kv_heads + hk) * kRows + in_tile;
+  const size_t step = (size_t)s.places<kTree>() * a.kv_heads * kRows;   // rows between two splits' parts
+  int place = s.row_tiles - 1 - (tile - s.before), slot = 0;
+  if (s.paired<kTree>() && place > tile - s.before) {
+    slot = s.splits_of<kRows>(place, a.group);
+    place = tile - s.before;
+  }
+  const size_t part0 = (((size_t)s.units_before + slot * s.places<kTree>() + place) * a.kv_heads + hk) * kRows + in_tile;
   const int n_rows = min(kEach, rows - row0 - in_tile);
 #pragma unroll 1
   for (int r = 0; r < n_rows; ++r) {
@@ -405,7 +419,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
   int row_tiles;                // of a KV head, at most
-  int most_units, good_units, least_chunk;  // of a KV head; 0 units: no splits
+  int most_units, least_chunk;  // of a KV head; 0 units: no splits
 };
 // Work-groups of a KV head that the compute units take at once: two few_rows_kernel each, or one shared_rows_kernel.
 int at_once(int rows, const quest_cache& c) { return std::max(1, (rows == kFewRows ? 512 : 256) / kv_heads(c)); }
@@ -422,8 +436,7 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
   const int rounds = likely * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
   p.least_chunk = few ? 2 : 8;
-  p.good_units = std::max(once * rounds, p.row_tiles + 1);
-  p.most_units = tree ? p.good_units : 2 * p.good_units;
+  p.most_units = std::max(once * rounds, p.row_tiles + (tree ? 1 : c.batch + 1));
   if (4 * p.row_tiles > once * (tree ? 16 : 3) || places <= 8 * kTileTokens) p.most_units = 0;
   return p;
 }
@@ -435,12 +448,8 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
                 const char* who, hipStream_t s) {
   Plan p = plan_of(c, total_tokens, kTree, topk != nullptr ? a.k_pages : 0);
   const size_t room = workspace != nullptr ? bytes / unit_bytes(p.rows, c) : 0;
-  if (room < (size_t)units_of(p)) {  // as far as it goes
-    p.most_units = room > (size_t)p.row_tiles ? (int)room : 0;
-    p.good_units = std::min(p.good_units, p.most_units);
-  }
+  if (room < (size_t)units_of(p)) p.most_units = room > (size_t)p.row_tiles ? (int)room : 0;  // as far as it goes
   a.most_units = p.most_units;
-  a.good_units = p.good_units;
   a.least_chunk = p.least_chunk;
   a.part_acc = (float*)workspace;
   a.part_ml = a.part_acc + (size_t)units_of(p) * a.kv_heads * p.rows * kHeadDim;

@@ -50,8 +50,7 @@ struct RowsArgs {
   int64_t q_stride, new_stride;   // bytes between tokens
   int batch, max_pages, page_shift, kv_heads, group;
   int mask_words, k_pages;
-  int most_units;           // units of a KV head that there is room for; 0: no splits
-  int good_units;           // and that have something to do, about
+  int most_units;           // units of a KV head that the tokens are split into at most; 0: no splits
   int least_chunk;          // token tiles of a split, at least
   int out_is_fp16;
   uint32_t q_sign;          // exclusive-ored onto q: sign bits where the scale is negative
@@ -87,55 +86,71 @@ __device__ __forceinline__ T up_to_lane(T v, int lane) {
   return v + before;
 }
 
-// The plan of one sequence, and where its units start.  A unit is a split of a row tile; sequence b's are in the order
-// split * row_tiles + row tile.
+// The plan of one sequence, and where its units start.  A unit is a split of a row tile.  Without splits and for trees
+// sequence b's are in the order split * row_tiles + row tile, the last row tile first.  A prompt's row tiles have fewer splits
+// the earlier they are: row tile j before the last and row tile j behind the first share `slots` places, about as
+// many as they need together, in the order slot * pairs + j.  (With places for as many splits of each as the last one has, half of
+// them had nothing to do; work-groups start in order, and those behind the idle ones started a round later.)
 struct Sequence {
   int b, first, tokens, seq_len;   // first: its first packed row
-  int row_tiles, splits, chunk;
+  int row_tiles, slots, chunk;     // chunk: INT32_MAX without splits
   int before;                      // units (row tiles) of the sequences before
   int units_before;
+
+  template <int kRows>
+  __device__ __forceinline__ int splits_of(int row_tile, int group) const {   // of a prompt's row tile
+    const int rows = tokens * group, limit = seq_len - tokens + (min((row_tile + 1) * kRows, rows) - 1) / group + 1;
+    const int tiles = (limit + kTileTokens - 1) / kTileTokens;
+    return (tiles + chunk - 1) / chunk;
+  }
+  template <bool kTree>
+  __device__ __forceinline__ bool paired() const { return !kTree && chunk != INT32_MAX && row_tiles > 1; }
+  template <bool kTree>
+  __device__ __forceinline__ int places() const { return paired<kTree>() ? (row_tiles + 1) / 2 : row_tiles; }  // of a slot
 };
 // Finds the sequence of unit `want` (kByTile: of row tile `want`, counted over all sequences); false: there is none.
 template <bool kTree, int kRows, bool kByTile>
 __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, const int32_t* __restrict__ cu,
                                               const int32_t* __restrict__ seq_lens, bool list, int want, int lane) {
-  int first = 0, tokens = 0, seq_len = 0, row_tiles = 0, tiles = 0;
+  int first = 0, tokens = 0, seq_len = 0, row_tiles = 0;
+  int places = 0, tiles = 0;   // token tiles, of a row tile (pair of row tiles, at most)
   auto read = [&](int base) {
     const int i = min(base + lane, a.batch - 1);
     first = cu[i];
     tokens = cu[i + 1] - first;
     seq_len = seq_lens[i];
-    row_tiles = base + lane < a.batch ? (tokens * a.group + kRows - 1) / kRows : 0;
+    row_tiles = places = base + lane < a.batch ? (tokens * a.group + kRows - 1) / kRows : 0;
     const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : seq_len;
     tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
+    if (!kTree && row_tiles > 1) {   // the last tokens of row tiles j and row_tiles - 1 - j add up to this at most
+      const int64_t both = 2 * (int64_t)(seq_len - tokens) + (row_tiles + 1) * kRows / a.group + 2;
+      tiles = (int)((both + 2 * (kTileTokens - 1)) / kTileTokens);
+      places = (row_tiles + 1) / 2;
+    }
   };
-  // A prompt's row tile j before the last attends to j kRows / G tokens less than the last.
-  const float less = kTree ? 0.f : 0.5f * kRows / (kTileTokens * a.group);
-  float all = 0.f, work = 0.f;
-  int count = 0;
+  // Slots of a sequence that is cut every `chunk` tiles.
+  auto slots_of = [&](int chunk) {
+    return !kTree && row_tiles > 1 ? (tiles - 2) / chunk + 2 : (tiles + chunk - 1) / chunk;
+  };
   auto whole = [](auto v) { return __builtin_bit_cast(decltype(v), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1)); };
+  float work = 0.f;
+  int count = 0;
   for (int base = 0; base < a.batch; base += kWave) {
     read(base);
-    const float most = (float)row_tiles * (float)tiles;
-    all += whole(up_to_lane(most, lane));
-    if (!kTree) work += whole(up_to_lane(most - less * (float)row_tiles * (float)(row_tiles - 1), lane));
-    count += whole(up_to_lane(row_tiles, lane));
+    work += whole(up_to_lane((float)places * (float)tiles, lane));
+    count += whole(up_to_lane(!kTree && row_tiles > 1 ? 2 * places : places, lane));
   }
-  if (kTree) work = all;
-  // The chunk: with this one the units, ceil(tiles / chunk) summed over the row tiles, are at most all / chunk + count, so
-  // no more than there is room for (a hundred-thousandth covers the roundings) ..
-  const float even = fmaxf(all / (float)max(a.most_units - count, 1), work / (float)max(a.good_units - count, 1)) * 1.00001f;
-  s.chunk = a.most_units <= count || even > 1e9f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
+  // The chunk: with this one the units are at most work / chunk + count, so no more than there is room for (a
+  // hundred-thousandth covers the roundings) ..
+  const float even = work / (float)max(a.most_units - count, 1) * 1.00001f;
+  s.chunk = a.most_units <= count || even > 4e7f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
   if (s.chunk != INT32_MAX && a.batch <= kWave) {
-    // .. and that is more than needed, as a last split is half a chunk on average: the smallest with which they are
-    // still no more than wanted, within 3 %.
-    const int usual = kTree ? tiles : tiles - (int)(less * (float)max(row_tiles - 1, 0));
-    int low = max(a.least_chunk, (int)(work / (float)a.good_units)), high = s.chunk;   // high: few enough
+    // .. and that is more than needed, as a last split is half a chunk on average: the smallest with which they still
+    // are, within 3 %.
+    int low = max(a.least_chunk, (int)(work / (float)a.most_units)), high = s.chunk;   // high: few enough
     while (high - low > high >> 5) {
       const int chunk = (low + high) >> 1;
-      const int units = row_tiles * ((usual + chunk - 1) / chunk), most = row_tiles * ((tiles + chunk - 1) / chunk);
-      const bool fits = whole(up_to_lane(units, lane)) <= a.good_units && (kTree || whole(up_to_lane(most, lane)) <= a.most_units);
-      if (fits)
+      if (whole(up_to_lane(places * slots_of(chunk), lane)) <= a.most_units)
         high = chunk;
       else
         low = chunk + 1;
@@ -145,8 +160,8 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
   int units_before = 0, tiles_before = 0;
   for (int base = 0; base < a.batch; base += kWave) {
     if (a.batch > kWave) read(base);
-    const int splits = tiles / s.chunk + (tiles % s.chunk != 0);
-    const int units = row_tiles * splits;
+    const int slots = s.chunk == INT32_MAX ? 1 : slots_of(s.chunk);
+    const int units = s.chunk == INT32_MAX ? row_tiles : places * slots;
     const int u = up_to_lane(units, lane) + units_before;
     const int t = kByTile ? up_to_lane(row_tiles, lane) + tiles_before : 0;
     const unsigned long long behind = __ballot((kByTile ? t : u) > want);  // (lanes without a sequence repeat the sum)
@@ -158,7 +173,7 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
       s.tokens = of(tokens);
       s.seq_len = of(seq_len);
       s.row_tiles = of(row_tiles);
-      s.splits = of(splits);
+      s.slots = of(slots);
       s.units_before = of(u - units);
       s.before = kByTile ? of(t - row_tiles) : s.units_before;
       return true;
