@@ -1,6 +1,6 @@
 // Attention of prompts (causal) and of trees of drafted tokens over the paged cache.  See quest_rows_core.h.
 //
-// Two kernels, chosen by the rows that a sequence has on average and by the tokens that a row may attend to (plan_of):
+// Two kernels, chosen by the rows that a sequence has on average and by how much there is to do (plan_of):
 //   many rows (shared_rows_kernel)  eight waves of 32 rows share the tiles of tokens, fetched once for 256 rows.  Bound by
 //            the matrix cores and by power: 32k tokens of 32 query / 8 KV heads 8.2 to 8.5 ms, 1040 to 1070 TFLOP/s (a large
 //            library product 1310), at 1.9 GHz; with zeros for data the clock stays at 2.4 GHz and it is 7.0.
@@ -407,15 +407,19 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 }
 
 // How a call is cut up, from what the host knows.
-//   Kernel: the small one up to 64 rows a sequence on average (64 rows at 65k tokens of 8 heads: 56 us and 63; 128 rows:
-//   89 and 67), and where no row can attend to more than 1536 tokens (1500 tokens of 32 / 8 heads: 51 us and 66; 2000: 80
-//   and 57).
 //   Splits: so many that the work-groups fill the compute units once; an even share then ends at the same time
 //   everywhere (26 drafts at 32k tokens: 105 us, with twice as many 110, four times 122).  Where there are row tiles for
 //   more than half of that (many rows of trees: a quarter) their unequal ends weigh more than a start does, and the share
 //   is cut into rounds: two, and four for many rows of trees (sixteen ragged trees of 1 to 2 tiles: 1830 us in one
 //   round, 1245 in two, 1000 in four).  None where the row tiles alone fill the compute units (prompts: to three
-//   quarters; 2000 tokens of 32 / 8 heads: 57 us, 77 with), or rows have at most eight tiles of tokens.
+//   quarters; 2000 tokens of 32 / 8 heads: 58 us, 90 with), or rows have at most eight tiles of tokens.
+//   Kernel: the small one does a quarter of the large one's work in the same time where there is enough of it, but is a
+//   third of it to start, split and join.  It has calls of up to 64 rows a sequence (64 rows at 65k tokens of 8 heads:
+//   56 us and 63 with the large one; 128 rows: 89 and 67), and those of little work, counted in 256 rows by 64 tokens: 600,
+//   if they are less than 64 row tiles of the large one (fifteen prompts of 500 tokens of 64 / 8 heads: 182 us and 82,
+//   of 100 of 8: 9 and 10), or 2400 where the large one would join splits of prompts (1000 tokens of 32 / 8 heads: 31 us and
+//   38, four sequences of 1500 tokens of 8 heads 39 and 54, of 500 tokens behind 1000 of 32 / 8: 65 and 47).  Over 378
+//   calls from 100 to 60000 tokens by 1 to 64 heads it takes 1 % longer than the better of both, at most 1.6 times.
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
   int row_tiles;                // of a KV head, at most
@@ -425,19 +429,23 @@ struct Plan {
 int at_once(int rows, const quest_cache& c) { return std::max(1, (rows == kFewRows ? 512 : 256) / kv_heads(c)); }
 // k_pages: listed pages (0: all).
 Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
-  Plan p;
   const int64_t rows = (int64_t)total_tokens * group_size(c), mean = (rows + c.batch - 1) / c.batch;
+  const int64_t new_tokens = total_tokens / c.batch;
   const int64_t pages = k_pages > 0 ? std::min(k_pages, c.max_pages_per_seq) : c.max_pages_per_seq;
-  const int64_t places = pages * c.page_size + (tree ? total_tokens / c.batch : 0);   // that a row may attend to
-  p.rows = mean <= 64 || places <= 1536 ? kFewRows : kSharedRows;
-  const bool few = p.rows == kFewRows;
+  const int64_t places = pages * c.page_size + (tree ? new_tokens : 0);   // that a row may attend to
+  auto row_tiles = [&](int of) { return (int)(rows / of + c.batch); };
+  auto splits = [&](int of) { return 4 * row_tiles(of) <= at_once(of, c) * (tree ? 16 : 3) && places > 8 * kTileTokens; };
+  const double wide = (double)rows * kv_heads(c) / kSharedRows;
+  const double work = wide * (tree ? places : std::max(places - new_tokens / 2, places / 2)) / kTileTokens;
+  Plan p;
+  const bool few = mean <= 64 || (!tree && splits(kSharedRows) ? work < 2400 : work < 600 && wide < 64);
+  p.rows = few ? kFewRows : kSharedRows;
+  p.row_tiles = row_tiles(p.rows);
   const int once = at_once(p.rows, c);
-  p.row_tiles = (int)(rows / p.rows + c.batch);
   const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
   const int rounds = likely * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
   p.least_chunk = few ? 2 : 8;
-  p.most_units = std::max(once * rounds, p.row_tiles + (tree ? 1 : c.batch + 1));
-  if (4 * p.row_tiles > once * (tree ? 16 : 3) || places <= 8 * kTileTokens) p.most_units = 0;
+  p.most_units = splits(p.rows) ? std::max(once * rounds, p.row_tiles + (tree ? 1 : c.batch + 1)) : 0;
   return p;
 }
 int units_of(const Plan& p) { return std::max(p.row_tiles, p.most_units); }

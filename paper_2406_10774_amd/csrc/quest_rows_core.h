@@ -113,7 +113,7 @@ template <bool kTree, int kRows, bool kByTile>
 __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, const int32_t* __restrict__ cu,
                                               const int32_t* __restrict__ seq_lens, bool list, int want, int lane) {
   int first = 0, tokens = 0, seq_len = 0, row_tiles = 0;
-  int places = 0, tiles = 0;   // token tiles, of a row tile (pair of row tiles, at most)
+  int places = 0, tiles = 0, last = 0;   // token tiles, of a pair of row tiles at most and of the last one
   auto read = [&](int base) {
     const int i = min(base + lane, a.batch - 1);
     first = cu[i];
@@ -121,8 +121,8 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
     seq_len = seq_lens[i];
     row_tiles = places = base + lane < a.batch ? (tokens * a.group + kRows - 1) / kRows : 0;
     const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : seq_len;
-    tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
-    if (!kTree && row_tiles > 1) {   // the last tokens of row tiles j and row_tiles - 1 - j add up to this at most
+    last = tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
+    if (!kTree && row_tiles > 1 && a.most_units > 0) {   // the last tokens of row tiles j and row_tiles - 1 - j add up to this at most
       const int64_t both = 2 * (int64_t)(seq_len - tokens) + (row_tiles + 1) * kRows / a.group + 2;
       tiles = (int)((both + 2 * (kTileTokens - 1)) / kTileTokens);
       places = (row_tiles + 1) / 2;
@@ -130,36 +130,40 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
   };
   // Slots of a sequence that is cut every `chunk` tiles.
   auto slots_of = [&](int chunk) {
-    return !kTree && row_tiles > 1 ? (tiles - 2) / chunk + 2 : (tiles + chunk - 1) / chunk;
+    const int most = (last + chunk - 1) / chunk;
+    return !kTree && row_tiles > 1 ? min((tiles - 2) / chunk + 2, 2 * most) : most;
   };
   auto whole = [](auto v) { return __builtin_bit_cast(decltype(v), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1)); };
-  float work = 0.f;
-  int count = 0;
-  for (int base = 0; base < a.batch; base += kWave) {
-    read(base);
-    work += whole(up_to_lane((float)places * (float)tiles, lane));
-    count += whole(up_to_lane(!kTree && row_tiles > 1 ? 2 * places : places, lane));
-  }
-  // The chunk: with this one the units are at most work / chunk + count, so no more than there is room for (a
-  // hundred-thousandth covers the roundings) ..
-  const float even = work / (float)max(a.most_units - count, 1) * 1.00001f;
-  s.chunk = a.most_units <= count || even > 4e7f ? INT32_MAX : max(a.least_chunk, (int)even + 1);
-  if (s.chunk != INT32_MAX && a.batch <= kWave) {
-    // .. and that is more than needed, as a last split is half a chunk on average: the smallest with which they still
-    // are, within 3 %.
-    int low = max(a.least_chunk, (int)(work / (float)a.most_units)), high = s.chunk;   // high: few enough
-    while (high - low > high >> 5) {
-      const int chunk = (low + high) >> 1;
-      if (whole(up_to_lane(places * slots_of(chunk), lane)) <= a.most_units)
-        high = chunk;
-      else
-        low = chunk + 1;
+  s.chunk = INT32_MAX;
+  if (a.most_units > 0) {
+    float work = 0.f;
+    int count = 0;
+    for (int base = 0; base < a.batch; base += kWave) {
+      read(base);
+      work += whole(up_to_lane((float)places * (float)tiles, lane));
+      count += whole(up_to_lane(!kTree && row_tiles > 1 ? 2 * places : places, lane));
     }
-    s.chunk = high;
+    // The chunk: with this one the units are at most work / chunk + count, so no more than there is room for (a
+    // hundred-thousandth covers the roundings) ..
+    const float even = work / (float)max(a.most_units - count, 1) * 1.00001f;
+    if (a.most_units > count && even < 4e7f) s.chunk = max(a.least_chunk, (int)even + 1);
+    if (s.chunk != INT32_MAX && a.batch <= kWave) {
+      // .. and that is more than needed, as a last split is half a chunk on average: the smallest with which they still
+      // are, within 3 %.
+      int low = max(a.least_chunk, (int)(work / (float)a.most_units)), high = s.chunk;   // high: few enough
+      while (high - low > high >> 5) {
+        const int chunk = (low + high) >> 1;
+        if (whole(up_to_lane(places * slots_of(chunk), lane)) <= a.most_units)
+          high = chunk;
+        else
+          low = chunk + 1;
+      }
+      s.chunk = high;
+    }
   }
   int units_before = 0, tiles_before = 0;
   for (int base = 0; base < a.batch; base += kWave) {
-    if (a.batch > kWave) read(base);
+    if (a.batch > kWave || a.most_units == 0) read(base);
     const int slots = s.chunk == INT32_MAX ? 1 : slots_of(s.chunk);
     const int units = s.chunk == INT32_MAX ? row_tiles : places * slots;
     const int u = up_to_lane(units, lane) + units_before;

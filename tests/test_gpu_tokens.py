@@ -11,7 +11,7 @@ from packed_util import D, Packed, Trees, check_prompt, check_tree
 
 pytestmark = pytest.mark.gpu
 SCALE = 1 / math.sqrt(D)
-ROOMS = [0, 8192]      # page-table rows that end with the sequence, and long ones: other kernels and splits
+ROOMS = [0, 1 << 18]     # page-table rows that end with the sequence, and long ones: other kernels and splits
 
 
 def run_prompt(p, half, scale=SCALE, workspace="full"):
@@ -71,6 +71,14 @@ def test_prompt_scales(scale):
         p = Packed([190], [190], heads=2, kv_heads=2, seed=5, spread=2.0, room=room)
         for half in (True, False):
             check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("kv_heads", [40, 8])
+def test_prompts_that_fill_the_card(kv_heads, half):
+    """Enough rows for the large kernel, in one piece."""
+    p = Packed([700, 950, 40], [700, 333, 40], heads=40, kv_heads=kv_heads, seed=kv_heads)
+    check_prompt(p, *run_prompt(p, half), half, SCALE)
 
 
 @pytest.mark.parametrize("most,heads", [(40, 4), (60, 12)])
