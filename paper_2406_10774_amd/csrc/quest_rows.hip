@@ -406,20 +406,26 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   }
 }
 
-// How a call is cut up, from what the host knows.
-//   Splits: so many that the work-groups fill the compute units once; an even share then ends at the same time
+// How a call is cut up, from what the host knows.  The figures are of 820 calls, from 6 to 12000 rows a sequence over contexts
+// up to 60000 tokens by 1 to 64 heads, each with both kernels, with and without splits: the rules take 2.5 % longer than the
+// best of the four on average.
+//   Splits: where the row tiles leave compute units idle for long enough.  Idle is the share of the units without
+//   a row tile times the row's tiles of tokens; a join costs as much as 8 to 12 of them (60 drafts of 8 heads at 600
+//   tokens 12 us with splits and 15 without), 20 to 25 where more than a third of the units have a row tile (sixteen
+//   sequences of 400 rows behind 2000 tokens: 37 us without, 43 with), and 30 to 50 where the splits do not fit the units
+//   at once any more (400 tokens behind 600 of 32 / 8 heads 22 us without, 46 with; 24 nodes in fifteen sequences of 20000
+//   tokens 340 without, 254 with).  None for rows of at most eight tiles.
+//   So many that the work-groups fill the compute units once; an even share then ends at the same time
 //   everywhere (26 drafts at 32k tokens: 105 us, with twice as many 110, four times 122).  Where there are row tiles for
 //   more than half of that (many rows of trees: a quarter) their unequal ends weigh more than a start does, and the share
 //   is cut into rounds: two, and four for many rows of trees (sixteen ragged trees of 1 to 2 tiles: 1830 us in one
-//   round, 1245 in two, 1000 in four).  None where the row tiles alone fill the compute units (prompts: to three
-//   quarters; 2000 tokens of 32 / 8 heads: 58 us, 90 with), or rows have at most eight tiles of tokens.
+//   round, 1245 in two, 1000 in four).
 //   Kernel: the small one does a quarter of the large one's work in the same time where there is enough of it, but is a
-//   third of it to start, split and join.  It has calls of up to 64 rows a sequence (64 rows at 65k tokens of 8 heads:
-//   56 us and 63 with the large one; 128 rows: 89 and 67), and those of little work, counted in 256 rows by 64 tokens: 600,
-//   if they are less than 64 row tiles of the large one (fifteen prompts of 500 tokens of 64 / 8 heads: 182 us and 82,
-//   of 100 of 8: 9 and 10), or 2400 where the large one would join splits of prompts (1000 tokens of 32 / 8 heads: 31 us and
-//   38, four sequences of 1500 tokens of 8 heads 39 and 54, of 500 tokens behind 1000 of 32 / 8: 65 and 47).  Over 378
-//   calls from 100 to 60000 tokens by 1 to 64 heads it takes 1 % longer than the better of both, at most 1.6 times.
+//   third of it to start and to join.  It has calls of up to 64 rows a sequence (64 rows at 65k tokens of 8 heads:
+//   56 us and 63 with the large one; 128 rows: 89 and 67), and those of less than 80 row tiles of the large one and
+//   little work, counted in 256 rows by 64 tokens: 3000 (400 tokens behind 600 of 32 / 8 heads: 22 us and 33; fifteen
+//   prompts of 500 tokens of 64 / 8 heads: 182 and 82), or 800 where the large one would split (60 tokens in ten
+//   sequences of 6000 of 64 / 8 heads 160 and 153, one of 150 behind 3000 59 and 40).
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
   int row_tiles;                // of a KV head, at most
@@ -433,17 +439,20 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   const int64_t new_tokens = total_tokens / c.batch;
   const int64_t pages = k_pages > 0 ? std::min(k_pages, c.max_pages_per_seq) : c.max_pages_per_seq;
   const int64_t places = pages * c.page_size + (tree ? new_tokens : 0);   // that a row may attend to
-  auto row_tiles = [&](int of) { return (int)(rows / of + c.batch); };
-  auto splits = [&](int of) { return 4 * row_tiles(of) <= at_once(of, c) * (tree ? 16 : 3) && places > 8 * kTileTokens; };
+  auto likely = [&](int of) { return std::max<int64_t>(c.batch, rows / of); };   // row tiles
+  auto splits = [&](int of) {
+    const double fill = (double)likely(of) / at_once(of, c), idle = (double)places / kTileTokens * (1 - fill);
+    const bool few = of == kFewRows;
+    return places > 8 * kTileTokens && idle > (fill < 0.15 ? 8 : fill < 0.3 ? 12 : fill < 0.5 ? (few ? 25 : 20) : few ? 50 : 30);
+  };
   const double wide = (double)rows * kv_heads(c) / kSharedRows;
   const double work = wide * (tree ? places : std::max(places - new_tokens / 2, places / 2)) / kTileTokens;
   Plan p;
-  const bool few = mean <= 64 || (!tree && splits(kSharedRows) ? work < 2400 : work < 600 && wide < 64);
+  const bool few = mean <= 64 || (wide < 80 && work < (splits(kSharedRows) ? 800 : 3000));
   p.rows = few ? kFewRows : kSharedRows;
-  p.row_tiles = row_tiles(p.rows);
+  p.row_tiles = (int)(rows / p.rows + c.batch);
   const int once = at_once(p.rows, c);
-  const int64_t likely = std::max<int64_t>(c.batch, rows / p.rows);  // row tiles
-  const int rounds = likely * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
+  const int rounds = likely(p.rows) * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
   p.least_chunk = few ? 2 : 8;
   p.most_units = splits(p.rows) ? std::max(once * rounds, p.row_tiles + (tree ? 1 : c.batch + 1)) : 0;
   return p;
@@ -510,14 +519,10 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
 // Enough for calls with any number of tokens up to this one: four rounds of units, and one more, of the largest
 // row tiles that they may have.
 size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) {
-  size_t most = 0;
-  for (const bool tree : {false, true}) {
-    const Plan p = plan_of(c, total_tokens, tree, 0);
-    const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + (tree ? total_tokens : 0);
-    if (places > 8 * kTileTokens && total_tokens > 0)
-      most = std::max(most, (4 * (size_t)at_once(p.rows, c) + 2) * unit_bytes(p.rows, c));
-  }
-  return most;
+  const int64_t rows = (int64_t)total_tokens * group_size(c);
+  const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + total_tokens;
+  const int of = rows <= 64 * (int64_t)c.batch ? kFewRows : kSharedRows;
+  return places > 8 * kTileTokens && total_tokens > 0 ? (4 * (size_t)at_once(of, c) + 2) * unit_bytes(of, c) : 0;
 }
 
 bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {

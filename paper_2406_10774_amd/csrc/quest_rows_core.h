@@ -59,6 +59,7 @@ struct RowsArgs {
 };
 
 constexpr int kTileTokens = 64;
+constexpr int kMostSplits = 64;   // of a sequence, about: joining more takes longer than they save (60k tokens of a head: 43 us, 30 with)
 
 #if defined(__HIPCC__)
 
@@ -136,21 +137,23 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
   auto whole = [](auto v) { return __builtin_bit_cast(decltype(v), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1)); };
   s.chunk = INT32_MAX;
   if (a.most_units > 0) {
-    float work = 0.f;
+    float work = 0.f, context = 0.f;
     int count = 0;
     for (int base = 0; base < a.batch; base += kWave) {
       read(base);
       work += whole(up_to_lane((float)places * (float)tiles, lane));
       count += whole(up_to_lane(!kTree && row_tiles > 1 ? 2 * places : places, lane));
+      context += whole(up_to_lane(row_tiles > 0 ? (float)last : 0.f, lane));
     }
+    const int least = max(a.least_chunk, (int)(context / (float)(kMostSplits * a.batch)));
     // The chunk: with this one the units are at most work / chunk + count, so no more than there is room for (a
     // hundred-thousandth covers the roundings) ..
     const float even = work / (float)max(a.most_units - count, 1) * 1.00001f;
-    if (a.most_units > count && even < 4e7f) s.chunk = max(a.least_chunk, (int)even + 1);
+    if (a.most_units > count && even < 4e7f) s.chunk = max(least, (int)even + 1);
     if (s.chunk != INT32_MAX && a.batch <= kWave) {
       // .. and that is more than needed, as a last split is half a chunk on average: the smallest with which they still
       // are, within 3 %.
-      int low = max(a.least_chunk, (int)(work / (float)a.most_units)), high = s.chunk;   // high: few enough
+      int low = max(least, (int)(work / (float)a.most_units)), high = s.chunk;   // high: few enough
       while (high - low > high >> 5) {
         const int chunk = (low + high) >> 1;
         if (whole(up_to_lane(places * slots_of(chunk), lane)) <= a.most_units)
