@@ -48,12 +48,10 @@ struct Part {
     const int index = unit - s.before, slot = index / s.places<kTree>();
     int split = slot, behind = index - slot * s.places<kTree>();   // the row tile, counted from the last one
     if (s.paired<kTree>()) {
-      const int splits = s.splits_of<kRows>(s.row_tiles - 1 - behind, a.group);
-      if (slot >= splits) {
-        split = slot - splits;
-        if (2 * behind + 1 == s.row_tiles) return false;   // the one in the middle has its place alone
-        behind = s.row_tiles - 1 - behind;
-      }
+      // The one in the middle has its place alone.
+      const int fewer = 2 * behind + 1 == s.row_tiles ? 0 : s.splits_of<kRows>(behind, a.group);
+      split = slot < 2 * fewer ? slot >> 1 : slot - fewer;
+      if (slot < 2 * fewer && (slot & 1)) behind = s.row_tiles - 1 - behind;
     }
     group = a.group;
     rows = s.tokens * group;
@@ -344,37 +342,45 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   const int parts = (stream.tiles + s.chunk - 1) / s.chunk;
   if (parts == 1) return;  // written already
   const size_t step = (size_t)s.places<kTree>() * a.kv_heads * kRows;   // rows between two splits' parts
-  int place = s.row_tiles - 1 - (tile - s.before), slot = 0;
-  if (s.paired<kTree>() && place > tile - s.before) {
-    slot = s.splits_of<kRows>(place, a.group);
-    place = tile - s.before;
+  // The slot of split i: 2 i + odd for the first `turns`, then i + turns.
+  int place = s.row_tiles - 1 - (tile - s.before), turns = 0, odd = 0;
+  if (s.paired<kTree>()) {
+    if (place > tile - s.before) {
+      place = tile - s.before;
+      turns = parts;
+      odd = 1;
+    } else if (place < tile - s.before) {
+      turns = s.splits_of<kRows>(place, a.group);
+    }
   }
-  const size_t part0 = (((size_t)s.units_before + slot * s.places<kTree>() + place) * a.kv_heads + hk) * kRows + in_tile;
+  auto slots_on = [&](int i) { return i < turns ? 2 * i : i + turns; };   // from split 0's to split i's
+  const size_t part0 = (((size_t)s.units_before + odd * s.places<kTree>() + place) * a.kv_heads + hk) * kRows + in_tile;
   const int n_rows = min(kEach, rows - row0 - in_tile);
 #pragma unroll 1
   for (int r = 0; r < n_rows; ++r) {
     const float2* from = reinterpret_cast<const float2*>(a.part_acc + (part0 + r) * kHeadDim) + lane;
+    int next = 0;
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + part0 + r;
     float2 v[8];
-    auto ask = [&](int n) {   // the next n parts' outputs
+    auto ask = [&] {   // the next eight parts' outputs
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 8; ++j, ++next) {
         v[j] = *from;
-        if (j < n - 1) from += step * (kHeadDim / 2);
+        if (next < parts - 1) from += next < turns ? step * kHeadDim : step * (kHeadDim / 2);
       }
     };
-    ask(parts);
+    ask();
     float top = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll 1
     for (int base = 0; base < parts; base += kWave) {
-      const float2 x = ml[min(base + lane, parts - 1) * step];
+      const float2 x = ml[slots_on(min(base + lane, parts - 1)) * step];
       if (x.y > 0.f) top = fmaxf(top, x.x);
     }
 #pragma unroll
     for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
 #pragma unroll 1
     for (int base = 0; base < parts; base += kWave) {
-      const float2 x = ml[min(base + lane, parts - 1) * step];
+      const float2 x = ml[slots_on(min(base + lane, parts - 1)) * step];
       const float weight = base + lane < parts && x.y > 0.f ? __builtin_amdgcn_exp2f((x.x - top) * a.scale) : 0.f;
       sum += weight * x.y;
       const int n = min(parts - base, kWave);
@@ -383,7 +389,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
         float2 now[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) now[j] = v[j];
-        if (base + i + 8 < parts) ask(parts - base - i - 8);
+        if (next < parts) ask();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float w = i + j < n ? from_lane(weight, i + j) : 0.f;

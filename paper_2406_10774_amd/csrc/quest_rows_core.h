@@ -90,7 +90,8 @@ __device__ __forceinline__ T up_to_lane(T v, int lane) {
 // The plan of one sequence, and where its units start.  A unit is a split of a row tile.  Without splits and for trees
 // sequence b's are in the order split * row_tiles + row tile, the last row tile first.  A prompt's row tiles have fewer splits
 // the earlier they are: row tile j before the last and row tile j behind the first share `slots` places, about as
-// many as they need together, in the order slot * pairs + j.  (With places for as many splits of each as the last one has, half of
+// many as they need together, in the order slot * pairs + j: by turns while both have splits, so that those of the same
+// tokens run at the same time.  (With places for as many splits of each as the last one has, half of
 // them had nothing to do; work-groups start in order, and those behind the idle ones started a round later.)
 struct Sequence {
   int b, first, tokens, seq_len;   // first: its first packed row
