@@ -413,7 +413,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 }
 
 // How a call is cut up, from what the host knows.  The figures are of 820 calls, from 6 to 12000 rows a sequence over contexts
-// up to 60000 tokens by 1 to 64 heads, each with both kernels, with and without splits: the rules take 2.5 % longer than the
+// up to 60000 tokens by 1 to 64 heads, each with both kernels, with and without splits: the rules take 1 % longer than the
 // best of the four on average.
 //   Splits: where the row tiles leave compute units idle for long enough.  Idle is the share of the units without
 //   a row tile times the row's tiles of tokens; a join costs as much as 8 to 12 of them (60 drafts of 8 heads at 600
