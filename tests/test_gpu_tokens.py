@@ -73,6 +73,23 @@ def test_prompt_scales(scale):
             check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_prompts_in_splits(seed):
+    """Ragged parts of prompts: odd and even numbers of row tiles, of both kernels, most of them in several splits."""
+    rng = np.random.default_rng(seed)
+    B, S = int(rng.integers(1, 5)), int(rng.choice([8, 16, 32, 64]))
+    kv_heads = int(rng.integers(1, 4))
+    heads = kv_heads * int(rng.choice([1, 2, 3, 4, 7]))
+    new = [int(rng.integers(1, 700)) for _ in range(B)]
+    lens = [n + int(rng.choice([0, rng.integers(0, 300), rng.integers(0, 5000)])) for n in new]
+    p = Packed(lens, new, heads=heads, kv_heads=kv_heads, S=S, seed=seed, room=ROOMS[seed % 2])
+    half = seed % 3 > 0
+    whole = run_prompt(p, half)
+    check_prompt(p, *whole, half, SCALE, seed)
+    again = run_prompt(p, half)
+    assert torch.equal(whole[0], again[0]) and torch.equal(whole[1], again[1])
+
+
 @pytest.mark.parametrize("half", [True, False])
 @pytest.mark.parametrize("kv_heads", [40, 8])
 def test_prompts_that_fill_the_card(kv_heads, half):
