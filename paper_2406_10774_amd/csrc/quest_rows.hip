@@ -356,6 +356,8 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   auto slots_on = [&](int i) { return i < turns ? 2 * i : i + turns; };   // from split 0's to split i's
   const size_t part0 = (((size_t)s.units_before + odd * s.places<kTree>() + place) * a.kv_heads + hk) * kRows + in_tile;
   const int n_rows = min(kEach, rows - row0 - in_tile);
+  const float2* ml0 = reinterpret_cast<const float2*>(a.part_ml) + part0 + slots_on(min(lane, parts - 1)) * step;
+  float2 first = *ml0;   // of a row's first 64 splits
 #pragma unroll 1
   for (int r = 0; r < n_rows; ++r) {
     const float2* from = reinterpret_cast<const float2*>(a.part_acc + (part0 + r) * kHeadDim) + lane;
@@ -370,9 +372,11 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
       }
     };
     ask();
-    float top = kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
+    const float2 these = first;
+    if (r + 1 < n_rows) first = ml0[r + 1];
+    float top = these.y > 0.f ? these.x : kNegBig, sum = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll 1
-    for (int base = 0; base < parts; base += kWave) {
+    for (int base = kWave; base < parts; base += kWave) {
       const float2 x = ml[slots_on(min(base + lane, parts - 1)) * step];
       if (x.y > 0.f) top = fmaxf(top, x.x);
     }
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
     for (int i = 1; i < kWave; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
 #pragma unroll 1
     for (int base = 0; base < parts; base += kWave) {
-      const float2 x = ml[slots_on(min(base + lane, parts - 1)) * step];
+      const float2 x = base == 0 ? these : ml[slots_on(min(base + lane, parts - 1)) * step];
       const float weight = base + lane < parts && x.y > 0.f ? __builtin_amdgcn_exp2f((x.x - top) * a.scale) : 0.f;
       sum += weight * x.y;
       const int n = min(parts - base, kWave);
