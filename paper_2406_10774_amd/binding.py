@@ -276,8 +276,9 @@ def _outputs(cache, out, lse, workspace, rows):
     _plain(cache, out, _half if out.dtype is _half else _types[0], rows * cache.heads * cache.head_dim, "out")
     if lse is not None:
         _plain(cache, lse, _types[0], rows * cache.heads, "lse")
-    if workspace is not None:
-        _plain(cache, workspace, workspace.dtype, 0, "workspace")
+    if workspace is not None and (workspace.get_device() != cache.device or not workspace.is_contiguous()):
+        raise QuestError(-2, f"workspace of strides {workspace.stride()} on {workspace.device}: has to be contiguous, on the "
+                             "cache's device")
 
 
 def _stream_of(cache, stream):
@@ -285,7 +286,7 @@ def _stream_of(cache, stream):
     device = cache.device
     if device >= 0 and _current_device() != device:
         raise QuestError(-2, f"the cache lies on device {device}, which is not the current one")
-    return _stream(stream)
+    return _stream(stream) if device < 0 or stream is not None else _raw_stream(device)
 
 
 def quest_append_tokens(cache: Cache, k_new, v_new, cu_tokens, rows=None, stream=None):

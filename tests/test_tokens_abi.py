@@ -193,6 +193,8 @@ def test_binding_refuses_other_devices_and_head_sizes(monkeypatch):
     one = binding.Cache(c.pool[:, :1], c.pool[:, :1], c.meta, c.cache.page_table, c.cache.seq_lens)
     with pytest.raises(binding.QuestError):   # 64 channels, 128 apart
         binding.quest_prompt_attention(one, c.q[:, :1, :64], c.cu, 1.0, torch.zeros(6, 1, 64), stream=0)
+    with pytest.raises(binding.QuestError, match="workspace"):
+        c.prompt(workspace=torch.zeros(64)[::2])
     c.cache.device = 0
     for call in (c.append, c.prompt, c.tree):
         with pytest.raises(binding.QuestError, match="on the cache's device"):
