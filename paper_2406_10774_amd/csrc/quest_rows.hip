@@ -207,8 +207,9 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
 
 // Few rows: tiles of 32 tokens, each wave its own; 16 KiB on the way to each wave's registers, 128 KiB for a compute unit.
 // With 64 rows a wave (one work-group on a compute unit instead of two) 64 rows took as long as two tiles of 32: 61 us and 58
-// at 65k tokens of 8 heads.
-template <bool kTree, bool kExact>
+// at 65k tokens of 8 heads.  Weights keep 22 bits whatever the output's type, so that an fp16 output is the fp32 one rounded, as in
+// the decode calls: a prompt of one token is as exact as a decode step.
+template <bool kTree, bool kHalfOut>
 __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   }
   const int first_position = w.position(w.row0);
 
-  RowState<kExact, false> st;
+  RowState<true, false> st;
   Walk<kTree, kTokens> walk;
   walk.init(w.stream, w.first_tile * kTileTokens + wave * kTokens, kWaves * kTokens);
   const int steps = ((w.end_tile - w.first_tile) * (kTileTokens / kTokens) - wave + kWaves - 1) / kWaves;
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   float* join = reinterpret_cast<float*>(lds);
   const float total = st.total();
   float* mine = join + (wave * kFewRows + (lane & 31)) * kStride;
-  st.each4(RowState<kExact, false>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
+  st.each4(RowState<true, false>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
   if (lane < kFewRows) {
     ml[0][wave][lane] = total > 0.f ? st.base : kNegBig;
     ml[1][wave][lane] = total;
@@ -312,10 +313,10 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   for (int j = 0; j < 4; ++j) {
     const float4 v = make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor);
     const size_t at = out_row * kHeadDim + d0 + 4 * j;
-    if constexpr (kExact)
-      *reinterpret_cast<float4*>((float*)a.out + at) = v;
-    else
+    if constexpr (kHalfOut)
       store_halves((_Float16*)a.out + at, v);
+    else
+      *reinterpret_cast<float4*>((float*)a.out + at) = v;
   }
   if (a.lse != nullptr && d0 == 0) a.lse[out_row] = st.lse(top, sum, a.scale);
 }
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
       *reinterpret_cast<half2_t*>((_Float16*)a.out + at) = half2_t{half_of(o0 * factor), half_of(o1 * factor)};
     else
       *reinterpret_cast<float2*>((float*)a.out + at) = make_float2(o0 * factor, o1 * factor);
-    if (a.lse != nullptr && lane == 0) a.lse[out_row] = RowState<false, false>::lse(top, sum, a.scale);
+    if (a.lse != nullptr && lane == 0) a.lse[out_row] = RowState<true, false>::lse(top, sum, a.scale);
   }
 }
 
@@ -476,13 +477,16 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   Plan p = plan_of(c, total_tokens, kTree, topk != nullptr ? a.k_pages : 0);
   const size_t room = workspace != nullptr ? bytes / unit_bytes(p.rows, c) : 0;
   if (room < (size_t)units_of(p)) p.most_units = room > (size_t)p.row_tiles ? (int)room : 0;  // as far as it goes
+  const bool exact = kExact || p.rows == kFewRows;
+  a.below = (exact ? RowState<true, false>::kBelow : RowState<false, true>::kBelow) / a.scale;
+  a.limit = (exact ? RowState<true, false>::kMove : RowState<false, true>::kMove) / a.scale;
   a.most_units = p.most_units;
   a.least_chunk = p.least_chunk;
   a.part_acc = (float*)workspace;
   a.part_ml = a.part_acc + (size_t)units_of(p) * a.kv_heads * p.rows * kHeadDim;
   const dim3 grid((unsigned)(units_of(p) * a.kv_heads)), block((p.rows == kSharedRows ? kSharedWaves : kWaves) * kWave);
   if (p.rows == kFewRows)
-    hipLaunchKernelGGL((few_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+    hipLaunchKernelGGL((few_rows_kernel<kTree, !kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   else
     hipLaunchKernelGGL((shared_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   const int r = check_launch(who);
@@ -519,8 +523,6 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
   a.out_is_fp16 = out_is_fp16;
   a.q_sign = sm_scale < 0.f ? 0x80008000u : 0u;
   a.scale = std::max(std::abs(sm_scale) * kLog2e, 1e-30f);  // scale 0: all weights alike
-  a.below = (out_is_fp16 ? RowState<false, false>::kBelow : RowState<true, false>::kBelow) / a.scale;
-  a.limit = (out_is_fp16 ? RowState<false, false>::kMove : RowState<true, false>::kMove) / a.scale;
   return a;
 }
 

@@ -1,0 +1,74 @@
+"""How exact attention of prompts and of drafted tokens is: fp16 outputs of few rows are the fp32 result, rounded once."""
+import math
+
+import pytest
+import torch
+
+from paper_2406_10774_amd import binding as Q
+from packed_util import D, Packed, Trees, attention64
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / math.sqrt(D)
+
+
+def run(p, t, half, workspace=True):
+    out, lse = p.results(half)
+    ws = p.workspace() if workspace else None
+    if t is None:
+        Q.quest_prompt_attention(p.cache, p.q, p.cu, SCALE, out, lse=lse, workspace=ws)
+    else:
+        Q.quest_tree_attention(p.cache, p.q, p.k_new, p.v_new, p.cu, t.mask, SCALE, out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def rounded_once(got, want, what):
+    """The fp32 limit (eight times the square root of the number of 2^-24 roundings of 128-channel sums, exp2 and n tokens, of
+    the sum of the weighted values' sizes), and half a step of fp16 at the result with that error: 2^-11 of it, 2^-25 at
+    least."""
+    o, _, weight, size, n = want
+    limit = 8 * (math.sqrt(D) * 2.0 ** -24 * size + 2.0 ** -21 + n.double().sqrt() * 2.0 ** -24)
+    bound = limit[:, None] * weight * (1 + 2.0 ** -11) + 2.0 ** -11 * o.abs() + 2.0 ** -25
+    off = (got.double() - o).abs()
+    assert bool((off <= bound).all()), (what, float((off / bound).max()), float(off.max()))
+
+
+@pytest.mark.parametrize("room", [0, 1 << 16])
+@pytest.mark.parametrize("new,past", [([1, 1], [900, 5000]), ([1], [0]), ([13], [0]), ([16, 3], [40, 2500]), ([5], [9000])])
+def test_few_rows(new, past, room):
+    """At most 64 rows (new tokens times query heads of a KV head) a sequence on average."""
+    p = Packed([n + m for n, m in zip(new, past)], new, heads=8, kv_heads=2, seed=sum(new), room=room)
+    trees = Packed(past, new, heads=8, kv_heads=2, seed=sum(new), room=room)
+    t = Trees(trees)
+    for ws in (True, False):
+        out, lse = run(p, None, True, ws)
+        single = run(p, None, False, ws)
+        assert torch.equal(lse, single[1])
+        drafts, _ = run(trees, t, True, ws)
+        for b in range(p.B):
+            at = p.rows(b)
+            position = torch.arange(p.lens[b] - p.new[b], p.lens[b], device=p.dev)
+            sees = torch.arange(p.lens[b], device=p.dev) <= position[:, None]
+            seen = torch.cat([torch.ones(new[b], past[b], dtype=torch.bool, device=p.dev), torch.from_numpy(t.sees[b]).to(p.dev)], 1)
+            for h in range(p.H):
+                k, v = p.cached(b, h // p.G)
+                rounded_once(out[at, h], attention64(p.q[at, h].double(), k, v, sees, SCALE), ("prompt", b, h, ws))
+                k, v = trees.cached(b, h // p.G)
+                k, v = torch.cat([k, trees.k_new[at, h // p.G].double()]), torch.cat([v, trees.v_new[at, h // p.G].double()])
+                rounded_once(drafts[at, h], attention64(trees.q[at, h].double(), k, v, seen, SCALE), ("tree", b, h, ws))
+
+
+def test_single_tokens_as_decode_steps():
+    """One token a sequence, fp16 outputs: as exact as the decode call's over all pages."""
+    p = Packed([700, 33, 4000], [1, 1, 1], heads=8, kv_heads=2, seed=3, spare_rows=0)
+    out, _ = run(p, None, True)
+    step = torch.empty_like(out)
+    ws = torch.zeros(Q.quest_workspace_bytes(p.cache, 1) // 4, device=p.dev)
+    Q.quest_sparse_decode(p.cache, p.q.contiguous(), None, 0, SCALE, step, workspace=ws)
+    torch.cuda.synchronize()
+    for b in range(p.B):
+        sees = torch.ones(1, p.lens[b], dtype=torch.bool, device=p.dev)
+        for h in range(p.H):
+            want = attention64(p.q[p.rows(b), h].double(), *p.cached(b, h // p.G), sees, SCALE)
+            rounded_once(step[p.rows(b), h], want, ("decode", b, h))
+            rounded_once(out[p.rows(b), h], want, ("prompt", b, h))
