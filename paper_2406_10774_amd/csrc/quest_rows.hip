@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   // Results: through LDS, so that 16 lanes write a row's 256 bytes together.  Two buffers that nobody reads any more have 8 KiB
   // for every wave; k_place spreads the lanes over the banks.
   if (row0 >= w.rows) return;
-  const float total = st.total();
+  const float total = st.total(), met = st.total_met();
   char* mine = lds[(steps + wave / 4) & (kBuffers - 1)][0] + wave % 4 * (32 * kRowBytes);
   const int r = lane & 31;
   auto write_rows = [&](char* to, int index, size_t row_bytes) {   // index: of the lane's row
@@ -190,12 +190,12 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   };
   if (!w.whole()) {
     const size_t part = w.part_row(a, wave * 32);
-    write_floats(st.kUnscale, a.part_acc + part * kHeadDim, r);
+    write_floats(kExact ? st.kUnscale : met > 0.f ? total / met : 1.f, a.part_acc + part * kHeadDim, r);   // (NaN stays in the sums)
     if (lane < 32 && there) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(st.base, total);
     return;
   }
   const int out_row = (w.s.first + token) * (a.kv_heads * a.group) + head;
-  const float factor = total > 0.f ? st.kUnscale / total : 0.f;
+  const float factor = met > 0.f ? st.kUnscale / met : 0.f;
   if constexpr (kExact) {
     write_floats(factor, (float*)a.out, out_row);
   } else {

@@ -22,10 +22,12 @@
 // Weights go to the product in fp16.  For fp32 outputs, and for all outputs of few rows, a weight is two fp16 numbers, 2^14 times its
 // value rounded and what that leaves, 22 bits of it: error 4e-7, three times below fp32 products one after the other.
 // For fp16 outputs of many rows one rounding of each weight, 2^-11 of it, which is what the
-// output's own rounding costs (error against 64 bits, 2-norm: 2.7e-4, 1.3 times that of one rounding at the end, while 22 bits take
-// 1.42 to 1.46 times as long, 32k tokens of 32 / 8 heads 12.2 ms and 8.4; of few rows they take 1.00 to 1.12 times); the base is
+// output's own rounding costs (error against 64 bits, 2-norm: 2.6e-4, 1.3 times that of one rounding at the end, while 22 bits take
+// 1.33 to 1.42 times as long, 32k tokens of 32 / 8 heads 12.0 ms and 8.6; of few rows they take 1.00 to 1.12 times); the base is
 // put so that the largest logit's weight is 2^7 and moves when a weight would pass 2^15, so weights keep all bits down
-// to 2^-21 of the largest and are not lost down to 2^-31.
+// to 2^-21 of the largest and are not lost down to 2^-31.  Outputs are divided by the sum of the weights as rounded, so that a row that
+// sees one value, or the same one everywhere, gets it back (32k tokens 8.35 -> 8.61 ms, error 2.75e-4 -> 2.64e-4); the log-sum-exp is of
+// the weights before.
 // Sums, maxima and accumulators are fp32.
 #pragma once
 
@@ -206,6 +208,7 @@ struct RowState {
   f32x16_t start;      // kShifted: -base
   float base, limit;   // moves when s - base is above; -3e38 while no token has counted
   float l;             // this lane's share of the row's sum
+  float met;           // the same of the weights as the values meet them (not kExact), which outputs are divided by
 
   // Asks for the row's query; what uses it comes after ready().
   __device__ __forceinline__ void init(const char* row, int lane) {
@@ -220,6 +223,7 @@ struct RowState {
     base = 0.f;
     limit = -3e38f;
     l = 0.f;
+    met = 0.f;
   }
   __device__ __forceinline__ void ready(uint32_t sign) {
     if (sign != 0) {
@@ -285,6 +289,7 @@ struct RowState {
       base += by;
       limit = move ? a.limit : limit;
       l *= alpha;
+      met *= alpha;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -315,6 +320,13 @@ struct RowState {
         }
       }
     l += sum[0] + sum[1];
+    if constexpr (!kExact) {
+#pragma unroll
+      for (int i = 0; i < 2 * kBlocks; ++i)
+#pragma unroll
+        for (int r = 0; r < 8; r += 2)
+          met = __builtin_amdgcn_fdot2(half2_t{p.w[i][r], p.w[i][r + 1]}, half2_t{(_Float16)1, (_Float16)1}, met, false);
+    }
   }
   // Add the weighted values, which lie in LDS.
   template <int kBlocks>
@@ -346,9 +358,11 @@ struct RowState {
     add(p, v, lane);
   }
 
-  // The row's whole sum and what the accumulators have to be multiplied by.
-  __device__ __forceinline__ float total() const {
-    const LanePair s = pair_across32(as_u(l));
+  // The row's whole sum, and that of the weights that its values met.
+  __device__ __forceinline__ float total() const { return both_halves(l); }
+  __device__ __forceinline__ float total_met() const { return both_halves(kExact ? l : met); }
+  __device__ __forceinline__ static float both_halves(float v) {
+    const LanePair s = pair_across32(as_u(v));
     return as_f(s.first) + as_f(s.second);
   }
   // log sum exp of a row, of its base and sum.
@@ -369,8 +383,8 @@ struct RowState {
   }
 };
 
-// An fp16 output.  It is a mean of fp16 values, but weights rounded to fp16 may add up to 2^-11 more than their sum: what
-// that carries past the largest fp16 is put back.
+// An fp16 output.  It is a mean of fp16 values: what the roundings of sums over a long context (2^-11 at most) carry past
+// the largest fp16 is put back.
 __device__ __forceinline__ _Float16 half_of(float x) {
   return (_Float16)(fabsf(x) < 65552.f ? __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f) : x);
 }

@@ -72,3 +72,47 @@ def test_single_tokens_as_decode_steps():
             want = attention64(p.q[p.rows(b), h].double(), *p.cached(b, h // p.G), sees, SCALE)
             rounded_once(step[p.rows(b), h], want, ("decode", b, h))
             rounded_once(out[p.rows(b), h], want, ("prompt", b, h))
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("new,past,heads,kv_heads,room", [([700], [0], 40, 40, 0), ([300], [1000], 8, 2, 1 << 16),
+                                                          ([90, 400], [1300, 10], 8, 2, 1 << 16)])
+def test_equal_values_come_back(new, past, heads, kv_heads, room, half):
+    """Many rows, in one piece and in splits, over tokens that all have the same value: that value, whatever the roundings of the
+    weights.  fp32: off by at most the roundings of two sums over n tokens (and a few more), 2.4 n 2^-24; below half a step of
+    fp16, 2^-12 of the value at least, so that fp16 outputs are the value."""
+    data = dict(heads=heads, kv_heads=kv_heads, seed=new[0], room=room, spread=2.0)
+    p, drafts = Packed([n + m for n, m in zip(new, past)], new, **data), Packed(past, new, **data)
+    value = torch.randn(D, device=p.dev).half()
+    for x in (p, drafts):
+        x.v_pool[...] = torch.where(x.v_pool.isnan(), x.v_pool, value)
+        x.v_new[:sum(new)] = value
+    t = Trees(drafts)
+    limit = 2.4 * max(p.lens) * 2.0 ** -24
+    assert limit < 2.0 ** -12
+    for ws in (True, False):
+        for x, tree in ((p, None), (drafts, t)):
+            off = (run(x, tree, half, ws)[0][:sum(new)].double() - value.double()).abs() / value.double().abs()
+            assert bool((off <= (0 if half else limit)).all()), float(off.max())
+
+
+def test_equal_values_under_small_weights():
+    """One key of weight 1 and 8000 of 2^-21.5, which are below fp16's normal numbers: left out of only one of the two sums they would be
+    8000 * 2^-21.5 of the result, 2.7e-3.  The limit as above, and half a step."""
+    n, past = 300, 8000
+    p = Packed([past + n], [n], heads=8, kv_heads=2, seed=5, room=1 << 16)
+    p.k_pool[...] = torch.where(p.k_pool.isnan(), p.k_pool, 0.0)
+    p.k_pool[p.table[0, 0].long(), :, 0, 0] = 1.0
+    p.q[:n] = 0.0
+    p.q[:n, :, 0] = 21.5 * math.log(2)
+    value = torch.randn(D, device=p.dev).half()
+    p.v_pool[...] = torch.where(p.v_pool.isnan(), p.v_pool, value)
+    limit = 2.4 * (past + n) * 2.0 ** -24 + 2.0 ** -11
+    for ws in (p.workspace(), None):
+        out, lse = p.results(True)
+        Q.quest_prompt_attention(p.cache, p.q, p.cu, 1.0, out, lse=lse, workspace=ws)
+        off = (out[:n].double() - value.double()).abs() / value.double().abs()
+        assert bool((off <= limit).all()), float(off.max())
+        want = [math.log(math.exp(float(p.q[0, 0, 0])) + past + i) for i in range(n)]
+        off = (lse[:n].double() - torch.tensor(want, device=p.dev, dtype=torch.float64)[:, None]).abs()
+        assert bool((off <= 2.4 * (past + n) * 2.0 ** -24 * want[0]).all()), float(off.max())
