@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_tokens_kernel(
   const int seq_len = seq_lens[b];
   const int first = seq_len - tokens;                              // position of the first new token
   const int page = first / kS + unit - (first_row / kS + 2 * b);
-  if (tokens <= 0 || first < 0 || page > (seq_len - 1) / kS) return;
+  if (tokens <= 0 || first < 0 || page > (seq_len - 1) / kS || page >= max_pages) return;   // (no page behind the row)
   const int from = max(first - page * kS, 0), to = min(seq_len - page * kS, kS);   // the page's new slots
   const int phys = page_table[(size_t)b * max_pages + page];
   const size_t block = ((size_t)phys * num_heads + head) * (kS * kRowBytes);
