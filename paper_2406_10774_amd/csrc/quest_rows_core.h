@@ -99,6 +99,7 @@ __device__ __forceinline__ T up_to_lane(T v, int lane) {
 // them had nothing to do; work-groups start in order, and those behind the idle ones started a round later.)
 struct Sequence {
   int b, first, tokens, seq_len;   // first: its first packed row
+  int length;                      // cached tokens that its page-table row has room for: nothing behind the row is read
   int row_tiles, slots, chunk;     // chunk: INT32_MAX without splits
   int before;                      // units (row tiles) of the sequences before
   int units_before;
@@ -106,7 +107,7 @@ struct Sequence {
   template <int kRows>
   __device__ __forceinline__ int splits_of(int row_tile, int group) const {   // of a prompt's row tile
     const int rows = tokens * group, limit = seq_len - tokens + (min((row_tile + 1) * kRows, rows) - 1) / group + 1;
-    const int tiles = (limit + kTileTokens - 1) / kTileTokens;
+    const int tiles = (min(limit, length) + kTileTokens - 1) / kTileTokens;
     return (tiles + chunk - 1) / chunk;
   }
   template <bool kTree>
@@ -118,18 +119,20 @@ struct Sequence {
 template <bool kTree, int kRows, bool kByTile>
 __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, const int32_t* __restrict__ cu,
                                               const int32_t* __restrict__ seq_lens, bool list, int want, int lane) {
-  int first = 0, tokens = 0, seq_len = 0, row_tiles = 0;
+  int first = 0, tokens = 0, seq_len = 0, length = 0, row_tiles = 0;
   int places = 0, tiles = 0, last = 0;   // token tiles, of a pair of row tiles at most and of the last one
   auto read = [&](int base) {
     const int i = min(base + lane, a.batch - 1);
     first = cu[i];
     tokens = cu[i + 1] - first;
     seq_len = seq_lens[i];
+    length = min(max(seq_len, 0), a.max_pages << a.page_shift);
     row_tiles = places = base + lane < a.batch ? (tokens * a.group + kRows - 1) / kRows : 0;
-    const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : seq_len;
+    const int context = list ? min(a.k_pages, a.max_pages) << a.page_shift : length;
     last = tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
     if (!kTree && row_tiles > 1 && a.most_units > 0) {   // the last tokens of row tiles j and row_tiles - 1 - j add up to this at most
-      const int64_t both = 2 * (int64_t)(seq_len - tokens) + (row_tiles + 1) * kRows / a.group + 2;
+      int64_t both = 2 * (int64_t)(seq_len - tokens) + (row_tiles + 1) * kRows / a.group + 2;
+      if (length < seq_len) both = min(both, 2 * (int64_t)length);
       tiles = (int)((both + 2 * (kTileTokens - 1)) / kTileTokens);
       places = (row_tiles + 1) / 2;
     }
@@ -184,6 +187,7 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
       s.first = of(first);
       s.tokens = of(tokens);
       s.seq_len = of(seq_len);
+      s.length = of(length);
       s.row_tiles = of(row_tiles);
       s.slots = of(slots);
       s.units_before = of(u - units);
@@ -444,9 +448,9 @@ struct Stream {
     pages = kTree && topk != nullptr ? topk + ((size_t)s.b * a.kv_heads + hk) * a.k_pages : nullptr;
     listed = min(a.k_pages, a.max_pages);
     page_shift = a.page_shift;
-    seq_len = s.seq_len;
+    seq_len = s.length;
     seq_pages = (seq_len + (1 << page_shift) - 1) >> page_shift;
-    limit = kTree ? seq_len : last + 1;
+    limit = kTree ? seq_len : min(last + 1, seq_len);
     const int places = pages != nullptr ? listed << page_shift : max(limit, 0);
     context = (places + kTileTokens - 1) & ~(kTileTokens - 1);
     first = s.first;
@@ -558,7 +562,7 @@ struct Walk {
   __device__ __forceinline__ uint64_t allow(const Stream<kTree>& s, uint64_t held, int step, int position,
                                             const int64_t* __restrict__ mask, int mask_words) const {
     const int at = start + step * stride;
-    if (!kTree) return first_bits(position + 1 - at);
+    if (!kTree) return first_bits(min(position + 1, s.limit) - at);
     if (at < s.context) return held;
     const int node = at - s.context;
     return (node >> 6) < mask_words ? ((uint64_t)mask[node >> 6] >> (node & 63)) & held : 0;
@@ -566,7 +570,7 @@ struct Walk {
   // Whether all rows from `position` on attend to all of them.
   __device__ __forceinline__ bool whole(const Stream<kTree>& s, uint64_t held, int step, int position) const {
     const int at = start + step * stride;
-    return kTree ? at < s.context && held == (kPlaces == 64 ? ~0ull : 0xffffffffull) : at + kPlaces - 1 <= position;
+    return kTree ? at < s.context && held == (kPlaces == 64 ? ~0ull : 0xffffffffull) : at + kPlaces <= min(position + 1, s.limit);
   }
 };
 

@@ -1,11 +1,13 @@
 """Many tokens a sequence, with lengths past the end of the page-table row.  No caller may pass them; insertion stores the tokens
-that the row has room for and nothing elsewhere."""
+that the row has room for and nothing elsewhere, attention is over the row's tokens and reads nothing behind the row."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2406_10774_amd import binding as Q
-from packed_util import D, Packed
+from packed_util import D, Packed, Trees, attention64, check, left_alone
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +37,48 @@ def test_insertion_past_the_row(S, pages, over, new):
     torch.cuda.synchronize()
     for got, w, name in zip((k_pool, v_pool, meta), want, ("k", "v", "meta")):
         assert torch.equal(got.view(torch.int16), w.view(torch.int16)), name
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("S,pages,heads,kv_heads,over,new", [
+    (16, 5, 4, 2, (1, 0, 1000), (1, 5, 40)),               # few rows, in one piece
+    (8, 333, 8, 2, (3, 1 << 24, 0), (2, 1, 7)),            # few rows in splits
+    (16, 37, 40, 40, (300, 7), (700, 650)),                # many rows, in one piece
+    (32, 300, 8, 2, (90, 0), (300, 260)),                  # many rows in splits, paired row tiles
+    (8, 1203, 16, 2, (250, 1 << 30), (300, 301)),          # queries before and behind the row's end
+])
+def test_attention_past_the_row(S, pages, heads, kv_heads, over, new, half):
+    """Sequence b's length is over[b] more than its row holds; a query behind the row's end sees the whole row."""
+    room = pages * S
+    p = Packed([room] * len(over), [min(n, room) for n in new], heads=heads, kv_heads=kv_heads, S=S, seed=S)
+    table = p.table[:, :pages].contiguous()                # the rows end with their pages
+    list_pages = [[list(range(0, pages, 2)) + [pages, pages + 3, 1 << 28]] * kv_heads] * p.B
+    t, listed = Trees(p), Trees(p, lists=list_pages)
+    full = torch.full((p.B,), room, dtype=torch.int32, device=p.dev)
+    past = torch.tensor([room + n for n in over], dtype=torch.int32, device=p.dev)
+    scale = 1 / math.sqrt(D)
+
+    def trees(lens, ws):
+        cache = Q.Cache(p.k_pool, p.v_pool, p.meta, table, lens, num_heads=heads)
+        results = []
+        for x in (t, listed):
+            out, lse = p.results(half)
+            Q.quest_tree_attention(cache, p.q, p.k_new, p.v_new, p.cu, x.mask, scale, out, topk_idx=x.lists, lse=lse, workspace=ws)
+            results += [out, lse]
+        return results
+
+    cache = Q.Cache(p.k_pool, p.v_pool, p.meta, table, past, num_heads=heads)
+    for ws in (p.workspace(), None):
+        for got, want in zip(trees(past, ws), trees(full, ws)):
+            assert torch.equal(got, want)
+        out, lse = p.results(half)
+        Q.quest_prompt_attention(cache, p.q, p.cu, scale, out, lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+        for b in range(p.B):
+            at = p.rows(b)
+            position = torch.arange(room + over[b] - p.new[b], room + over[b], device=p.dev)
+            sees = torch.arange(room, device=p.dev) <= position[:, None]
+            for h in range(heads):
+                want = attention64(p.q[at, h].double(), *p.cached(b, h // p.G), sees, scale)
+                check(out[at, h], lse[at, h], want, half, (b, h))
+        left_alone(p, out, lse)
