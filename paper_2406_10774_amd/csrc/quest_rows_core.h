@@ -405,19 +405,19 @@ __device__ __forceinline__ int v_place(int token, int slot) {
 
 // 16 bytes a lane from memory to LDS at `to` + 16 lane, without registers in between: from a wave's address and a
 // lane's offset, or a lane's address.  The compiler does not count these: dma_arrived<n> waits until at
-// most the last n (and what was loaded since) are under way.  (M0 is the instruction's LDS base; the compiler sets it itself
-// right before where it needs it, which on this target nothing here does.)
+// most the last n (and what was loaded since) are under way.  M0 is the instruction's LDS base; it is an operand here, so that the
+// compiler writes it and knows that what it held is gone.
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 __device__ __forceinline__ void dma16(uint32_t to, const char* base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               ::"{m0}"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
                : "memory");
 }
 __device__ __forceinline__ void dma16(uint32_t to, const char* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               ::"{m0}"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
                : "memory");
 }
 template <int N>
