@@ -8,7 +8,7 @@
 //            stream tokens however few the rows are; their results are joined in LDS.  Bound by memory, or by the chain
 //            of loads before the first tile: 26 drafts at 32k tokens of 32 heads 105 us, 5.1 TB/s.
 // A row tile's tokens are walked in splits where that gives the compute units more to do; a row tile with more than one
-// leaves partial results, which merge_rows_kernel joins (a launch of its own: 4 to 7 us, and up to 64 splits are
+// leaves partial results, which merge_rows_kernel joins (a launch of its own: 4 to 7 us, and up to 95 splits are
 // joined by as many work-groups as there are rows, not by the last one to arrive).
 #include <algorithm>
 

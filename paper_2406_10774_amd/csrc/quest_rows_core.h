@@ -63,7 +63,9 @@ struct RowsArgs {
 };
 
 constexpr int kTileTokens = 64;
-constexpr int kMostSplits = 64;   // of a sequence, about: joining more takes longer than they save (60k tokens of a head: 43 us, 30 with)
+// Splits of the longest sequence, about (a chunk is a whole number of tiles: up to 95): joining more takes longer than they save (60k
+// tokens of a head: 43 us, 30 with).
+constexpr int kMostSplits = 64;
 
 #if defined(__HIPCC__)
 
@@ -89,6 +91,17 @@ __device__ __forceinline__ T up_to_lane(T v, int lane) {
     if (lane >= row * 16) before += end;
   }
   return v + before;
+}
+// The largest v of the wave's lanes (none below 0).
+__device__ __forceinline__ int largest_of_wave(int v) {
+  v = max(v, row_shr<1>(v));
+  v = max(v, row_shr<2>(v));
+  v = max(v, row_shr<4>(v));
+  v = max(v, row_shr<8>(v));
+  int of_rows = 0;
+#pragma unroll
+  for (int row = 1; row <= 4; ++row) of_rows = max(of_rows, __builtin_amdgcn_readlane(v, row * 16 - 1));
+  return of_rows;
 }
 
 // The plan of one sequence, and where its units start.  A unit is a split of a row tile.  Without splits and for trees
@@ -145,15 +158,15 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
   auto whole = [](auto v) { return __builtin_bit_cast(decltype(v), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1)); };
   s.chunk = INT32_MAX;
   if (a.most_units > 0) {
-    float work = 0.f, context = 0.f;
-    int count = 0;
+    float work = 0.f;
+    int count = 0, longest = 0;   // longest: of those that have rows
     for (int base = 0; base < a.batch; base += kWave) {
       read(base);
       work += whole(up_to_lane((float)places * (float)tiles, lane));
       count += whole(up_to_lane(!kTree && row_tiles > 1 ? 2 * places : places, lane));
-      context += whole(up_to_lane(row_tiles > 0 ? (float)last : 0.f, lane));
+      longest = max(longest, largest_of_wave(row_tiles > 0 ? last : 0));
     }
-    const int least = max(a.least_chunk, (int)(context / (float)(kMostSplits * a.batch)));
+    const int least = max(a.least_chunk, longest / kMostSplits);
     // The chunk: with this one the units are at most work / chunk + count, so no more than there is room for (a
     // hundred-thousandth covers the roundings) ..
     const float even = work / (float)max(a.most_units - count, 1) * 1.00001f;
