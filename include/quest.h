@@ -331,7 +331,7 @@ int quest_append_tokens(const quest_cache* cache, const void* k_new, const void*
 /* Bytes of device workspace for quest_prompt_attention and quest_tree_attention on this cache
  * with up to total_tokens packed tokens; it does not fall as total_tokens grows (0: none is used).
  * Pure host function.  The workspace holds the partial results of calls that walk the
- * tokens in several splits: about 35 MB, or 145 MB where sequences may have more than 64 rows (new
+ * tokens in several splits: up to 27 MB, or 140 MB where sequences may have more than 64 rows (new
  * tokens times query heads of a KV head).  It need not be initialised
  * and keeps nothing between calls; calls that share a workspace must not overlap in time.
  * A smaller workspace, or NULL, is accepted: fewer splits, slower, results equal within rounding. */

@@ -444,6 +444,16 @@ struct Plan {
 };
 // Work-groups of a KV head that the compute units take at once: two few_rows_kernel each, or one shared_rows_kernel.
 int at_once(int rows, const quest_cache& c) { return std::max(1, (rows == kFewRows ? 512 : 256) / kv_heads(c)); }
+// Whether tokens are split where row tiles of `of` rows fill a share of the units, and into how many rounds.
+bool worth_splits(int of, double fill, int64_t places) {
+  const double idle = (double)places / kTileTokens * (1 - fill);
+  const bool few = of == kFewRows;
+  return places > 8 * kTileTokens && idle > (fill < 0.15 ? 8 : fill < 0.3 ? 12 : fill < 0.5 ? (few ? 25 : 20) : few ? 50 : 30);
+}
+int rounds_of(int of, int64_t row_tiles, int once, bool tree) {
+  const int most = tree && of == kSharedRows ? 4 : 2;
+  return row_tiles * most <= once ? 1 : most;
+}
 // k_pages: listed pages (0: all).
 Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   const int64_t rows = (int64_t)total_tokens * group_size(c), mean = (rows + c.batch - 1) / c.batch;
@@ -451,11 +461,7 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   const int64_t pages = k_pages > 0 ? std::min(k_pages, c.max_pages_per_seq) : c.max_pages_per_seq;
   const int64_t places = pages * c.page_size + (tree ? new_tokens : 0);   // that a row may attend to
   auto likely = [&](int of) { return std::max<int64_t>(c.batch, rows / of); };   // row tiles
-  auto splits = [&](int of) {
-    const double fill = (double)likely(of) / at_once(of, c), idle = (double)places / kTileTokens * (1 - fill);
-    const bool few = of == kFewRows;
-    return places > 8 * kTileTokens && idle > (fill < 0.15 ? 8 : fill < 0.3 ? 12 : fill < 0.5 ? (few ? 25 : 20) : few ? 50 : 30);
-  };
+  auto splits = [&](int of) { return worth_splits(of, (double)likely(of) / at_once(of, c), places); };
   const double wide = (double)rows * kv_heads(c) / kSharedRows;
   const double work = wide * (tree ? places : std::max(places - new_tokens / 2, places / 2)) / kTileTokens;
   Plan p;
@@ -463,9 +469,8 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
   p.rows = few ? kFewRows : kSharedRows;
   p.row_tiles = (int)(rows / p.rows + c.batch);
   const int once = at_once(p.rows, c);
-  const int rounds = likely(p.rows) * (tree && !few ? 4 : 2) <= once ? 1 : tree && !few ? 4 : 2;
   p.least_chunk = few ? 2 : 8;
-  p.most_units = splits(p.rows) ? std::max(once * rounds, p.row_tiles + (tree ? 1 : c.batch + 1)) : 0;
+  p.most_units = splits(p.rows) ? std::max(once * rounds_of(p.rows, likely(p.rows), once, tree), p.row_tiles + (tree ? 1 : c.batch + 1)) : 0;
   return p;
 }
 int units_of(const Plan& p) { return std::max(p.row_tiles, p.most_units); }
@@ -528,13 +533,21 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
 
 }  // namespace
 
-// Enough for calls with any number of tokens up to this one: four rounds of units, and one more, of the largest
-// row tiles that they may have.
+// The most that plan_of asks for in calls with any number of tokens up to this one: of each kernel that such a call may have, and
+// only if any of them is split.  Fewer tokens have fewer row tiles, and row tiles that fill the units are not split.
 size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens) {
   const int64_t rows = (int64_t)total_tokens * group_size(c);
-  const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + total_tokens;
-  const int of = rows <= 64 * (int64_t)c.batch ? kFewRows : kSharedRows;
-  return places > 8 * kTileTokens && total_tokens > 0 ? (4 * (size_t)at_once(of, c) + 2) * unit_bytes(of, c) : 0;
+  const int64_t places = (int64_t)c.max_pages_per_seq * c.page_size + total_tokens / c.batch;
+  auto most = [&](int of) -> size_t {
+    const int once = at_once(of, c);
+    if (!worth_splits(of, (double)c.batch / once, places)) return 0;
+    const int64_t tiles = std::min<int64_t>(rows / of, once);
+    const int rounds = rounds_of(of, std::max<int64_t>(tiles, c.batch), once, true);
+    return (size_t)std::max<int64_t>((int64_t)once * rounds, tiles + 2 * (int64_t)c.batch + 1) * unit_bytes(of, c);
+  };
+  const double wide = (double)rows * kv_heads(c) / kSharedRows;
+  const bool many = rows > 64 * (int64_t)c.batch && (wide >= 80 || wide * places / kTileTokens >= 800);
+  return total_tokens == 0 ? 0 : std::max(most(kFewRows), many ? most(kSharedRows) : 0);
 }
 
 bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {
