@@ -344,8 +344,9 @@ int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens,
  *   lse[row][h]    = log sum_{j <= p} exp(sm_scale * q.k_j)            (nullable),
  * out [total_tokens][num_heads][head_dim] and lse [total_tokens][num_heads] dense.  fp32 logits, softmax and
  * sums; out is fp32 or fp16 as in quest_sparse_decode.  The softmax weights keep 22 bits when they meet the
- * values; with fp16 out of calls of more than 64 rows (new tokens times query heads of a KV head) a sequence on
- * average they may be rounded to fp16 there.
+ * values (down to 2^-16 of the row's largest weight; smaller ones are off by up to 2^-39 of it); with fp16 out of
+ * calls of more than 64 rows (new tokens times query heads of a KV head) a sequence on average they may be rounded
+ * to fp16 there (11 bits, down to 2^-21 of the largest weight; smaller ones are off by up to 2^-32 of it).
  * Values of all seq_lens[b] tokens have to be finite, also for queries that stand before them (a later token has the
  * weight 0, and 0 times infinity is not 0); slots behind the last token may hold anything.
  * Results must not overlap what the call reads. */

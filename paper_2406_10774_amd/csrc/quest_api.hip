@@ -99,7 +99,7 @@ size_t workspace_bytes_of(const quest_cache& c) {
   return attention_workspace_bytes(c) + selection_workspace_bytes(c);
 }
 
-// What the calls on packed tokens have in common.  `stride`: elements between tokens of `heads` heads.
+// What the calls on packed tokens have in common.
 int check_packed(const quest_cache* c, const int32_t* cu, int32_t total, const char* who) {
   const int r = check_cache(c, who);
   if (r != QUEST_OK) return r;
@@ -119,6 +119,7 @@ int check_packed(const quest_cache* c, const int32_t* cu, int32_t total, const c
   return QUEST_OK;
 }
 
+// Packed rows; `stride`: elements between tokens of `heads` heads.
 int check_rows(const void* data, int64_t stride, int heads, const char* what, const char* who) {
   if (data == nullptr) {
     set_error("%s: %s must not be NULL", who, what);

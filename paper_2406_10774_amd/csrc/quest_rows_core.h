@@ -20,7 +20,8 @@
 // value with 4 (token % 4): the lanes of a read spread over all banks.
 //
 // Weights go to the product in fp16.  For fp32 outputs, and for all outputs of few rows, a weight is two fp16 numbers, 2^14 times its
-// value rounded and what that leaves, 22 bits of it: error 4e-7, three times below fp32 products one after the other.
+// value rounded and what that leaves, 22 bits of it down to 2^-16 of the largest weight, below that to within 2^-39 of the largest (the
+// smallest step of what is left; weights under 2^-39 are in the sum alone): error 4e-7, three times below fp32 products one after the other.
 // For fp16 outputs of many rows one rounding of each weight, 2^-11 of it, which is what the
 // output's own rounding costs (error against 64 bits, 2-norm: 2.6e-4, 1.3 times that of one rounding at the end, while 22 bits take
 // 1.33 to 1.42 times as long, 32k tokens of 32 / 8 heads 12.0 ms and 8.6; of few rows they take 1.00 to 1.12 times); the base is

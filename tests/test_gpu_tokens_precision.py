@@ -116,3 +116,35 @@ def test_equal_values_under_small_weights():
         want = [math.log(math.exp(float(p.q[0, 0, 0])) + past + i) for i in range(n)]
         off = (lse[:n].double() - torch.tensor(want, device=p.dev, dtype=torch.float64)[:, None]).abs()
         assert bool((off <= 2.4 * (past + n) * 2.0 ** -24 * want[0]).all()), float(off.max())
+
+
+@pytest.mark.parametrize("n,room", [(3, 0), (300, 1 << 16)])
+@pytest.mark.parametrize("bits", [14, 20, 25, 31, 36, 38, 41])
+def test_small_weights(bits, n, room):
+    """One key of weight 1 and value 0, 4000 of 2^-bits with values around 1: what they add up to.  With fp32 outputs a weight is off by
+    2^-22 of itself or by 2^-39; with fp16 outputs of many rows by 2^-11 or 2^-32 (the base is put 2^-7 of the largest weight and
+    fp16's smallest step, rounded to half of it, is 2^-24).  Beside that the fp32 limits."""
+    past = 4000
+    p = Packed([past + n], [n], heads=8, kv_heads=2, seed=bits, room=room)
+    p.k_pool[...] = torch.where(p.k_pool.isnan(), p.k_pool, 0.0)
+    p.k_pool[p.table[0, 0].long(), :, 0, 0] = 1.0
+    p.q[:n] = 0.0
+    p.q[:n, :, 0] = bits * math.log(2)
+    p.v_pool[...] = torch.where(p.v_pool.isnan(), p.v_pool, p.v_pool.abs().clamp(max=3.0))
+    p.v_pool[p.table[0, 0].long(), :, 0] = 0.0
+    sees = torch.arange(past + n, device=p.dev) <= torch.arange(past, past + n, device=p.dev)[:, None]
+    for ws in (p.workspace(), None):
+        for half in (True, False):
+            out, lse = p.results(half)
+            Q.quest_prompt_attention(p.cache, p.q, p.cu, 1.0, out, lse=lse, workspace=ws)
+            for h in (0, 7):
+                k, v = p.cached(0, h // p.G)
+                o, l, weight, size, seen = attention64(p.q[:n, h].double(), k, v, sees, 1.0)
+                fp32 = 8 * (math.sqrt(D) * 2.0 ** -24 * size + 2.0 ** -21 + seen.double().sqrt() * 2.0 ** -24)
+                few = not half or n < 64
+                bound = (fp32[:, None] + (2.0 ** -22 if few else 2.0 ** -11)) * weight + seen[:, None] * 3.0 * 2.0 ** (-39 if few else -32)
+                if half:
+                    bound = bound + 2.0 ** -11 * o.abs() + 2.0 ** -25
+                off = (out[:n, h].double() - o).abs()
+                assert bool((off <= bound).all()), (half, float((off / bound).max()))
+                assert bool(((lse[:n, h].double() - l).abs() <= fp32 * l.abs().clamp(min=1.0)).all())
