@@ -327,7 +327,11 @@ def quest_tree_attention(cache: Cache, q, k_new, v_new, cu_tokens, tree_mask, sm
     shape, heads, new_shape = q.shape, cache.heads, k_new.shape
     q_stride = _rows_of(cache, shape, q, heads)
     new_stride = _rows_of(cache, new_shape, k_new, cache.kv_heads, v_new)
-    total, (mask_rows, words), k_pages = shape[0], tree_mask.shape, 0
+    total, k_pages = shape[0], 0
+    if tree_mask.dim() != 2 or topk_idx is not None and (topk_idx.dim() != 3 or topk_idx.shape[1] != cache.kv_heads):
+        raise QuestError(-2, f"tree_mask of shape {tuple(tree_mask.shape)}{'' if topk_idx is None else f' and topk_idx of {tuple(topk_idx.shape)}'}"
+                             f": have to be [rows][words] and [batch][{cache.kv_heads}][k_pages]")
+    mask_rows, words = tree_mask.shape
     if new_shape[0] < total or mask_rows < total:
         raise QuestError(-2, f"{new_shape[0]} rows of keys and values and {mask_rows} of masks for {total} of queries")
     _plain(cache, tree_mask, i64, 0, "tree_mask")
