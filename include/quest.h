@@ -334,7 +334,11 @@ int quest_append_tokens(const quest_cache* cache, const void* k_new, const void*
  * tokens in several splits: up to 27 MB, or 140 MB where sequences may have more than 64 rows (new
  * tokens times query heads of a KV head).  It need not be initialised
  * and keeps nothing between calls; calls that share a workspace must not overlap in time.
- * A smaller workspace, or NULL, is accepted: fewer splits, slower, results equal within rounding. */
+ * A smaller workspace, or NULL, is accepted: fewer splits, slower (without any, few rows over a long context are
+ * walked by one work-group a KV head), results equal within rounding.  Nothing is split either where the batch
+ * times the KV heads is about 512 or more (256 with more than 64 rows a sequence), sequences without new tokens
+ * included: a sequence much longer than the others is faster in a call of its own there.  Short prompts are up to
+ * twice as fast with a page table that is no wider than they need: its width is taken for the longest length. */
 int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens, size_t* out_bytes);
 
 /* Causal attention of packed queries over the cache: the last n_b of the seq_lens[b] cached tokens

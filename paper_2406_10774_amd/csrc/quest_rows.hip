@@ -2,11 +2,11 @@
 //
 // Two kernels, chosen by the rows that a sequence has on average and by how much there is to do (plan_of):
 //   many rows (shared_rows_kernel)  eight waves of 32 rows share the tiles of tokens, fetched once for 256 rows.  Bound by
-//            the matrix cores and by power: 32k tokens of 32 query / 8 KV heads 8.2 to 8.5 ms, 1040 to 1070 TFLOP/s (a large
-//            library product 1310), at 1.9 GHz; with zeros for data the clock stays at 2.4 GHz and it is 7.0.
+//            the matrix cores and by power: 32k tokens of 32 query / 8 KV heads 8.45 to 8.65 ms, 1020 to 1040 TFLOP/s (a large
+//            library product 1310), at 1.9 GHz; with zeros for data the clock stays at 2.4 GHz (7.0 ms where it was 8.2 to 8.5).
 //   few rows (few_rows_kernel)      every wave of a work-group has all 32 rows and tiles of its own, so that four waves
 //            stream tokens however few the rows are; their results are joined in LDS.  Bound by memory, or by the chain
-//            of loads before the first tile: 26 drafts at 32k tokens of 32 heads 105 us, 5.1 TB/s.
+//            of loads before the first tile: 26 drafts at 32k tokens of 32 heads 107 us, 5.0 TB/s.
 // A row tile's tokens are walked in splits where that gives the compute units more to do; a row tile with more than one
 // leaves partial results, which merge_rows_kernel joins (a launch of its own: 4 to 7 us, and up to 95 splits are
 // joined by as many work-groups as there are rows, not by the last one to arrive).
@@ -77,7 +77,7 @@ struct Part {
 // the fetch 300 to 700.  32k tokens of 32 / 8 heads took 12.2 ms with all waves in the same turn, 8.5 with the tiles through
 // registers (this: 8.2), 9.7 in work-groups of 128 rows and no turns, two on a compute unit, and 9.9 with one
 // wave of 64 rows on each SIMD and the softmax between its own products.  Reading keys or values of the next turn
-// ahead changed it by less than 1 %.
+// ahead changed it by less than 1 %.  (All before the sum of the weights as rounded, 16 instructions of the softmax, which adds 3 to 4 %.)
 template <bool kTree, bool kExact>
 __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -419,7 +419,10 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 
 // How a call is cut up, from what the host knows.  The figures are of 820 calls, from 6 to 12000 rows a sequence over contexts
 // up to 60000 tokens by 1 to 64 heads, each with both kernels, with and without splits: the rules take 1 % longer than the
-// best of the four on average.
+// best of the four on average.  (The lengths of a batch were from half or a quarter of the longest, page-table rows ended with it, and the small
+// kernel rounded the weights of fp16 outputs, 1.00 to 1.12 times as fast as it is.)  The row of the page table is taken for the longest
+// length: in wide tables short prompts have the large kernel and splits that find nothing to split (77 tokens of 32 heads in rows of 2048
+// pages 13.4 us, in rows of their own length 6.7).
 //   Splits: where the row tiles leave compute units idle for long enough.  Idle is the share of the units without
 //   a row tile times the row's tiles of tokens; a join costs as much as 8 to 12 of them (60 drafts of 8 heads at 600
 //   tokens 12 us with splits and 15 without), 20 to 25 where more than a third of the units have a row tile (sixteen
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 //   third of it to start and to join.  It has calls of up to 64 rows a sequence (64 rows at 65k tokens of 8 heads:
 //   56 us and 63 with the large one; 128 rows: 89 and 67), and those of less than 80 row tiles of the large one and
 //   little work, counted in 256 rows by 64 tokens: 3000 (400 tokens behind 600 of 32 / 8 heads: 22 us and 33; fifteen
-//   prompts of 500 tokens of 64 / 8 heads: 182 and 82), or 800 where the large one would split (60 tokens in ten
+//   prompts of 250 to 500 tokens of 64 / 8 heads: 182 and 82), or 800 where the large one would split (60 tokens in ten
 //   sequences of 6000 of 64 / 8 heads 160 and 153, one of 150 behind 3000 59 and 40).
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
