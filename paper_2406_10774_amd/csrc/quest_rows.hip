@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
   Stream<kTree> stream;
   stream.init(a, s, hk, s.seq_len - s.tokens + (min(row0 + kRows, rows) - 1) / a.group, nullptr, topk);
   const int parts = (stream.tiles + s.chunk - 1) / s.chunk;
-  if (parts == 1) return;  // written already
+  if (parts <= 1) return;  // written already, or rows that see nothing
   const size_t step = (size_t)s.places<kTree>() * a.kv_heads * kRows;   // rows between two splits' parts
   // The slot of split i: 2 i + odd for the first `turns`, then i + turns.
   int place = s.row_tiles - 1 - (tile - s.before), turns = 0, odd = 0;

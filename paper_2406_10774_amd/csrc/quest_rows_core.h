@@ -123,7 +123,7 @@ struct Sequence {
   template <int kRows>
   __device__ __forceinline__ int splits_of(int row_tile, int group) const {   // of a prompt's row tile
     const int rows = tokens * group, limit = seq_len - tokens + (min((row_tile + 1) * kRows, rows) - 1) / group + 1;
-    const int tiles = (min(limit, length) + kTileTokens - 1) / kTileTokens;
+    const int tiles = (max(min(limit, length), 0) + kTileTokens - 1) / kTileTokens;
     return (tiles + chunk - 1) / chunk;
   }
   template <bool kTree>
@@ -148,7 +148,7 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
     last = tiles = (context + kTileTokens - 1) / kTileTokens + (kTree ? (tokens + kTileTokens - 1) / kTileTokens : 0);
     if (!kTree && row_tiles > 1 && a.most_units > 0) {   // the last tokens of row tiles j and row_tiles - 1 - j add up to this at most
       int64_t both = 2 * (int64_t)(seq_len - tokens) + (row_tiles + 1) * kRows / a.group + 2;
-      if (length < seq_len) both = min(both, 2 * (int64_t)length);
+      if (length < seq_len || seq_len < tokens) both = 2 * (int64_t)length;   // (past the row, or before the first token)
       tiles = (int)((both + 2 * (kTileTokens - 1)) / kTileTokens);
       places = (row_tiles + 1) / 2;
     }

@@ -82,3 +82,33 @@ def test_attention_past_the_row(S, pages, heads, kv_heads, over, new, half):
                 want = attention64(p.q[at, h].double(), *p.cached(b, h // p.G), sees, scale)
                 check(out[at, h], lse[at, h], want, half, (b, h))
         left_alone(p, out, lse)
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,lens,new,short", [
+    (8, 2, (5000, 700, 3000), (300, 300, 200), 40),         # many rows in splits, paired row tiles
+    (8, 2, (9000, 64, 9000), (20, 40, 3), 1),               # few rows in splits
+    (40, 40, (700, 650), (700, 600), 0),                    # many rows, in one piece
+])
+def test_lengths_without_the_new_tokens(heads, kv_heads, lens, new, short, half):
+    """Sequence 1's length is less than its new tokens (it does not count them yet, say).  No caller may pass that; the other sequences have
+    their results, and queries at positions from 0 on theirs."""
+    p = Packed(lens, new, heads=heads, kv_heads=kv_heads, seed=short, room=1 << 14 if kv_heads < 40 else 0)
+    p.lens[1] = short
+    p.seq_lens.copy_(torch.tensor(p.lens))
+    scale = 1 / math.sqrt(D)
+    for ws in (p.workspace(), None):
+        out, lse = p.results(half)
+        Q.quest_prompt_attention(p.cache, p.q, p.cu, scale, out, lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+        for b in range(p.B):
+            position = torch.arange(p.lens[b] - p.new[b], p.lens[b], device=p.dev)
+            there = position >= 0
+            at = torch.arange(int(p.cu_np[b]), int(p.cu_np[b + 1]), device=p.dev)[there]
+            if not len(at):
+                continue
+            sees = torch.arange(p.lens[b], device=p.dev) <= position[there][:, None]
+            for h in range(heads):
+                want = attention64(p.q[at, h].double(), *p.cached(b, h // p.G), sees, scale)
+                check(out[at, h], lse[at, h], want, half, (b, h))
+        left_alone(p, out, lse)
