@@ -16,7 +16,8 @@
  *                       is the whole step in one call)
  *
  * and what comes before and beside it, many tokens at a time: quest_append_tokens,
- * quest_prompt_attention, quest_tree_attention.
+ * quest_prompt_attention, quest_tree_attention; quest_rotate_append_tokens turns queries and
+ * keys by their position on the way.  Pages may hold 8 bits a number (QUEST_FLAG_E4M3_PAGES).
  *
  * Conventions for every entry point
  *   - All data pointers are DEVICE pointers owned by the caller.  The library
@@ -91,6 +92,8 @@ typedef enum quest_status {
  *    counter (the textbook form of the hand-over; by default the results
  *    travel through device-scope stores and loads and need no fence).  For
  *    testing that path: slower, changes no result.
+ *  QUEST_FLAG_E4M3_PAGES: k_pool and v_pool hold 8-bit numbers ("Pages of 8 bits"
+ *    below).
  *  QUEST_FLAG_KEEP_FIRST_PAGE, QUEST_FLAG_KEEP_NEWEST_PAGE: selection policy of
  *    quest_topk and quest_decode_step.  The paper selects purely by score
  *    (Section 3.4) and that is the default; with these flags logical page 0
@@ -102,7 +105,8 @@ enum {
   QUEST_FLAG_SEPARATE_LAUNCHES = 1,
   QUEST_FLAG_DEVICE_FENCES = 2,
   QUEST_FLAG_KEEP_FIRST_PAGE = 4,
-  QUEST_FLAG_KEEP_NEWEST_PAGE = 8
+  QUEST_FLAG_KEEP_NEWEST_PAGE = 8,
+  QUEST_FLAG_E4M3_PAGES = 16
 };
 
 /* Description of one layer's paged KV cache.  Host struct, passed by pointer;
@@ -122,7 +126,28 @@ typedef struct quest_cache {
   const int32_t* seq_lens;    /* device                                      */
   int32_t num_kv_heads;       /* 0 or num_heads: one KV head per query head;
                                  else a divisor of num_heads (see below)     */
+  float* scales;              /* device; read with QUEST_FLAG_E4M3_PAGES only */
 } quest_cache;
+
+/* Pages of 8 bits (QUEST_FLAG_E4M3_PAGES): half the bytes of the fp16 cache.
+ *   k_pool, v_pool : e4m3 (1 sign, 4 exponent, 3 mantissa bits, no infinities; OCP),
+ *                    [num_phys_pages][KV heads][page_size][head_dim], on 16 bytes
+ *   scales         : fp32 [num_phys_pages][KV heads][2], of the keys and of the values
+ *                    of a (page, KV head), on 8 bytes
+ * A number stands for its e4m3 value times its scale.  A scale is a power of two, 2^e:
+ * the smallest e from -15 on with which the largest magnitude of the page's tokens is at
+ * most 448 * 2^e; magnitudes above 61440 count as 61440.  So a stored number is off by at most 2^-4 of its
+ * value or 2^-10 * 2^e, whichever is more, and is always an fp16 number: attention over these pages is
+ * attention over an fp16 cache that holds what they stand for.  A page that gets more tokens keeps its
+ * e or takes a larger one; what it holds is then rounded to that (exact, but for what becomes an e4m3 subnormal).
+ * Metadata is of the keys in fp16, before they are rounded to 8 bits, so that the same
+ * pages are selected as with the fp16 cache.
+ * Calls on such a cache: quest_append_tokens and quest_rotate_append_tokens fill it (a decode step's token
+ * too); quest_estimate and quest_topk as on any cache; quest_sparse_decode, quest_select_decode,
+ * quest_decode_step and quest_prompt_attention read it (select and step as launches of
+ * their own for each phase).  QUEST_ERR_UNSUPPORTED: quest_build_meta, quest_tree_attention, quest_decode_step_static, and
+ * a token's insertion by the single-token calls (k_pool_write != 0).  quest_sparse_decode and its like take any workspace, or
+ * NULL, without a refusal: a smaller one makes fewer splits, slower. */
 
 /* Bytes of device workspace for quest_sparse_decode, quest_select_decode and
  * quest_decode_step on this cache: one size for every call on the cache shape
@@ -327,6 +352,34 @@ int quest_decode_step_static(const quest_cache* cache, const void* k_new, const 
  * trusted), row rows[cu_tokens[b] + i]: the accepted ones among drafted tokens. */
 int quest_append_tokens(const quest_cache* cache, const void* k_new, const void* v_new, int64_t new_stride,
                         const int32_t* rows, const int32_t* cu_tokens, int32_t total_tokens, void* stream);
+
+/* Rotation of queries and keys by their position.  Of the first rotary_dim channels of a head, pair i is
+ *   (x, y) -> (x c - y s, x s + y c),   c = table[position][i],  s = table[position][rotary_dim / 2 + i];
+ * pair i is channels i and rotary_dim / 2 + i, or 2 i and 2 i + 1 if interleaved; channels from rotary_dim on stay as they
+ * are.  Products and sums are rounded to fp32, results to fp16.  The table (device, fp32 [num_positions][rotary_dim],
+ * on 16 bytes) is the caller's, so any frequencies and scalings will do; far positions want their angles in 64 bits.
+ * The position of packed token i of sequence b is seq_lens[b] - n_b + i, or positions[its row] (nullable, device int32,
+ * total_tokens entries: drafted nodes at their depth).  A position outside the table makes the channels NaN. */
+typedef struct quest_rotation {
+  const float* table;         /* device                                      */
+  const int32_t* positions;   /* device, or NULL                             */
+  int32_t num_positions;      /* rows of the table, >= 1                     */
+  int32_t rotary_dim;         /* a multiple of 16, 16 to head_dim            */
+  int32_t interleaved;
+} quest_rotation;
+
+/* Packed rows of `heads` heads, turned: out[row] = rotation of x[row] for rows below cu_tokens[batch].  Of the cache only its
+ * shape and seq_lens are used.  Strides in elements, as above; out may be x itself with the same stride, and must not overlap it otherwise. */
+int quest_rotate_tokens(const quest_cache* cache, const quest_rotation* rotation, const void* x, int64_t x_stride,
+                        int32_t heads, const int32_t* cu_tokens, int32_t total_tokens, void* out, int64_t out_stride,
+                        void* stream);
+
+/* quest_rotate_tokens of q into q_out and of k_new, then quest_append_tokens of the turned keys and of v_new, in one
+ * launch: the same results, bit for bit; k_new and v_new are only read.  A prompt's tokens, or a decode step's.  q (and
+ * q_out) may be NULL: keys and values only.  q_out may be q itself with the same stride; results must not overlap inputs otherwise. */
+int quest_rotate_append_tokens(const quest_cache* cache, const quest_rotation* rotation, const void* q, int64_t q_stride,
+                               void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new,
+                               int64_t new_stride, const int32_t* cu_tokens, int32_t total_tokens, void* stream);
 
 /* Bytes of device workspace for quest_prompt_attention and quest_tree_attention on this cache
  * with up to total_tokens packed tokens; it does not fall as total_tokens grows (0: none is used).

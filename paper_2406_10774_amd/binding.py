@@ -18,6 +18,7 @@ QUEST_FLAG_SEPARATE_LAUNCHES = 1
 QUEST_FLAG_DEVICE_FENCES = 2
 QUEST_FLAG_KEEP_FIRST_PAGE = 4
 QUEST_FLAG_KEEP_NEWEST_PAGE = 8
+QUEST_FLAG_E4M3_PAGES = 16
 STATUS_NAMES = {0: "QUEST_OK", -1: "QUEST_ERR_NULL", -2: "QUEST_ERR_SHAPE",
                 -3: "QUEST_ERR_UNSUPPORTED", -4: "QUEST_ERR_WORKSPACE", -5: "QUEST_ERR_HIP"}
 
@@ -25,7 +26,8 @@ EXPORTS = ("quest_workspace_bytes", "quest_build_meta", "quest_append_meta", "qu
            "quest_append_estimate", "quest_topk", "quest_topk_workspace_bytes", "quest_sparse_decode",
            "quest_select_decode", "quest_step_workspace_bytes", "quest_decode_step",
            "quest_decode_step_static", "quest_append_tokens", "quest_tokens_workspace_bytes",
-           "quest_prompt_attention", "quest_tree_attention", "quest_last_error")
+           "quest_prompt_attention", "quest_tree_attention", "quest_rotate_tokens",
+           "quest_rotate_append_tokens", "quest_last_error")
 
 
 class QuestError(RuntimeError):
@@ -42,8 +44,13 @@ class quest_cache(ctypes.Structure):
         ("num_phys_pages", ctypes.c_int64),
         ("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("meta", ctypes.c_void_p),
         ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
-        ("num_kv_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("scales", ctypes.c_void_p),
     ]
+
+
+class quest_rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("num_positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 _lib = None
@@ -80,6 +87,9 @@ def load():
     lib.quest_prompt_attention.argtypes = [cp, vp, i64, vp, i32, f32, vp, i32, vp, vp, ctypes.c_size_t, vp]
     lib.quest_tree_attention.argtypes = [cp, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, f32, vp, i32, vp, vp,
                                          ctypes.c_size_t, vp]
+    rp = ctypes.POINTER(quest_rotation)
+    lib.quest_rotate_tokens.argtypes = [cp, rp, vp, i64, i32, vp, i32, vp, i64, vp]
+    lib.quest_rotate_append_tokens.argtypes = [cp, rp, vp, i64, vp, i64, vp, vp, i64, vp, i32, vp]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = ctypes.c_int
     lib.quest_last_error.argtypes = []
@@ -133,16 +143,34 @@ def _check(status):
         raise QuestError(status, load().quest_last_error().decode())
 
 
+def _check_e4m3(k_pool, v_pool, scales):
+    import torch
+    N, Hkv = k_pool.shape[:2]
+    for pool in (k_pool, v_pool):
+        if pool is None or pool.dtype not in (torch.float8_e4m3fn, torch.uint8) or not pool.is_contiguous() or pool.shape != k_pool.shape:
+            raise QuestError(-2, "pools of 8 bits have to be float8_e4m3fn (or uint8), contiguous and of the same shape")
+    if (scales is None or scales.dtype is not torch.float32 or not scales.is_contiguous() or tuple(scales.shape) != (N, Hkv, 2)
+            or scales.device != k_pool.device or v_pool.device != k_pool.device):
+        raise QuestError(-2, f"pages of 8 bits need scales: float32 [{N}][{Hkv}][2], contiguous, on the pools' device")
+
+
 class Cache:
     """Host-side description of one layer's paged KV cache (see quest_cache in quest.h).
 
     Holds references to the caller's torch tensors so they outlive the calls."""
 
-    def __init__(self, k_pool, v_pool, meta, page_table, seq_lens, flags=0, num_heads=None):
+    def __init__(self, k_pool, v_pool, meta, page_table, seq_lens, flags=0, num_heads=None, scales=None):
         """num_heads: query heads, if more than the KV heads of the pools (grouped-query
-        attention); default: one KV head per query head."""
+        attention); default: one KV head per query head.  scales: float32 [pages][KV heads][2] of pools of 8 bits
+        (torch.float8_e4m3fn, or its bytes as torch.uint8)."""
         N, Hkv, S, D = k_pool.shape
         H = Hkv if num_heads is None else int(num_heads)
+        if scales is not None or k_pool.element_size() == 1:
+            _check_e4m3(k_pool, v_pool, scales)
+            flags = int(flags) | QUEST_FLAG_E4M3_PAGES
+        elif int(flags) & QUEST_FLAG_E4M3_PAGES:
+            raise QuestError(-2, "pages of 8 bits need scales")
+        self.scales = scales
         self.k_pool, self.v_pool, self.meta = k_pool, v_pool, meta
         self.page_table, self.seq_lens = page_table, seq_lens
         self.c = quest_cache(
@@ -150,9 +178,33 @@ class Cache:
             max_pages_per_seq=page_table.shape[1], flags=int(flags), num_phys_pages=N,
             k_pool=k_pool.data_ptr(), v_pool=v_pool.data_ptr() if v_pool is not None else None,
             meta=meta.data_ptr(), page_table=page_table.data_ptr(), seq_lens=seq_lens.data_ptr(),
-            num_kv_heads=0 if H == Hkv else Hkv)
+            num_kv_heads=0 if H == Hkv else Hkv, scales=None if scales is None else scales.data_ptr())
         self.heads, self.kv_heads, self.batch, self.head_dim = H, Hkv, page_table.shape[0], D
         self.device = k_pool.get_device()
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+class Rotation:
+    """Rotation of queries and keys by their position (see quest_rotation in quest.h).
+
+    table: float32 [positions][rotary_dim], the cosines of a position's angles, then their sines; positions: int32, of
+    every packed row, if not where the sequence's length puts it."""
+
+    def __init__(self, table, interleaved=False, positions=None):
+        import torch
+        if table.dim() != 2 or table.dtype is not torch.float32 or not table.is_contiguous():
+            raise QuestError(-2, f"table of shape {tuple(table.shape)} ({table.dtype}): has to be float32 [positions][rotary_dim], contiguous")
+        if positions is not None and (positions.dtype is not torch.int32 or not positions.is_contiguous()
+                                      or positions.device != table.device):
+            raise QuestError(-2, f"positions ({positions.dtype}, {positions.device}): have to be int32, contiguous, on the table's device")
+        self.table, self.positions = table, positions
+        self.rows = None if positions is None else positions.numel()
+        self.device = table.get_device()
+        self.c = quest_rotation(table=table.data_ptr(), positions=_ptr(positions), num_positions=table.shape[0],
+                                rotary_dim=table.shape[1], interleaved=int(bool(interleaved)))
 
     @property
     def ref(self):
@@ -344,3 +396,42 @@ def quest_tree_attention(cache: Cache, q, k_new, v_new, cu_tokens, tree_mask, sm
         cache.ref, q.data_ptr(), q_stride, k_new.data_ptr(), v_new.data_ptr(), new_stride, cu_tokens.data_ptr(),
         total, tree_mask.data_ptr(), words, _ptr(topk_idx), k_pages, float(sm_scale), out.data_ptr(),
         out.dtype is _half, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream_of(cache, stream)))
+
+
+def _rotation_of(cache, rotation, total):
+    if rotation.device != cache.device or rotation.rows is not None and rotation.rows < total:
+        raise QuestError(-2, f"rotation on device {rotation.device} with positions of {rotation.rows} rows: has to be on the cache's "
+                             f"device, with a position for each of {total} rows")
+
+
+def quest_rotate_tokens(cache: Cache, rotation: Rotation, x, cu_tokens, out, stream=None):
+    _, i32, _ = _types or _types_of_torch()
+    shape, out_shape = x.shape, out.shape
+    heads = shape[1] if len(shape) == 3 else 0
+    stride, out_stride = _rows_of(cache, shape, x, heads), _rows_of(cache, out_shape, out, heads)
+    if out_shape[0] < shape[0]:
+        raise QuestError(-2, f"{out_shape[0]} rows of results for {shape[0]}")
+    _rotation_of(cache, rotation, shape[0])
+    _plain(cache, cu_tokens, i32, cache.batch + 1, "cu_tokens")
+    _check(load().quest_rotate_tokens(cache.ref, rotation.ref, x.data_ptr(), stride, heads, cu_tokens.data_ptr(), shape[0],
+                                      out.data_ptr(), out_stride, _stream_of(cache, stream)))
+
+
+def quest_rotate_append_tokens(cache: Cache, rotation: Rotation, q, k_new, v_new, cu_tokens, q_out=None, stream=None):
+    """q and q_out: None for keys and values only."""
+    _, i32, _ = _types or _types_of_torch()
+    shape = k_new.shape
+    stride = _rows_of(cache, shape, k_new, cache.kv_heads, v_new)
+    total, q_stride, out_stride = shape[0], 0, 0
+    if (q is None) != (q_out is None):
+        raise QuestError(-1, "q and q_out: both or neither")
+    if q is not None:
+        q_shape, out_shape = q.shape, q_out.shape
+        q_stride, out_stride = _rows_of(cache, q_shape, q, cache.heads), _rows_of(cache, out_shape, q_out, cache.heads)
+        if q_shape[0] < total or out_shape[0] < total:
+            raise QuestError(-2, f"{q_shape[0]} rows of queries and {out_shape[0]} of results for {total} of keys")
+    _rotation_of(cache, rotation, total)
+    _plain(cache, cu_tokens, i32, cache.batch + 1, "cu_tokens")
+    _check(load().quest_rotate_append_tokens(
+        cache.ref, rotation.ref, _ptr(q), q_stride, _ptr(q_out), out_stride, k_new.data_ptr(), v_new.data_ptr(), stride,
+        cu_tokens.data_ptr(), total, _stream_of(cache, stream)))

@@ -2,6 +2,7 @@
 // kernel launchers.  Nothing here allocates, frees or synchronises.
 #include "quest_common.h"
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 
@@ -95,8 +96,73 @@ bool take_workspace(const quest_cache& c, int32_t k_pages, bool selects, void* w
   return true;
 }
 
+// A phase is a launch of its own on pages of 8 bits.
+quest_cache separate(const quest_cache& c) {
+  quest_cache r = c;
+  r.flags |= QUEST_FLAG_SEPARATE_LAUNCHES;
+  return r;
+}
+size_t attention_e4m3_bytes(const quest_cache& c) { return (decode_e4m3_workspace_bytes(c) + 255) / 256 * 256; }
 size_t workspace_bytes_of(const quest_cache& c) {
+  if (e4m3_pages(c)) return attention_e4m3_bytes(c) + selection_workspace_bytes(separate(c));
   return attention_workspace_bytes(c) + selection_workspace_bytes(c);
+}
+
+// What calls that read or write pages of 8 bits need; fp16 pages need nothing here.
+int check_e4m3(const quest_cache& c, const char* who) {
+  if (!e4m3_pages(c)) return QUEST_OK;
+  if (c.scales == nullptr) {
+    set_error("%s: pages of 8 bits need scales", who);
+    return QUEST_ERR_NULL;
+  }
+  if ((uintptr_t)c.k_pool % 16 != 0 || (uintptr_t)c.v_pool % 16 != 0 || (uintptr_t)c.scales % 8 != 0) {
+    set_error("%s: pools of 8 bits must lie on 16 bytes, their scales on 8", who);
+    return QUEST_ERR_SHAPE;
+  }
+  if (!decode_e4m3_fits_a_launch(c)) {
+    set_error("%s: batch and heads do not fit a launch", who);
+    return QUEST_ERR_SHAPE;
+  }
+  return QUEST_OK;
+}
+// Calls that know fp16 pages only.
+int refuse_e4m3(const quest_cache& c, const char* what, const char* who) {
+  if (!e4m3_pages(c)) return QUEST_OK;
+  set_error("%s: %s is for fp16 pages only", who, what);
+  return QUEST_ERR_UNSUPPORTED;
+}
+
+int check_rotation(const quest_rotation* r, const char* who) {
+  if (r == nullptr || r->table == nullptr) {
+    set_error("%s: rotation and its table must not be NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  if (r->rotary_dim < 16 || r->rotary_dim > kHeadDim || r->rotary_dim % 16 != 0) {
+    set_error("%s: rotary_dim must be a multiple of 16 from 16 to %d (got %d)", who, kHeadDim, r->rotary_dim);
+    return QUEST_ERR_UNSUPPORTED;
+  }
+  if (r->num_positions < 1 || (uintptr_t)r->table % 16 != 0) {
+    set_error("%s: the table must lie on 16 bytes and have a row (got %d)", who, r->num_positions);
+    return QUEST_ERR_SHAPE;
+  }
+  return QUEST_OK;
+}
+
+// Attention over pages of 8 bits; scores: select the pages first.
+int attend_e4m3(const quest_cache& c, const void* q, const float* scores, const int32_t* topk_idx, int32_t* topk_out,
+                int32_t* k_eff, int32_t k_pages, float sm_scale, void* out, int32_t out_is_fp16, float* lse, void* workspace,
+                size_t bytes, const char* who, hipStream_t s) {
+  if (workspace == nullptr) bytes = 0;
+  const size_t attention = std::min(bytes, attention_e4m3_bytes(c));
+  if (scores != nullptr) {
+    const size_t candidates = topk_scratch_bytes(c, k_pages);
+    const int r = candidates > 0 && bytes - attention >= candidates
+                      ? launch_topk_chunked(c, scores, k_pages, topk_out, k_eff, (char*)workspace + attention, s)
+                      : launch_topk(c, scores, k_pages, topk_out, k_eff, s);
+    if (r != QUEST_OK) return r;
+    topk_idx = topk_out;
+  }
+  return launch_decode_e4m3(c, q, topk_idx, k_pages, sm_scale, out, out_is_fp16 != 0, lse, workspace, attention, who, s);
 }
 
 // What the calls on packed tokens have in common.
@@ -166,6 +232,7 @@ int quest_workspace_bytes(const quest_cache* cache, int32_t k_pages, size_t* out
 int quest_build_meta(const quest_cache* cache, void* stream) {
   int r = check_cache(cache, "quest_build_meta");
   if (r != QUEST_OK) return r;
+  if ((r = refuse_e4m3(*cache, "the call", "quest_build_meta")) != QUEST_OK) return r;
   if (cache->k_pool == nullptr || cache->meta == nullptr) {
     set_error("quest_build_meta: k_pool and meta must not be NULL");
     return QUEST_ERR_NULL;
@@ -177,6 +244,7 @@ int quest_append_meta(const quest_cache* cache, const void* k_new, const void* v
                       int32_t k_pool_write, void* stream) {
   int r = check_cache(cache, "quest_append_meta");
   if (r != QUEST_OK) return r;
+  if (k_pool_write && (r = refuse_e4m3(*cache, "k_pool_write", "quest_append_meta")) != QUEST_OK) return r;
   if (cache->meta == nullptr || k_new == nullptr) {
     set_error("quest_append_meta: meta and k_new must not be NULL");
     return QUEST_ERR_NULL;
@@ -203,6 +271,7 @@ int quest_append_estimate(const quest_cache* cache, const void* k_new, const voi
                           int32_t k_pool_write, const void* q, float* scores, void* stream) {
   int r = check_cache(cache, "quest_append_estimate");
   if (r != QUEST_OK) return r;
+  if (k_pool_write && (r = refuse_e4m3(*cache, "k_pool_write", "quest_append_estimate")) != QUEST_OK) return r;
   if (cache->meta == nullptr || k_new == nullptr || q == nullptr || scores == nullptr) {
     set_error("quest_append_estimate: meta, k_new, q and scores must not be NULL");
     return QUEST_ERR_NULL;
@@ -264,6 +333,11 @@ int quest_sparse_decode(const quest_cache* cache, const void* q, const int32_t* 
     set_error("quest_sparse_decode: k_pages must be >= 1 with a page list (got %d)", k_pages);
     return QUEST_ERR_SHAPE;
   }
+  if (e4m3_pages(*cache)) {
+    if ((r = check_e4m3(*cache, "quest_sparse_decode")) != QUEST_OK) return r;
+    return attend_e4m3(*cache, q, nullptr, topk_idx, nullptr, nullptr, k_pages, sm_scale, out, out_is_fp16, lse, workspace,
+                       workspace_bytes, "quest_sparse_decode", (hipStream_t)stream);
+  }
   Workspace w;
   if (!take_workspace(*cache, topk_idx ? k_pages : 0, false, workspace, workspace_bytes, &w, "quest_sparse_decode"))
     return QUEST_ERR_WORKSPACE;
@@ -288,6 +362,11 @@ int quest_select_decode(const quest_cache* cache, const void* q, const float* sc
   if (k_pages < 1) {
     set_error("quest_select_decode: k_pages must be >= 1 (got %d)", k_pages);
     return QUEST_ERR_SHAPE;
+  }
+  if (e4m3_pages(*cache)) {
+    if ((r = check_e4m3(*cache, "quest_select_decode")) != QUEST_OK) return r;
+    return attend_e4m3(*cache, q, scores, nullptr, topk_idx, k_eff, k_pages, sm_scale, out, out_is_fp16, lse, workspace,
+                       workspace_bytes, "quest_select_decode", (hipStream_t)stream);
   }
   Workspace w;
   if (!take_workspace(*cache, k_pages, true, workspace, workspace_bytes, &w, "quest_select_decode"))
@@ -318,6 +397,7 @@ int quest_decode_step(const quest_cache* cache, const void* k_new, const void* v
                       void* stream) {
   int r = check_cache(cache, "quest_decode_step");
   if (r != QUEST_OK) return r;
+  if (k_new != nullptr && k_pool_write && (r = refuse_e4m3(*cache, "k_pool_write", "quest_decode_step")) != QUEST_OK) return r;
   if (cache->k_pool == nullptr || cache->v_pool == nullptr || cache->meta == nullptr ||
       q == nullptr || scores == nullptr || topk_idx == nullptr || out == nullptr) {
     set_error("quest_decode_step: k_pool, v_pool, meta, q, scores, topk_idx and out must not be NULL");
@@ -330,6 +410,14 @@ int quest_decode_step(const quest_cache* cache, const void* k_new, const void* v
   if (k_pages < 1) {
     set_error("quest_decode_step: k_pages must be >= 1 (got %d)", k_pages);
     return QUEST_ERR_SHAPE;
+  }
+  if (e4m3_pages(*cache)) {
+    if ((r = check_e4m3(*cache, "quest_decode_step")) != QUEST_OK) return r;
+    r = k_new != nullptr ? launch_append_estimate(*cache, k_new, nullptr, 0, q, scores, (hipStream_t)stream)
+                         : launch_estimate(*cache, q, scores, (hipStream_t)stream);
+    if (r != QUEST_OK) return r;
+    return attend_e4m3(*cache, q, scores, nullptr, topk_idx, k_eff, k_pages, sm_scale, out, out_is_fp16, lse, workspace,
+                       workspace_bytes, "quest_decode_step", (hipStream_t)stream);
   }
   Workspace w;
   if (!take_workspace(*cache, k_pages, true, workspace, workspace_bytes, &w, "quest_decode_step"))
@@ -344,6 +432,7 @@ int quest_decode_step_static(const quest_cache* cache, const void* k_new, const 
                              int32_t out_is_fp16, float* lse, void* stream) {
   int r = check_cache(cache, "quest_decode_step_static");
   if (r != QUEST_OK) return r;
+  if ((r = refuse_e4m3(*cache, "the call", "quest_decode_step_static")) != QUEST_OK) return r;
   if (cache->k_pool == nullptr || cache->v_pool == nullptr || cache->meta == nullptr ||
       q == nullptr || scores == nullptr || topk_idx == nullptr || out == nullptr) {
     set_error("quest_decode_step_static: k_pool, v_pool, meta, q, scores, topk_idx and out must not be NULL");
@@ -373,7 +462,49 @@ int quest_append_tokens(const quest_cache* cache, const void* k_new, const void*
   }
   if ((r = check_rows(k_new, new_stride, kv_heads(*cache), "k_new", who)) != QUEST_OK) return r;
   if ((r = check_rows(v_new, new_stride, kv_heads(*cache), "v_new", who)) != QUEST_OK) return r;
+  if (e4m3_pages(*cache)) {
+    if ((r = check_e4m3(*cache, who)) != QUEST_OK) return r;
+    return launch_insert(*cache, {cu_tokens, total_tokens}, nullptr, nullptr, 0, nullptr, 0, k_new, v_new, new_stride, rows, who,
+                         (hipStream_t)stream);
+  }
   return launch_append_tokens(*cache, {cu_tokens, total_tokens}, k_new, v_new, new_stride, rows, (hipStream_t)stream);
+}
+
+int quest_rotate_tokens(const quest_cache* cache, const quest_rotation* rotation, const void* x, int64_t x_stride,
+                        int32_t heads, const int32_t* cu_tokens, int32_t total_tokens, void* out, int64_t out_stride,
+                        void* stream) {
+  const char* who = "quest_rotate_tokens";
+  int r = check_packed(cache, cu_tokens, total_tokens, who);
+  if (r != QUEST_OK || (r = check_rotation(rotation, who)) != QUEST_OK || total_tokens == 0) return r;
+  if (heads < 1 || heads > 65535 || (int64_t)total_tokens * heads > INT32_MAX) {
+    set_error("%s: heads must be 1 to 65535 and total_tokens * heads fit a launch (got %d)", who, heads);
+    return QUEST_ERR_SHAPE;
+  }
+  if ((r = check_rows(x, x_stride, heads, "x", who)) != QUEST_OK) return r;
+  if ((r = check_rows(out, out_stride, heads, "out", who)) != QUEST_OK) return r;
+  return launch_rotate_rows(*cache, {cu_tokens, total_tokens}, *rotation, x, x_stride, heads, out, out_stride,
+                            (hipStream_t)stream);
+}
+
+int quest_rotate_append_tokens(const quest_cache* cache, const quest_rotation* rotation, const void* q, int64_t q_stride,
+                               void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new,
+                               int64_t new_stride, const int32_t* cu_tokens, int32_t total_tokens, void* stream) {
+  const char* who = "quest_rotate_append_tokens";
+  int r = check_packed(cache, cu_tokens, total_tokens, who);
+  if (r != QUEST_OK || (r = check_rotation(rotation, who)) != QUEST_OK || total_tokens == 0) return r;
+  if (cache->k_pool == nullptr || cache->v_pool == nullptr || cache->meta == nullptr) {
+    set_error("%s: k_pool, v_pool and meta must not be NULL", who);
+    return QUEST_ERR_NULL;
+  }
+  if ((r = check_rows(k_new, new_stride, kv_heads(*cache), "k_new", who)) != QUEST_OK) return r;
+  if ((r = check_rows(v_new, new_stride, kv_heads(*cache), "v_new", who)) != QUEST_OK) return r;
+  if (q != nullptr) {
+    if ((r = check_rows(q, q_stride, cache->num_heads, "q", who)) != QUEST_OK) return r;
+    if ((r = check_rows(q_out, q_out_stride, cache->num_heads, "q_out", who)) != QUEST_OK) return r;
+  }
+  if ((r = check_e4m3(*cache, who)) != QUEST_OK) return r;
+  return launch_insert(*cache, {cu_tokens, total_tokens}, rotation, q, q_stride, q_out, q_out_stride, k_new, v_new, new_stride,
+                       nullptr, who, (hipStream_t)stream);
 }
 
 int quest_tokens_workspace_bytes(const quest_cache* cache, int32_t total_tokens, size_t* out_bytes) {
@@ -396,6 +527,7 @@ int quest_prompt_attention(const quest_cache* cache, const void* q, int64_t q_st
   if (r != QUEST_OK || total_tokens == 0) return r;
   if ((r = check_rows(q, q_stride, cache->num_heads, "q", who)) != QUEST_OK) return r;
   if ((r = check_results(*cache, out, workspace, who)) != QUEST_OK) return r;
+  if ((r = check_e4m3(*cache, who)) != QUEST_OK) return r;
   return launch_prompt(*cache, {cu_tokens, total_tokens}, q, q_stride, sm_scale, out, out_is_fp16 != 0, lse, workspace,
                        workspace_bytes, (hipStream_t)stream);
 }
@@ -406,7 +538,8 @@ int quest_tree_attention(const quest_cache* cache, const void* q, int64_t q_stri
                          int32_t out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   const char* who = "quest_tree_attention";
   int r = check_packed(cache, cu_tokens, total_tokens, who);
-  if (r != QUEST_OK || total_tokens == 0) return r;
+  if (r != QUEST_OK) return r;
+  if ((r = refuse_e4m3(*cache, "the call", who)) != QUEST_OK || total_tokens == 0) return r;
   if ((r = check_rows(q, q_stride, cache->num_heads, "q", who)) != QUEST_OK) return r;
   if ((r = check_rows(k_new, new_stride, kv_heads(*cache), "k_new", who)) != QUEST_OK) return r;
   if ((r = check_rows(v_new, new_stride, kv_heads(*cache), "v_new", who)) != QUEST_OK) return r;

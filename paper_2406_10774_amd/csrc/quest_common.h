@@ -33,6 +33,7 @@ typedef short short2_t __attribute__((ext_vector_type(2)));
 // KV heads and query heads per KV head of a cache (grouped-query attention).
 inline int kv_heads(const quest_cache& c) { return c.num_kv_heads > 0 ? c.num_kv_heads : c.num_heads; }
 inline int group_size(const quest_cache& c) { return c.num_heads / kv_heads(c); }
+inline bool e4m3_pages(const quest_cache& c) { return (c.flags & QUEST_FLAG_E4M3_PAGES) != 0; }
 
 // ---------------------------------------------------------------- host side
 void set_error(const char* fmt, ...);
@@ -129,6 +130,17 @@ struct PackedTokens {
 };
 int launch_append_tokens(const quest_cache& c, const PackedTokens& p, const void* k_new, const void* v_new,
                          int64_t new_stride, const int32_t* rows, hipStream_t s);
+// Insertion with rotation (rotation != nullptr; then also of q into q_out, if given), or into pages of 8 bits, or both.
+int launch_insert(const quest_cache& c, const PackedTokens& p, const quest_rotation* rotation, const void* q, int64_t q_stride,
+                  void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new, int64_t new_stride,
+                  const int32_t* rows, const char* who, hipStream_t s);
+int launch_rotate_rows(const quest_cache& c, const PackedTokens& p, const quest_rotation& rotation, const void* x, int64_t x_stride,
+                       int heads, void* out, int64_t out_stride, hipStream_t s);
+// Attention over pages of 8 bits (topk_idx == nullptr: all).  With less workspace fewer splits; none is needed.
+size_t decode_e4m3_workspace_bytes(const quest_cache& c);
+bool decode_e4m3_fits_a_launch(const quest_cache& c);
+int launch_decode_e4m3(const quest_cache& c, const void* q, const int32_t* topk_idx, int k_pages, float sm_scale, void* out,
+                       int out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, const char* who, hipStream_t s);
 // Attention of packed query rows (strides in elements between tokens).  With less workspace than
 // tokens_workspace_bytes the tokens are walked in fewer splits; none is needed.
 size_t tokens_workspace_bytes(const quest_cache& c, int total_tokens);

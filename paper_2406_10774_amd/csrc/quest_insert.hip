@@ -1,0 +1,369 @@
+// Insertion of tokens with their rotation on the way, and insertion into pages of 8 bits (with or without rotation).
+// (Insertion into fp16 pages as keys and values are given: quest_append.hip.)
+//
+// Rotation: of the first rotary_dim channels pair (x, y) becomes (x c - y s, x s + y c), c and s from the table's row of the token's
+// position.  Products and the sum are rounded to fp32 one by one, so that the result is what the same three operations give anywhere
+// (a fused multiply-add would be nearer to the exact value by less than the rounding to fp16 that follows).
+//
+// 8 bits: the scale of a page belongs to all of its tokens, so a wave has a whole (page, head) in registers before it rounds the first
+// number.  A page that held tokens before keeps its scale unless the new ones need a larger one; then its old numbers are rounded again.
+//
+// Bound by memory: every number is read once and written once.  A wave has one (page, head), the waves of a work-group adjacent
+// heads; queries follow in the same launch, a wave having four tokens (whose table rows it then reads once) of kQHeads heads.
+//
+// Without any length on the host: the pages of sequence b start at unit floor(cu[b] / S) + 2 b, which leaves
+// room for the floor((n + S - 2) / S) + 1 pages that n >= 1 tokens can touch.
+#include "quest_common.h"
+#include "quest_e4m3.h"
+
+namespace quest {
+
+namespace {
+
+constexpr int kInsertWaves = 4;
+constexpr int kQHeads = 4;
+
+struct InsertArgs {
+  char* k_pool;
+  char* v_pool;
+  char* meta;
+  float2* scales;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  const int32_t* cu;
+  const int32_t* rows;
+  const char* k_new;
+  const char* v_new;
+  const char* q;
+  char* q_out;
+  int64_t new_stride, q_stride, q_out_stride;   // bytes between tokens
+  int batch, kv_heads, q_heads, max_pages, total;
+  int64_t num_phys_pages, waves;                // waves: of the insertion
+  int64_t insert_blocks;
+  const float* table;
+  const int32_t* positions;
+  int num_positions, rotary, interleaved;
+};
+
+// The last sequence that starts at or before `what` (of its packed row, or its page's unit).
+template <class Start>
+__device__ __forceinline__ int sequence_at(const InsertArgs& a, int what, int lane, Start start) {
+  int b = -1;
+  for (int base = 0; base < a.batch; base += kWave) {
+    const int i = base + lane;
+    const bool before = i < a.batch && start(i < a.batch ? i : 0) <= what;
+    const int n = __popcll(__ballot(before));
+    b += n;
+    if (n < kWave) break;
+  }
+  return __builtin_amdgcn_readfirstlane(b);
+}
+
+// A lane's cosines and sines: it has channels 8 c .. 8 c + 7 of a token, c = lane % 16.
+struct Turn {
+  float4 cos0, cos1, sin0, sin1;   // (interleaved: the first of each)
+  __device__ __forceinline__ void load(const InsertArgs& a, int position, int chunk) {
+    const int half = a.rotary >> 1;
+    if (chunk * 8 >= a.rotary) return;
+    const bool there = position >= 0 && position < a.num_positions;
+    const int first = a.interleaved ? chunk * 4 : chunk * 8 < half ? chunk * 8 : chunk * 8 - half;
+    const float* row = a.table + (size_t)(there ? position : 0) * a.rotary + first;
+    cos0 = *reinterpret_cast<const float4*>(row);
+    sin0 = *reinterpret_cast<const float4*>(row + half);
+    if (!a.interleaved) {
+      cos1 = *reinterpret_cast<const float4*>(row + 4);
+      sin1 = *reinterpret_cast<const float4*>(row + half + 4);
+    }
+    if (!there) {   // no number for a position without a row
+      const float none = __builtin_nanf("");
+      cos0 = cos1 = sin0 = sin1 = make_float4(none, none, none, none);
+    }
+  }
+};
+
+__device__ __forceinline__ uint32_t two_halves(float a, float b) {
+  return __builtin_bit_cast(uint32_t, half2_t{(_Float16)a, (_Float16)b});
+}
+// own c + other s, each operation rounded.
+__device__ __forceinline__ float turned(float own, float c, float other, float s) {
+#pragma clang fp contract(off)
+  const float a = own * c, b = other * s;
+  return a + b;
+}
+__device__ __forceinline__ float half_lo(uint32_t h) { return (float)__builtin_bit_cast(half2_t, h)[0]; }
+__device__ __forceinline__ float half_hi(uint32_t h) { return (float)__builtin_bit_cast(half2_t, h)[1]; }
+
+// The rotation of 8 channels; every lane of the wave has to be here (halves are exchanged between lanes).
+__device__ __forceinline__ uint4 turn(const InsertArgs& a, uint4 v, const Turn& t, int chunk, int lane) {
+  const bool stays = chunk * 8 >= a.rotary;
+  uint4 r;
+  if (a.interleaved) {
+    auto pair = [&](uint32_t h, float c, float s) {
+      const float x = half_lo(h), y = half_hi(h);
+      return two_halves(turned(x, c, -y, s), turned(y, c, x, s));
+    };
+    r = make_uint4(pair(v.x, t.cos0.x, t.sin0.x), pair(v.y, t.cos0.y, t.sin0.y), pair(v.z, t.cos0.z, t.sin0.z),
+                   pair(v.w, t.cos0.w, t.sin0.w));
+  } else {
+    const int by = a.rotary >> 4;   // lanes between the channels of a pair
+    const bool second = chunk >= by;
+    const int from = (stays ? lane : second ? lane - by : lane + by) * 4;
+    const uint4 o = make_uint4(__builtin_amdgcn_ds_bpermute(from, v.x), __builtin_amdgcn_ds_bpermute(from, v.y),
+                               __builtin_amdgcn_ds_bpermute(from, v.z), __builtin_amdgcn_ds_bpermute(from, v.w));
+    const float sign = second ? 1.f : -1.f;
+    auto two = [&](uint32_t own, uint32_t other, float c0, float s0, float c1, float s1) {
+      return two_halves(turned(half_lo(own), c0, half_lo(other), sign * s0), turned(half_hi(own), c1, half_hi(other), sign * s1));
+    };
+    r = make_uint4(two(v.x, o.x, t.cos0.x, t.sin0.x, t.cos0.y, t.sin0.y), two(v.y, o.y, t.cos0.z, t.sin0.z, t.cos0.w, t.sin0.w),
+                   two(v.z, o.z, t.cos1.x, t.sin1.x, t.cos1.y, t.sin1.y), two(v.w, o.w, t.cos1.z, t.sin1.z, t.cos1.w, t.sin1.w));
+  }
+  return stays ? v : r;
+}
+
+// Queries (any packed rows): four tokens of kQHeads heads.
+__device__ __forceinline__ void turn_rows(const InsertArgs& a, int64_t at, int lane) {
+  const int sub = lane >> 4, chunk = lane & 15;
+  const int groups = (a.q_heads + kQHeads - 1) / kQHeads;
+  const int64_t four = at / groups;
+  const int head0 = (int)(at - four * groups) * kQHeads;
+  if (four * 4 >= a.total) return;
+  const int row0 = (int)four * 4, rows_there = a.cu[a.batch];
+  if (row0 >= rows_there) return;
+  const int row = min(row0 + sub, rows_there - 1);
+  const bool mine = row0 + sub < rows_there;
+  uint4 v[kQHeads];
+#pragma unroll
+  for (int i = 0; i < kQHeads; ++i)
+    v[i] = ld16_stream(a.q + row * a.q_stride + (int64_t)min(head0 + i, a.q_heads - 1) * kRowBytes + chunk * 16);
+  int position;
+  if (a.positions != nullptr) {
+    position = a.positions[row];
+  } else {
+    int b = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int of = sequence_at(a, min(row0 + k, rows_there - 1), lane, [&](int i) { return a.cu[i]; });
+      if (sub == k) b = of;
+    }
+    position = a.seq_lens[b] - (a.cu[b + 1] - row);
+  }
+  Turn t;
+  t.load(a, position, chunk);
+#pragma unroll
+  for (int i = 0; i < kQHeads; ++i) {
+    const uint4 r = turn(a, v[i], t, chunk, lane);
+    if (mine && head0 + i < a.q_heads) st16(a.q_out + row * a.q_out_stride + (int64_t)(head0 + i) * kRowBytes + chunk * 16, r);
+  }
+}
+
+__global__ __launch_bounds__(kInsertWaves* kWave) void rotate_rows_kernel(const InsertArgs a) {
+  turn_rows(a, (int64_t)blockIdx.x * kInsertWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane_id());
+}
+
+// The largest 16-bit magnitude of the wave.
+__device__ __forceinline__ uint32_t largest_half(uint32_t m2) {
+  m2 = key_max2(m2, m2 >> 16);
+  m2 = key_max2(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, 0x128, 0xf, 0xf, true));
+  m2 = key_max2(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, 0x124, 0xf, 0xf, true));
+  m2 = key_max2(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, 0x122, 0xf, 0xf, true));
+  m2 = key_max2(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, 0x121, 0xf, 0xf, true));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)rows_key_max2(m2)) & 0xffffu;
+}
+
+// The page's numbers (keys or values) to 8 bits; x: slots 4 i + sub, channels 8 chunk ..+7.  Returns the scale.
+template <int kLoads>
+__device__ __forceinline__ float round_page(char* block, const uint4 (&x)[kLoads], int from, int to, float old, int lane) {
+  const int sub = lane >> 4, chunk = lane & 15;
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int slot = 4 * i + sub;
+    if (slot >= from && slot < to)
+      most = key_max2(key_max2(key_max2(most, magnitude2(x[i].x)), key_max2(magnitude2(x[i].y), magnitude2(x[i].z))),
+                      magnitude2(x[i].w));
+  }
+  int e = exponent_for(largest_half(most));
+  if (from > 0) e = max(e, exponent_of(old));
+  const float scale = scale_of(e);
+  if (from > 0 && scale != old) {
+    for (int slot = sub; slot < from; slot += 4) {
+      uint2* at = reinterpret_cast<uint2*>(block + slot * kRowBytes8 + chunk * 8);
+      *at = codes_of(halves_of(*at, old), scale);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int slot = 4 * i + sub;
+    if (slot >= from && slot < to)
+      *reinterpret_cast<uint2*>(block + slot * kRowBytes8 + chunk * 8) = codes_of(at_most8(x[i]), scale);
+  }
+  return scale;
+}
+
+template <int kS, bool k8, bool kRotate>
+__global__ __launch_bounds__(kInsertWaves* kWave) void insert_kernel(const InsertArgs a) {
+  constexpr int kLoads = kS / 4;   // wave-wide loads of four tokens each
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (kRotate && blockIdx.x >= a.insert_blocks) {
+    turn_rows(a, (blockIdx.x - a.insert_blocks) * kInsertWaves + wave, lane);
+    return;
+  }
+  const int64_t at = (int64_t)blockIdx.x * kInsertWaves + wave;
+  if (at >= a.waves) return;
+  const int unit = (int)(at / a.kv_heads);
+  const int head = (int)(at - (int64_t)unit * a.kv_heads);
+  const int b = sequence_at(a, unit, lane, [&](int i) { return a.cu[i] / kS + 2 * i; });
+  const int first_row = a.cu[b];
+  const int tokens = a.cu[b + 1] - first_row;
+  const int seq_len = a.seq_lens[b];
+  const int first = seq_len - tokens;                              // position of the first new token
+  const int page = first / kS + unit - (first_row / kS + 2 * b);
+  if (tokens <= 0 || first < 0 || page > (seq_len - 1) / kS || page >= a.max_pages) return;   // (no page behind the row)
+  const int from = max(first - page * kS, 0), to = min(seq_len - page * kS, kS);   // the page's new slots
+  const int phys = a.page_table[(size_t)b * a.max_pages + page];
+  const size_t block = (size_t)phys * a.kv_heads + head;
+  const int sub = lane >> 4, chunk = lane & 15;
+
+  uint4 k[kLoads], v[kLoads];
+  int row[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int slot = 4 * i + sub;
+    const bool here = slot >= from && slot < to;
+    row[i] = first_row + (here ? page * kS + slot - first : 0);
+    int source = row[i];
+    if (a.rows != nullptr) source = a.rows[source];
+    const int64_t off = source * a.new_stride + (int64_t)head * kRowBytes + chunk * 16;
+    k[i] = ld16_stream(a.k_new + off);
+    v[i] = ld16_stream(a.v_new + off);
+  }
+  float2 old = make_float2(0.f, 0.f);
+  if (k8 && from > 0) old = a.scales[block];
+  if constexpr (kRotate) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      Turn t;
+      t.load(a, a.positions != nullptr ? a.positions[row[i]] : first + row[i] - first_row, chunk);
+      k[i] = turn(a, k[i], t, chunk, lane);
+    }
+  }
+
+  uint4 mn = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+  uint4 mx = make_uint4(0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int slot = 4 * i + sub;
+    if (slot >= from && slot < to) {
+      const uint4 key = order_key8(k[i]);
+      mn = key_min8(mn, key);
+      mx = key_max8(mx, key);
+    }
+  }
+  if constexpr (k8) {
+    const float k_scale = round_page<kLoads>(a.k_pool + block * (kS * kRowBytes8), k, from, to, old.x, lane);
+    const float v_scale = round_page<kLoads>(a.v_pool + block * (kS * kRowBytes8), v, from, to, old.y, lane);
+    if (lane == 0) a.scales[block] = make_float2(k_scale, v_scale);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int slot = 4 * i + sub;
+      if (slot >= from && slot < to) {
+        const size_t off = block * (kS * kRowBytes) + (size_t)slot * kRowBytes + chunk * 16;
+        st16(a.k_pool + off, k[i]);
+        st16(a.v_pool + off, v[i]);
+      }
+    }
+  }
+  mn = rows_key_min8(mn);
+  mx = rows_key_max8(mx);
+  if (lane < 32) {
+    char* entry = a.meta + meta_offset(a.num_phys_pages, phys, head) + lane * 16;
+    uint4 mine = sub == 0 ? mn : mx;
+    if (from > 0) {
+      const uint4 before = order_key8(ld16(entry));
+      mine = sub == 0 ? key_min8(mine, before) : key_max8(mine, before);
+    }
+    st16(entry, order_key8(mine));
+  }
+}
+
+int64_t waves_of_rows(const InsertArgs& a) { return ((int64_t)a.total + 3) / 4 * ((a.q_heads + kQHeads - 1) / kQHeads); }
+
+template <int kS>
+int launch_insert_for(const InsertArgs& a, bool pages8, bool rotate, const char* who, hipStream_t s) {
+  const int64_t rows = rotate && a.q != nullptr ? (waves_of_rows(a) + kInsertWaves - 1) / kInsertWaves : 0;
+  const dim3 grid((unsigned)(a.insert_blocks + rows)), block(kInsertWaves * kWave);
+  if (!pages8)
+    hipLaunchKernelGGL((insert_kernel<kS, false, true>), grid, block, 0, s, a);
+  else if (rotate)
+    hipLaunchKernelGGL((insert_kernel<kS, true, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((insert_kernel<kS, true, false>), grid, block, 0, s, a);
+  return check_launch(who);
+}
+
+InsertArgs rotation_args(const quest_cache& c, const PackedTokens& p, const quest_rotation* r) {
+  InsertArgs a = {};
+  a.seq_lens = c.seq_lens;
+  a.cu = p.cu;
+  a.batch = c.batch;
+  a.total = p.total;
+  if (r != nullptr) {
+    a.table = r->table;
+    a.positions = r->positions;
+    a.num_positions = r->num_positions;
+    a.rotary = r->rotary_dim;
+    a.interleaved = r->interleaved != 0;
+  }
+  return a;
+}
+
+}  // namespace
+
+int launch_insert(const quest_cache& c, const PackedTokens& p, const quest_rotation* rotation, const void* q, int64_t q_stride,
+                  void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new, int64_t new_stride,
+                  const int32_t* rows, const char* who, hipStream_t s) {
+  InsertArgs a = rotation_args(c, p, rotation);
+  a.k_pool = (char*)c.k_pool;
+  a.v_pool = (char*)c.v_pool;
+  a.meta = (char*)c.meta;
+  a.scales = e4m3_pages(c) ? (float2*)c.scales : nullptr;
+  a.page_table = c.page_table;
+  a.rows = rows;
+  a.k_new = (const char*)k_new;
+  a.v_new = (const char*)v_new;
+  a.new_stride = new_stride * 2;
+  a.q = (const char*)q;
+  a.q_out = (char*)q_out;
+  a.q_stride = q_stride * 2;
+  a.q_out_stride = q_out_stride * 2;
+  a.kv_heads = kv_heads(c);
+  a.q_heads = c.num_heads;
+  a.max_pages = c.max_pages_per_seq;
+  a.num_phys_pages = c.num_phys_pages;
+  a.waves = ((int64_t)p.total / c.page_size + 2 * (int64_t)c.batch) * a.kv_heads;
+  a.insert_blocks = (a.waves + kInsertWaves - 1) / kInsertWaves;
+  const bool pages8 = e4m3_pages(c), rotate = rotation != nullptr;
+  switch (c.page_size) {
+    case 8: return launch_insert_for<8>(a, pages8, rotate, who, s);
+    case 32: return launch_insert_for<32>(a, pages8, rotate, who, s);
+    case 64: return launch_insert_for<64>(a, pages8, rotate, who, s);
+    default: return launch_insert_for<16>(a, pages8, rotate, who, s);
+  }
+}
+
+int launch_rotate_rows(const quest_cache& c, const PackedTokens& p, const quest_rotation& rotation, const void* x, int64_t x_stride,
+                       int heads, void* out, int64_t out_stride, hipStream_t s) {
+  InsertArgs a = rotation_args(c, p, &rotation);
+  a.q = (const char*)x;
+  a.q_out = (char*)out;
+  a.q_stride = x_stride * 2;
+  a.q_out_stride = out_stride * 2;
+  a.q_heads = heads;
+  const int64_t blocks = (waves_of_rows(a) + kInsertWaves - 1) / kInsertWaves;
+  hipLaunchKernelGGL(rotate_rows_kernel, dim3((unsigned)blocks), dim3(kInsertWaves * kWave), 0, s, a);
+  return check_launch("quest_rotate_tokens");
+}
+
+}  // namespace quest

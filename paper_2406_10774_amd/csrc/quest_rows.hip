@@ -78,7 +78,10 @@ struct Part {
 // registers (this: 8.2), 9.7 in work-groups of 128 rows and no turns, two on a compute unit, and 9.9 with one
 // wave of 64 rows on each SIMD and the softmax between its own products.  Reading keys or values of the next turn
 // ahead changed it by less than 1 %.  (All before the sum of the weights as rounded, 16 instructions of the softmax, which adds 3 to 4 %.)
-template <bool kTree, bool kExact>
+//
+// k8: pages of 8 bits.  A wave has eight tokens of a tile, which are on their way to its registers for a whole step: in its turn of
+// softmax of tile t it puts its share of tile t + 2 into LDS as fp16 numbers and asks for that of tile t + 3.
+template <bool kTree, bool kExact, bool k8>
 __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   const int wave_first = w.position(row0);
 
   RowState<kExact, true> st;
-  Walk<kTree, kTileTokens> walk;
+  Walk<kTree, kTileTokens, k8> walk;
   walk.init(w.stream, w.first_tile * kTileTokens, kTileTokens);
   const int steps = w.end_tile - w.first_tile;
   uint64_t held = 0, held1 = 0, held2 = 0;   // of tiles t, t + 1, ..
@@ -111,12 +114,47 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
                  lds_address(values(step)));
     return kTree ? walk.held(step, lane) : 0;
   };
-  walk.find(w.stream, 0, lane);
-  st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
-  held = fetch(0);
-  held1 = fetch(1);
-  st.ready(a.q_sign);
-  dma_arrived<0>();
+  // k8: a wave's eight tokens of a tile, asked for and put into LDS
+  static_assert(!k8 || (!kTree && kTileTokens == 8 * kSharedWaves), "eight tokens a wave");
+  uint4 key8, value8;
+  auto ask8 = [&](int step) {
+    if (step >= steps) return;
+    if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
+    walk.load8(a, w.stream, w.hk, step, wave * 8, lane, key8, value8);
+  };
+  auto put8 = [&](int step) {
+    if (step < steps) walk.put8(step, wave * 8, lane, key8, value8, keys(step), values(step));
+  };
+  if constexpr (k8) {
+    walk.find8(a, w.stream, w.hk, 0, lane);
+    st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+    ask8(0);
+    const uint4 key0 = key8, value0 = value8;
+    ask8(1);
+    walk.put8(0, wave * 8, lane, key0, value0, keys(0), values(0));
+    put8(1);
+    ask8(2);
+    st.ready(a.q_sign);
+  } else {
+    walk.find(w.stream, 0, lane);
+    st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+    held = fetch(0);
+    held1 = fetch(1);
+    st.ready(a.q_sign);
+    dma_arrived<0>();
+  }
+  auto arrived = [] {
+    if constexpr (!k8) dma_arrived<0>();
+  };
+  auto next = [&](int step) -> uint64_t {
+    if constexpr (k8) {
+      put8(step);
+      ask8(step + 1);
+      return 0;
+    } else {
+      return fetch(step);
+    }
+  };
   __syncthreads();
   const bool second = wave >= kSharedWaves / 2;
   if (second) __syncthreads();
@@ -135,10 +173,10 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
       held = held1, held1 = held2;
     };
     auto rest = [&](int step) {
-      dma_arrived<0>();
+      arrived();
       __builtin_amdgcn_s_setprio(0);
       turn();
-      held2 = fetch(step + 2);
+      held2 = next(step + 2);
       softmax(step);
       __builtin_amdgcn_s_setprio(1);   // products first where both waves could issue (1 % of the time)
       turn();
@@ -153,9 +191,9 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     st.template add<2>(p, values(steps - 1), lane);
   } else {
     for (int step = 0; step < steps; ++step) {
-      dma_arrived<0>();
+      arrived();
       turn();
-      held2 = fetch(step + 2);
+      held2 = next(step + 2);
       held = held1, held1 = held2;
       turn();
     }
@@ -209,11 +247,11 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
 // With 64 rows a wave (one work-group on a compute unit instead of two) 64 rows took as long as two tiles of 32: 61 us and 58
 // at 65k tokens of 8 heads.  Weights keep 22 bits whatever the output's type, so that an fp16 output is the fp32 one rounded, as in
 // the decode calls: a prompt of one token is as exact as a decode step.
-template <bool kTree, bool kHalfOut>
+template <bool kTree, bool kHalfOut, bool k8>
 __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
-  constexpr int kTokens = 32, kLoads = kTokens / 4;
+  constexpr int kTokens = 32, kEach = k8 ? 8 : 4, kLoads = kTokens / kEach;   // kEach: tokens of a wave-wide load
   constexpr int kStride = kHeadDim + 4;
   constexpr int kStage = 2 * kTokens * kRowBytes, kJoin = kFewRows * kStride * 4;
   __shared__ __align__(16) char lds[kWaves * (kStage > kJoin ? kStage : kJoin)];
@@ -231,7 +269,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   const int first_position = w.position(w.row0);
 
   RowState<true, false> st;
-  Walk<kTree, kTokens> walk;
+  Walk<kTree, kTokens, k8> walk;
   walk.init(w.stream, w.first_tile * kTileTokens + wave * kTokens, kWaves * kTokens);
   const int steps = ((w.end_tile - w.first_tile) * (kTileTokens / kTokens) - wave + kWaves - 1) / kWaves;
   char* stage_k = lds + wave * kStage;
@@ -239,23 +277,39 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   uint64_t held = 0, held_next = 0;
   uint4 k[kLoads], v[kLoads];
   bool token_there[kLoads];
+  auto find = [&](int step) {
+    if constexpr (k8)
+      walk.find8(a, w.stream, w.hk, step, lane);
+    else
+      walk.find(w.stream, step, lane);
+  };
   auto load = [&](int step) {
-    if (!walk.knows(step)) walk.find(w.stream, step, lane);
+    if (!walk.knows(step)) find(step);
+    if constexpr (k8) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) walk.load8(a, w.stream, w.hk, step, i * 8, lane, k[i], v[i]);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) token_there[i] = walk.load(a, w.stream, w.hk, step, i * 4, lane, k[i], v[i]);
     if (kTree) held_next = walk.held(step, lane);
   };
-  if (steps > 0) walk.find(w.stream, 0, lane);
+  if (steps > 0) find(0);
   st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
   if (steps > 0) load(0);
   st.ready(a.q_sign);
   for (int step = 0; step < steps; ++step) {
     held = held_next;
+    if constexpr (k8) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = i * 4 + (lane >> 4);
-      st16(stage_k + k_place(at, lane & 15), k[i]);
-      st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
+      for (int i = 0; i < kLoads; ++i) walk.put8(step, i * 8, lane, k[i], v[i], stage_k, stage_v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = i * 4 + (lane >> 4);
+        st16(stage_k + k_place(at, lane & 15), k[i]);
+        st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
+      }
     }
     lds_in_order();
     if (step + 1 < steps) load(step + 1);
@@ -479,7 +533,7 @@ Plan plan_of(const quest_cache& c, int total_tokens, bool tree, int k_pages) {
 int units_of(const Plan& p) { return std::max(p.row_tiles, p.most_units); }
 size_t unit_bytes(int rows, const quest_cache& c) { return (size_t)kv_heads(c) * rows * (kHeadDim + 2) * sizeof(float); }
 
-template <bool kTree, bool kExact>
+template <bool kTree, bool kExact, bool k8 = false>
 int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32_t* topk, void* workspace, size_t bytes,
                 const char* who, hipStream_t s) {
   Plan p = plan_of(c, total_tokens, kTree, topk != nullptr ? a.k_pages : 0);
@@ -494,9 +548,9 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   a.part_ml = a.part_acc + (size_t)units_of(p) * a.kv_heads * p.rows * kHeadDim;
   const dim3 grid((unsigned)(units_of(p) * a.kv_heads)), block((p.rows == kSharedRows ? kSharedWaves : kWaves) * kWave);
   if (p.rows == kFewRows)
-    hipLaunchKernelGGL((few_rows_kernel<kTree, !kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+    hipLaunchKernelGGL((few_rows_kernel<kTree, !kExact, k8>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   else
-    hipLaunchKernelGGL((shared_rows_kernel<kTree, kExact>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
+    hipLaunchKernelGGL((shared_rows_kernel<kTree, kExact, k8>), grid, block, 0, s, a, a.cu, a.seq_lens, c.page_table, topk, a.mask);
   const int r = check_launch(who);
   if (r != QUEST_OK || p.most_units == 0) return r;
   const unsigned tiles = (unsigned)(p.row_tiles * a.kv_heads);
@@ -518,6 +572,7 @@ RowsArgs rows_args(const quest_cache& c, const PackedTokens& p, const void* q, i
   a.q = (const char*)q;
   a.k_pool = (const char*)c.k_pool;
   a.v_pool = (const char*)c.v_pool;
+  a.scales = e4m3_pages(c) ? (const float2*)c.scales : nullptr;
   a.cu = p.cu;
   a.seq_lens = c.seq_lens;
   a.out = out;
@@ -560,7 +615,8 @@ bool rows_fit_a_launch(const quest_cache& c, int total_tokens) {
 int launch_prompt(const quest_cache& c, const PackedTokens& p, const void* q, int64_t q_stride, float sm_scale, void* out,
                   int out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, hipStream_t s) {
   RowsArgs a = rows_args(c, p, q, q_stride, sm_scale, out, out_is_fp16, lse);
-  const auto launch = out_is_fp16 ? launch_rows<false, false> : launch_rows<false, true>;
+  const auto launch = e4m3_pages(c) ? (out_is_fp16 ? launch_rows<false, false, true> : launch_rows<false, true, true>)
+                                    : (out_is_fp16 ? launch_rows<false, false> : launch_rows<false, true>);
   return launch(c, a, p.total, nullptr, workspace, workspace_bytes, "quest_prompt_attention", s);
 }
 

@@ -38,6 +38,7 @@
 
 #include "quest_common.h"
 #include "quest_decode_core.h"
+#include "quest_e4m3.h"
 
 namespace quest {
 
@@ -45,6 +46,7 @@ struct RowsArgs {
   const char* q;
   const char* k_pool;
   const char* v_pool;
+  const float2* scales;     // pages of 8 bits
   const int32_t* cu;
   const int32_t* seq_lens;
   void* out;
@@ -479,13 +481,15 @@ struct Stream {
 // is in is looked up for many steps at a time, one page (or part of one, where a page is longer than a step) a lane:
 // lane e of the first step's, then the next step's, ..  The lookups' latency, twice a memory access with a list, is
 // then paid once in 16 to 64 steps, and nothing waits for a lookup behind the keys and values under way.
-template <bool kTree, int kPlaces>
+// k8: pages of 8 bits, whose numbers become fp16 numbers on the way from registers to LDS (prompts only).
+template <bool kTree, int kPlaces, bool k8 = false>
 struct Walk {
   int start, stride;
   int shift;            // log2 of the places a lane looks up: a page, at most a step
   int per_step_log2;    // lanes of a step
   int first_step;       // step of lane 0
   int phys, left;       // this lane's page, and how many of its places (from its first on) hold a token
+  float2 scale;         // k8: of its keys and values
   static constexpr int kLog2 = kPlaces == 64 ? 6 : 5;
 
   __device__ __forceinline__ void init(const Stream<kTree>& s, int start_, int stride_) {
@@ -514,6 +518,31 @@ struct Walk {
       phys = s.table[at >> s.page_shift];
       left = s.limit - at;
     }
+  }
+  __device__ __forceinline__ void find8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int lane) {
+    find(s, step, lane);
+    scale = make_float2(1.f, 1.f);   // (a page without tokens may have any)
+    if (left > 0) scale = a.scales[(size_t)phys * a.kv_heads + hk];
+  }
+  // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15.
+  __device__ __forceinline__ void load8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int eight, int lane, uint4& key,
+                                        uint4& value) const {
+    const int page = __builtin_amdgcn_readlane(phys, ((step - first_step) << per_step_log2) + (eight >> shift));
+    const int at = start + step * stride + eight;
+    const int64_t row = (((int64_t)page * a.kv_heads + hk) << s.page_shift) + (at & ((1 << s.page_shift) - 1));
+    key = ld16(a.k_pool + row * kRowBytes8 + lane * 16);   // eight rows of 128 bytes
+    value = ld16(a.v_pool + row * kRowBytes8 + lane * 16);
+  }
+  // What load8 brought, as fp16 numbers into LDS (k, v: the tile); before another find8.  A value that is not there is zero.
+  __device__ __forceinline__ void put8(int step, int eight, int lane, uint4 key, uint4 value, char* k, char* v) const {
+    const int from = ((step - first_step) << per_step_log2) + (eight >> shift);
+    const float k_scale = from_lane(scale.x, from), v_scale = from_lane(scale.y, from);
+    const int sub = lane >> 3, token = eight + sub, slot = (lane & 7) * 2;
+    if ((eight & ((1 << shift) - 1)) + sub >= __builtin_amdgcn_readlane(left, from)) value = make_uint4(0, 0, 0, 0);
+    st16(k + k_place(token, slot), halves_of(make_uint2(key.x, key.y), k_scale));
+    st16(k + k_place(token, slot + 1), halves_of(make_uint2(key.z, key.w), k_scale));
+    st16(v + v_place(token, slot), halves_of(make_uint2(value.x, value.y), v_scale));
+    st16(v + v_place(token, slot + 1), halves_of(make_uint2(value.z, value.w), v_scale));
   }
   // 16 bytes of the key and of the value of the step's place `four` + lane / 16 (`four`: a multiple of 4).  Returns whether
   // there is a token; if not, the value has to be zeroed when it has arrived: stale slots may hold anything, and

@@ -1,0 +1,297 @@
+"""Attention over pages of 8 bits on the GPU, against 64 bits over the numbers that the pages stand for."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_10774_amd import binding as Q
+from e4m3_util import Packed8
+from packed_util import D, attention64, check, check_prompt
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / math.sqrt(D)
+ROOMS = [0, 1 << 17]
+
+
+def one_query(lens, **kw):
+    return Packed8(lens, [1] * len(lens), spare_rows=0, **kw)
+
+
+def run_decode(p, half, lists=None, scale=SCALE, workspace="full", lse=True):
+    out, l = p.results(half)
+    k_pages = 0 if lists is None else lists.shape[2]
+    n = Q.quest_workspace_bytes(p.cache, k_pages)
+    ws = torch.zeros(max(n, 16) // 4, device=p.dev) if workspace == "full" else workspace
+    Q.quest_sparse_decode(p.cache, p.q.contiguous(), lists, k_pages, scale, out, lse=l if lse else None, workspace=ws)
+    torch.cuda.synchronize()
+    if workspace == "full":                                        # every call leaves the arrival counters at zero
+        assert not bool(ws.view(torch.int32)[:p.B * p.H * 64].any()) or n < p.B * p.H * 256
+    return out, l
+
+
+def check_decode(p, out, lse, half, lists=None, scale=SCALE, what=""):
+    for b in range(p.B):
+        for hk in range(p.Hkv):
+            k, v = p.cached(b, hk)
+            if lists is not None:                                  # a page listed twice counts twice
+                pages = lists[b, hk, :p.table.shape[1]].long()
+                pages = pages[(pages >= 0) & (pages < -(-p.lens[b] // p.S))]
+                j = (pages[:, None] * p.S + torch.arange(p.S, device=p.dev)).flatten()
+                j = j[j < p.lens[b]]
+                k, v = k[j], v[j]
+            sees = torch.ones(p.G, k.shape[0], dtype=torch.bool, device=p.dev)
+            at = slice(hk * p.G, (hk + 1) * p.G)
+            check(out[b, at], lse[b, at], attention64(p.q[b, at].double(), k, v, sees, scale), half, (what, b, hk))
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("heads,kv_heads", [(3, 3), (4, 2)])
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 65, 127, 200, 511, 512, 513, 2047, 2049, 2600, 9001])
+def test_lengths(n, heads, kv_heads, half):
+    for room in ROOMS:
+        p = one_query([n], heads=heads, kv_heads=kv_heads, seed=n, room=room)
+        for ws in ("full", None):
+            check_decode(p, *run_decode(p, half, workspace=ws), half, what=(n, ws))
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (5, 5), (4, 2), (6, 2), (16, 2), (18, 1), (40, 5)])
+def test_ragged_batches_and_groups(heads, kv_heads, S):
+    """Sequences of very different lengths, one of them empty: out 0, lse -inf."""
+    p = one_query([1500, 1, 0, 333, 64, 7000], heads=heads, kv_heads=kv_heads, S=S, seed=S)
+    for half in (True, False):
+        out, lse = run_decode(p, half)
+        check_decode(p, out, lse, half, what=(heads, kv_heads, S))
+        assert bool((out[2] == 0).all()) and bool((lse[2] == -math.inf).all())
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("K", [1, 3, 17, 130, 400])
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (8, 2)])
+def test_lists(S, K, heads, kv_heads):
+    """As the selection leaves them; with holes, ids of pages without tokens, a page twice; nothing at all."""
+    rng = np.random.default_rng(S * K)
+    p = one_query([3000, 30, 777], heads=heads, kv_heads=kv_heads, S=S, seed=K)
+    lists = np.full((3, kv_heads, K), -1, np.int32)
+    for b in range(3):
+        pages = -(-p.lens[b] // S)
+        for h in range(kv_heads):
+            m = min(K, pages)
+            lists[b, h, :m] = np.sort(rng.permutation(pages)[:m])
+    rough = lists.copy()
+    for b in range(3):
+        for h in range(kv_heads):
+            rng.shuffle(rough[b, h])
+            if K >= 3:
+                rough[b, h, K // 2] = -5 if h else 2 ** 31 - 1
+                rough[b, h, 0] = rough[b, h, 1]
+    none = np.full_like(lists, -1)
+    for these in (lists, rough, none):
+        t = torch.from_numpy(these).to(p.dev)
+        for half in (True, False):
+            for ws in ("full", None):
+                check_decode(p, *run_decode(p, half, t, workspace=ws), half, t, what=(S, K, half, ws))
+
+
+@pytest.mark.parametrize("scale", [SCALE, -SCALE, 0.0, 1.0])
+def test_scales_of_the_softmax(scale):
+    for heads, kv_heads in ((2, 2), (6, 2)):
+        p = one_query([700, 33], heads=heads, kv_heads=kv_heads, seed=5, spread=2.0)
+        for half in (True, False):
+            check_decode(p, *run_decode(p, half, scale=scale), half, scale=scale, what=scale)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (8, 1)])
+@pytest.mark.parametrize("down", [False, True])
+def test_logits_that_rise_and_fall(heads, kv_heads, down):
+    """The base of the weights moves at every step of a wave, or never; pages differ in scale by up to 2^20."""
+    p = one_query([1000], heads=heads, kv_heads=kv_heads, seed=7)
+    t = torch.arange(1000, device=p.dev)
+    phys = p.table[0].long()[t // p.S]
+    order = (1000 - t if down else t)
+    ramp = (order.float() / 1000)[:, None, None] * torch.ones(1, kv_heads, D, device=p.dev)
+    codes = (ramp * 256).to(torch.float8_e4m3fn)
+    p.k_pool.view(torch.uint8)[phys, :, t % p.S] = codes.view(torch.uint8)
+    p.scales[phys, :, 0] = torch.exp2(torch.floor(t.float() / 16) % 3 - 9)[:, None]
+    p.scales[phys, :, 1] = torch.exp2((torch.floor(t.float() / 16) * 7) % 21 - 15)[:, None]
+    p.q.copy_(p.q.abs() * 8)
+    for half in (True, False):
+        check_decode(p, *run_decode(p, half), half, what=down)
+
+
+def test_more_sequences_than_lanes():
+    rng = np.random.default_rng(9)
+    for heads, kv_heads in ((1, 1), (2, 1), (8, 8)):
+        lens = [int(x) for x in rng.integers(0, 200, 140)]
+        lens[100] = 20000
+        p = one_query(lens, heads=heads, kv_heads=kv_heads, seed=9)
+        for half in (True, False):
+            check_decode(p, *run_decode(p, half), half, what=(heads, half))
+
+
+@pytest.mark.parametrize("seed", range(20))
+def test_random_shapes(seed):
+    rng = np.random.default_rng(seed)
+    B, S = int(rng.integers(1, 9)), int(rng.choice([8, 16, 32, 64]))
+    kv_heads = int(rng.integers(1, 9))
+    heads = kv_heads * int(rng.choice([1, 1, 2, 4, 8, 9]))
+    lens = [int(np.exp(rng.uniform(0, math.log(20000)))) for _ in range(B)]
+    p = one_query(lens, heads=heads, kv_heads=kv_heads, S=S, seed=seed, room=ROOMS[seed % 2])
+    half = seed % 3 > 0
+    first = run_decode(p, half)
+    check_decode(p, *first, half, what=seed)
+    again = run_decode(p, half)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])     # whoever arrives last
+
+
+def test_workspaces_of_any_size():
+    """Used as far as they go; nothing is written behind them."""
+    for heads, kv_heads in ((4, 4), (8, 2)):
+        p = one_query([6000, 3500], heads=heads, kv_heads=kv_heads, seed=4)
+        full = Q.quest_workspace_bytes(p.cache, 0)
+        for size in (0, 256, p.B * heads * 256, p.B * heads * 256 + 20000, full // 2, full):
+            ws = torch.zeros(full // 4 + 64, device=p.dev)
+            ws[size // 4:] = 5.0
+            out, lse = run_decode(p, False, workspace=ws[:size // 4])
+            check_decode(p, out, lse, False, what=size)
+            assert bool((ws[size // 4:] == 5).all())
+
+
+def test_one_workspace_for_both_kinds_of_pages():
+    """Counters lie at the same places, so calls on an fp16 cache and on one of 8 bits of the same shape take turns on a buffer."""
+    from packed_util import Packed
+    p = one_query([5000, 900], heads=8, kv_heads=2, seed=3)
+    h = Packed([5000, 900], [1, 1], heads=8, kv_heads=2, seed=3, spare_rows=0)
+    size = max(Q.quest_workspace_bytes(p.cache, 0), Q.quest_workspace_bytes(h.cache, 0))
+    ws = torch.zeros(size // 4, device=p.dev)
+    alone = []
+    for turn in range(3):
+        out, lse = run_decode(p, False, workspace=ws)
+        check_decode(p, out, lse, False)
+        o, l = h.results(False)
+        Q.quest_sparse_decode(h.cache, h.q.contiguous(), None, 0, SCALE, o, lse=l, workspace=ws)
+        check_decode(h, o, l, False)
+        alone.append((out, o))
+    assert all(torch.equal(a, alone[0][0]) and torch.equal(b, alone[0][1]) for a, b in alone)
+
+
+def test_without_lse_and_with_fences():
+    p = one_query([4000, 77], heads=6, kv_heads=2, seed=2)
+    want = run_decode(p, True)[0]
+    assert torch.equal(run_decode(p, True, lse=False)[0], want)
+    p.describe(flags=Q.QUEST_FLAG_DEVICE_FENCES)
+    assert torch.equal(run_decode(p, True)[0], want)
+
+
+@pytest.mark.parametrize("S,pages,K,heads,kv_heads", [(16, 130, 20, 4, 4), (16, 600, 128, 8, 2), (8, 17000, 300, 2, 1), (64, 40, 64, 3, 3)])
+def test_selection_and_steps(S, pages, K, heads, kv_heads):
+    """quest_select_decode and quest_decode_step select what quest_topk does from the same scores, and attend over it."""
+    p = one_query([pages * S - 3, pages * S // 2], heads=heads, kv_heads=kv_heads, S=S, seed=K)
+    half = one_query([pages * S - 3, pages * S // 2], heads=heads, kv_heads=kv_heads, S=S, seed=K)
+    p.meta.copy_(torch.randn_like(p.meta).sort(2).values)
+    width = p.table.shape[1]
+    q = p.q.contiguous()
+    scores, idx, eff = torch.zeros(2, kv_heads, width, device=p.dev), torch.zeros(2, kv_heads, K, device=p.dev, dtype=torch.int32), torch.zeros(2, device=p.dev, dtype=torch.int32)
+    Q.quest_estimate(p.cache, q, scores)
+    Q.quest_topk(p.cache, scores, K, idx, eff)
+    assert min(int(x) for x in eff) == min(K, pages // 2 + (pages * S // 2 % S > 0))
+    want = run_decode(p, False, idx)
+    check_decode(p, *want, False, idx)
+    for ws in (torch.zeros(Q.quest_step_workspace_bytes(p.cache, K) // 4, device=p.dev), None):
+        for call in ("select", "step"):
+            i2, e2, s2 = torch.full_like(idx, -7), torch.zeros_like(eff), torch.zeros_like(scores)
+            out, lse = p.results(False)
+            if call == "select":
+                Q.quest_select_decode(p.cache, q, scores, K, SCALE, i2, out, k_eff=e2, lse=lse, workspace=ws)
+            else:
+                Q.quest_decode_step(p.cache, None, None, False, q, K, SCALE, s2, i2, out, ws, k_eff=e2, lse=lse)
+                for b in range(2):
+                    n = -(-p.lens[b] // S)
+                    assert torch.equal(s2[b, :, :n], scores[b, :, :n])
+            assert torch.equal(i2, idx) and torch.equal(e2, eff)
+            check_decode(p, out, lse, False, idx)
+            if ws is not None:
+                assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+# ---- prompts
+
+def run_prompt(p, half, scale=SCALE, workspace="full"):
+    out, lse = p.results(half)
+    Q.quest_prompt_attention(p.cache, p.q, p.cu, scale, out, lse=lse, workspace=p.workspace() if workspace == "full" else None)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("room", ROOMS)
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257, 515, 1100])
+def test_whole_prompts(n, room, half):
+    p = Packed8([n], [n], heads=3, kv_heads=3, seed=n, room=room)
+    for ws in ("full", None):
+        check_prompt(p, *run_prompt(p, half, workspace=ws), half, SCALE, (n, ws))
+
+
+@pytest.mark.parametrize("room", ROOMS)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 4), (4, 1), (6, 2), (10, 2), (16, 2), (18, 1), (40, 1)])
+def test_prompt_groups_ragged(heads, kv_heads, room):
+    p = Packed8([150, 40, 333, 1, 70], [150, 0, 37, 1, 65], heads=heads, kv_heads=kv_heads, seed=heads, room=room)
+    for half in (True, False):
+        check_prompt(p, *run_prompt(p, half), half, SCALE, (heads, kv_heads, half))
+
+
+@pytest.mark.parametrize("room", ROOMS)
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+def test_prompt_page_sizes_and_strides(S, room):
+    for stride in (0, 8, 3 * D):
+        p = Packed8([301, 64, 7, 1210], [301, 20, 7, 100], heads=8, kv_heads=2, S=S, seed=S, stride=stride, room=room)
+        check_prompt(p, *run_prompt(p, True), True, SCALE, (S, stride))
+
+
+@pytest.mark.parametrize("new,past", [(1, 5000), (5, 3001), (64, 4100), (300, 2000)])
+def test_prompt_parts_behind_long_contexts(new, past):
+    p = Packed8([past + new, past // 3 + 1], [new, 1], heads=8, kv_heads=2, seed=new)
+    for half in (True, False):
+        for ws in ("full", None):
+            check_prompt(p, *run_prompt(p, half, workspace=ws), half, SCALE, (new, past, half, ws))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_prompts_in_splits(seed):
+    rng = np.random.default_rng(seed)
+    B, S = int(rng.integers(1, 5)), int(rng.choice([8, 16, 32, 64]))
+    kv_heads = int(rng.integers(1, 4))
+    heads = kv_heads * int(rng.choice([1, 2, 3, 4, 7]))
+    new = [int(rng.integers(1, 700)) for _ in range(B)]
+    lens = [n + int(rng.choice([0, rng.integers(0, 300), rng.integers(0, 5000)])) for n in new]
+    p = Packed8(lens, new, heads=heads, kv_heads=kv_heads, S=S, seed=seed, room=ROOMS[seed % 2])
+    half = seed % 3 > 0
+    whole = run_prompt(p, half)
+    check_prompt(p, *whole, half, SCALE, seed)
+    again = run_prompt(p, half)
+    assert torch.equal(whole[0], again[0]) and torch.equal(whole[1], again[1])
+
+
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("kv_heads", [40, 8])
+def test_prompts_that_fill_the_card(kv_heads, half):
+    p = Packed8([700, 950, 40], [700, 333, 40], heads=40, kv_heads=kv_heads, seed=kv_heads)
+    check_prompt(p, *run_prompt(p, half), half, SCALE)
+
+
+@pytest.mark.parametrize("scale", [-SCALE, 0.0, 1.0])
+def test_prompt_scales(scale):
+    for room in ROOMS:
+        p = Packed8([190], [190], heads=2, kv_heads=2, seed=5, spread=2.0, room=room)
+        for half in (True, False):
+            check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
+
+
+def test_prompt_lengths_past_the_page_table_row():
+    """A sequence is as long as its row at most; one that is shorter than its new tokens spoils nothing else."""
+    p = Packed8([200, 300], [70, 80], heads=4, kv_heads=2, seed=3)
+    want = run_prompt(p, False)
+    p.seq_lens[0] = 60
+    out, lse = run_prompt(p, False)
+    assert torch.equal(out[p.rows(1)], want[0][p.rows(1)]) and torch.equal(lse[p.rows(1)], want[1][p.rows(1)])

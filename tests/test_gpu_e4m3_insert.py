@@ -1,0 +1,195 @@
+"""Insertion into pages of 8 bits on the GPU, bit for bit against the definition slot by slot."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_10774_amd import binding as Q
+from e4m3_util import Packed8, Pages, VALUES, nearest
+from packed_util import D, Packed
+
+pytestmark = pytest.mark.gpu
+HALVES = np.arange(65536, dtype=np.uint16).view(np.float16)
+
+
+def pool8(N, Hkv, S, dev="cuda:0"):
+    """Pools whose slots and scales nobody has written."""
+    return dict(k_pool=torch.full((N, Hkv, S, D), 0x7f, dtype=torch.uint8, device=dev),
+                v_pool=torch.full((N, Hkv, S, D), 0x7f, dtype=torch.uint8, device=dev),
+                meta=torch.zeros(Hkv, N, 2, D, device=dev, dtype=torch.float16),
+                scales=torch.full((N, Hkv, 2), math.nan, device=dev))
+
+
+@pytest.mark.parametrize("e", range(-15, 9))
+def test_every_fp16_number_at_every_scale(e):
+    """All finite fp16 numbers that a scale of 2^e holds, in pages that need it: the nearest e4m3 number, ties to even; and all of
+    them come back from attention over one token as they are stored."""
+    most = min(448.0 * 2.0 ** e, 65504.0)
+    x = HALVES[np.isfinite(HALVES) & (np.abs(HALVES.astype(np.float64)) <= most)]
+    tokens = -(-len(x) // (D - 1))
+    rows = np.zeros((tokens, D), np.float16)
+    rows[:, 1:].reshape(-1)[:len(x)] = x
+    rows[:, 0] = min(448.0 * 2.0 ** e, 61440.0)                    # what needs the scale
+    S = 8
+    pages = -(-tokens // S)
+    p = pool8(pages, 1, S)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda:0")[None]
+    cache = Q.Cache(p["k_pool"], p["v_pool"], p["meta"], table, torch.tensor([tokens], dtype=torch.int32, device="cuda:0"),
+                    scales=p["scales"])
+    kv = torch.from_numpy(rows).to("cuda:0")[:, None]
+    Q.quest_append_tokens(cache, kv, (-kv).contiguous(), torch.tensor([0, tokens], dtype=torch.int32, device="cuda:0"))
+    assert bool((p["scales"] == 2.0 ** e).all())
+    for pool, sign in ((p["k_pool"], 1.0), (p["v_pool"], -1.0)):
+        codes = pool.reshape(-1, D)[:tokens].cpu().numpy()
+        want = nearest(np.clip(sign * rows.astype(np.float64), -61440.0, 61440.0) * 2.0 ** -e)
+        assert np.array_equal(codes, want)
+    # one token a sequence, every query group size's kernel
+    for heads in (1, 2):
+        out = torch.empty(tokens, heads, D, device="cuda:0")
+        slot = torch.arange(tokens, dtype=torch.int32, device="cuda:0")
+        v = p["v_pool"].reshape(-1, 1, D)[:tokens, :, None].expand(-1, -1, S, -1).contiguous()
+        scales = p["scales"].reshape(-1, 1, 1, 2).expand(-1, S, 1, 2).reshape(-1, 1, 2)[:tokens].contiguous()
+        cache1 = Q.Cache(v, v, p["meta"], slot[:, None], torch.ones_like(slot), num_heads=heads, scales=scales)
+        Q.quest_sparse_decode(cache1, torch.zeros(tokens, heads, D, device="cuda:0", dtype=torch.float16), None, 0, 1.0, out)
+        want = VALUES[p["v_pool"].reshape(-1, D)[:tokens].cpu().numpy()] * 2.0 ** e
+        assert np.array_equal(out.cpu().numpy().astype(np.float64), np.repeat(want[:, None], heads, 1))
+
+
+class Oracle:
+    """The cache's pools slot by slot, from what they hold before a call."""
+
+    def __init__(self, p):
+        scales = p.scales.nan_to_num(1.0).cpu().numpy()
+        self.k, self.v = (Pages(pool.view(torch.uint8).cpu().numpy(), scales[..., i]) for i, pool in enumerate((p.k_pool, p.v_pool)))
+
+    def insert(self, p, rows=None):
+        k, v = p.k_new.double().cpu().numpy(), p.v_new.double().cpu().numpy()
+        touched = set()
+        for b in range(p.B):
+            first = p.lens[b] - p.new[b]
+            at = np.arange(p.cu_np[b], p.cu_np[b + 1]) if rows is None else rows[p.cu_np[b]:p.cu_np[b + 1]]
+            for page in range(first // p.S, -(-p.lens[b] // p.S)):
+                lo, hi = max(first, page * p.S), min(p.lens[b], (page + 1) * p.S)
+                if lo >= hi:
+                    continue
+                phys = int(p.table_np[b, page])
+                touched.add(phys)
+                for h in range(p.Hkv):
+                    self.k.insert(phys, h, lo - page * p.S, k[at[lo - first:hi - first], h])
+                    self.v.insert(phys, h, lo - page * p.S, v[at[lo - first:hi - first], h])
+        return sorted(touched)
+
+    def check(self, p, touched):
+        for i, (pool, mine) in enumerate(((p.k_pool, self.k), (p.v_pool, self.v))):
+            assert np.array_equal(pool.view(torch.uint8).cpu().numpy(), mine.codes), "codes"
+            assert np.array_equal(p.scales[touched, :, i].cpu().numpy(), 2.0 ** mine.e[touched]), "scales"
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (6, 3), (5, 5)])
+def test_ragged_insertion(S, heads, kv_heads):
+    """Whole pages, ends and beginnings of pages, one token, none; strided rows; slots that get no token and pages of others stay."""
+    for stride in (0, 8, 2 * D):
+        p = Packed8([150, 40, 3 * S, 1, 70, S - 1, 2 * S + 3], [150, 0, S, 1, 65, 2, 2], heads=heads, kv_heads=kv_heads, S=S, seed=S,
+                    stride=stride)
+        half = Packed([150, 40, 3 * S, 1, 70, S - 1, 2 * S + 3], [150, 0, S, 1, 65, 2, 2], heads=heads, kv_heads=kv_heads, S=S, seed=S,
+                      stride=stride)
+        o = Oracle(p)
+        Q.quest_append_tokens(p.cache, p.k_new, p.v_new, p.cu)
+        Q.quest_append_tokens(half.cache, half.k_new, half.v_new, half.cu)
+        o.check(p, o.insert(p))
+        assert torch.equal(p.meta.view(torch.int16), half.meta.view(torch.int16))          # of the keys before they are rounded
+
+
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+def test_scales_that_grow_token_by_token(S):
+    """One token a call, each larger than the last by up to 2^12, and some smaller: what the page holds is rounded again, down into
+    the subnormals and to zero."""
+    rng = np.random.default_rng(S)
+    p = Packed8([0, 0], [1, 1], heads=2, kv_heads=2, S=S, seed=S, room=128, cached=False, spare_rows=0)
+    N = 128 // S * 2
+    p.table_np = rng.permutation(N).astype(np.int32).reshape(2, -1)
+    p.__dict__.update(table=torch.from_numpy(p.table_np).to(p.dev), **pool8(N, 2, S))
+    p.describe()
+    o, touched = Oracle(p), set()
+    for step in range(70):
+        p.lens = [step + 1, step + 1]
+        p.seq_lens.fill_(step + 1)
+        size = np.exp2(rng.uniform(-14, 14, (2, 2, 1))) if step % 5 else np.array([0.0, 2.0 ** -24, 60000.0, 1.0]).reshape(2, 2, 1)
+        for t in (p.k_new, p.v_new):
+            t.copy_(torch.from_numpy((rng.uniform(-1, 1, (2, 2, D)) * size).astype(np.float16)))
+        Q.quest_append_tokens(p.cache, p.k_new, p.v_new, p.cu)
+        touched.update(o.insert(p))
+    o.check(p, sorted(touched))
+
+
+def test_picked_rows_and_repeats():
+    """Accepted drafts: rows anywhere in the packed arrays, one of them twice; the same call again changes nothing."""
+    p = Packed8([300, 77, 64], [7, 3, 5], heads=4, kv_heads=2, seed=1, spare_rows=0)
+    given = torch.randn(40, 2, D, device=p.dev).half()
+    rows = np.random.default_rng(0).integers(0, 40, 15).astype(np.int32)
+    rows[3] = rows[11] = 39
+    o = Oracle(p)
+    values = (given * 3).contiguous()
+    p.k_new, p.v_new = given, values
+    for _ in range(2):
+        Q.quest_append_tokens(p.cache, given, values, p.cu, rows=torch.from_numpy(rows).to(p.dev))
+    touched = o.insert(p, rows)
+    o.check(p, touched)
+
+
+def test_numbers_that_are_not_finite():
+    """NaN stays NaN; infinities count as the largest number.  Other pages and heads are as without them."""
+    p = Packed8([33], [33], heads=2, kv_heads=2, seed=4, spare_rows=0)
+    p.k_new[5, 1, 7], p.k_new[20, 0, 9], p.v_new[21, 0, 3] = math.nan, math.inf, -math.inf
+    clean = Packed8([33], [33], heads=2, kv_heads=2, seed=4, spare_rows=0)
+    for x in (p, clean):
+        Q.quest_append_tokens(x.cache, x.k_new, x.v_new, x.cu)
+    codes = p.k_pool.view(torch.uint8)
+    at = lambda t: (int(p.table_np[0, t // 16]), t % 16)                     # noqa: E731
+    page, slot = at(5)
+    assert int(codes[page, 1, slot, 7]) & 0x7f == 0x7f
+    page, slot = at(20)
+    assert VALUES[int(codes[page, 0, slot, 9])] * float(p.scales[page, 0, 0]) == 61440.0
+    page, slot = at(21)
+    assert VALUES[int(p.v_pool.view(torch.uint8)[page, 0, slot, 3])] * float(p.scales[page, 0, 1]) == -61440.0
+    for h, pages in ((0, [0, 2]), (1, [1, 2])):
+        phys = [int(p.table_np[0, i]) for i in pages]
+        assert torch.equal(codes[phys, h], clean.k_pool.view(torch.uint8)[phys, h]) and torch.equal(p.scales[phys, h], clean.scales[phys, h])
+
+
+def test_lengths_that_do_not_fit():
+    """A length past the page-table row writes nothing behind it; one below the new tokens' number leaves that sequence alone."""
+    p = Packed8([64, 20, 48], [30, 20, 9], heads=2, kv_heads=1, seed=8)
+    width = p.table.shape[1]
+    long = (width + 2) * p.S
+    p.seq_lens.copy_(torch.tensor([64, 19, long], dtype=torch.int32))
+    before = [t.view(torch.uint8).clone() for t in (p.k_pool, p.v_pool)]
+    Q.quest_append_tokens(p.cache, p.k_new, p.v_new, p.cu)
+    torch.cuda.synchronize()
+    changed = {int(x) for x in (before[0] != p.k_pool.view(torch.uint8)).flatten(1).any(1).nonzero()}
+    assert changed <= {int(x) for x in p.table_np[0]}
+
+
+def test_pools_beyond_32_bits():
+    """Offsets past 4 GiB of codes."""
+    N, Hkv, S = 8400, 64, 64
+    dev = "cuda:0"
+    k, v = (torch.zeros(N, Hkv, S, D, dtype=torch.uint8, device=dev) for _ in range(2))
+    assert k.nbytes > 2 ** 32
+    table = torch.tensor([[N - 1, N - 2]], dtype=torch.int32, device=dev)
+    cache = Q.Cache(k, v, torch.zeros(Hkv, N, 2, D, device=dev, dtype=torch.float16), table, torch.tensor([S + 5], dtype=torch.int32, device=dev),
+                    scales=torch.ones(N, Hkv, 2, device=dev))
+    x = torch.randn(S + 5, Hkv, D, device=dev).half()
+    cu = torch.tensor([0, S + 5], dtype=torch.int32, device=dev)
+    Q.quest_append_tokens(cache, x, x, cu)
+    out = torch.empty(1, Hkv, D, device=dev)
+    Q.quest_sparse_decode(cache, torch.zeros(1, Hkv, D, device=dev, dtype=torch.float16), None, 0, 1.0, out)
+    scale = cache.scales[[N - 1, N - 2], :, 1].double()
+    rows = torch.from_numpy(VALUES).to(dev)[v[[N - 1, N - 2]].long()] * scale[..., None, None]
+    want = torch.cat([rows[0], rows[1, :, :5]], 1).mean(1)
+    assert bool(((rows[0] - x[:S].double().transpose(0, 1)).abs() <= 2.0 ** -4 * x[:S].double().transpose(0, 1).abs() + 2.0 ** -10 * scale[0][:, None, None]).all())
+    size = torch.cat([rows[0], rows[1, :, :5]], 1).abs().mean(1)   # all weights are 1: 69 additions, each off by 2^-24 of a part of the sum
+    assert bool(((out[0].double() - want).abs() <= 69 * 2.0 ** -24 * size + 2.0 ** -24).all())
+    assert int((k != 0).flatten(1).any(1).sum()) == 2
