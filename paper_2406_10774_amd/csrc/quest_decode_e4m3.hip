@@ -1,12 +1,12 @@
 // Attention of one query a sequence over pages of 8 bits: listed pages, or all.
 //
 // Bound by memory: a token's key and value of a head are 256 bytes, read once.  The tokens of a sequence are cut into tiles of
-// 64, of which each of a work-group's four waves has 16; a lane looks up the page of eight of them for 32 tiles ahead, so that nothing
-// waits for a lookup behind keys and values under way.  Four steps of 4 KiB are on their way to a wave at a time.
+// 64 (128 where query heads share a KV head), a quarter for each of a work-group's four waves; a lane looks up the page of eight tokens, ahead of
+// the keys and values, which are on their way to a wave 16 KiB at a time, and go on across the lookups.
 //
-// The host knows no lengths, so every work-group works out for itself how the tokens of all sequences are cut: the length of a
-// split is what gives as many units (splits of a sequence) as the host asks for, however ragged the batch.  The split of a
-// (sequence, KV head) that arrives last joins them (quest_team.h).
+// The host knows no lengths: the tiles of all sequences are one line that is cut into equal shares, a work-group each, however ragged
+// the batch.  A share that ends inside a sequence leaves a partial result; the share of a (sequence, KV head) that arrives last joins
+// them (quest_team.h).
 //
 // One query head per KV head: the vector unit.  A lane has 16 channels of every eighth token; products of pairs in fp16, which e4m3
 // numbers times their scale are exactly, summed in fp32.  Weights are relative to a base that moves when a logit passes it by
@@ -26,75 +26,102 @@ namespace quest {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kSteps = 4;                // steps under way
-constexpr int kWalkSteps = 32;           // looked up at a time: two lanes a step
-constexpr int kMostParts = 64;           // splits of a sequence, about
-constexpr int kTileTokens8 = 64;
+constexpr int kMostParts = 64;           // shares of a sequence, about
 
 struct DecodeArgs : AttnArgs {
   const float2* scales;
   const int32_t* topk;
   int k_pages, listed;    // entries of a list, and how many of them count
-  int most_units;         // over all sequences; 0: one a sequence
+  int shares;             // of the line of all sequences' tiles; 0: one work-group a sequence
 };
 
-// A sequence's part: tiles [first_tile, end_tile).
-struct Unit {
-  int b, seq_len, first_tile, end_tile;
-  int part, parts;        // which of the sequence's parts, of how many
-};
+// The tiles of all sequences, one after the other, are one line that is cut into shares of `length` tiles.  A sequence has a tile at
+// least.
+struct Line {
+  int length;
+  int b, seq_len, first, tiles;   // the sequence that the share begins in: its first tile on the line, and how many it has
 
-__device__ __forceinline__ int tiles_of(const DecodeArgs& a, int seq_len) {
-  const int tokens = a.topk != nullptr ? a.listed << a.page_shift : min(max(seq_len, 0), a.max_pages << a.page_shift);
-  return (tokens + kTileTokens8 - 1) / kTileTokens8;
-}
-__device__ __forceinline__ float whole_sum(float v, int lane) {
-  return as_f((uint32_t)__builtin_amdgcn_readlane((int)as_u(up_to_lane(v, lane)), kWave - 1));
-}
-__device__ __forceinline__ bool find_unit(Unit& u, const DecodeArgs& a, int unit, int lane) {
-  int chunk = INT32_MAX;
-  int tiles = 0, seq_len = 0;
-  auto read = [&](int base) {
-    seq_len = a.seq_lens[min(base + lane, a.batch - 1)];
-    tiles = base + lane < a.batch ? tiles_of(a, seq_len) : 0;
-  };
-  if (a.most_units > 0) {
-    float sum = 0.f;
-    int longest = 0;
-    for (int base = 0; base < a.batch; base += kWave) {
-      read(base);
-      sum += whole_sum((float)tiles, lane);
-      longest = max(longest, largest_of_wave(tiles));
-    }
-    // With this chunk the units are at most sum / chunk + batch (a ten-thousandth covers the roundings).
-    const float even = fminf(sum / (float)(a.most_units - a.batch) * 1.0001f, 1e9f);
-    chunk = max((int)even + 1, (longest + kMostParts - 1) / kMostParts);
+  template <int kTile>
+  __device__ __forceinline__ static int tiles_of(const DecodeArgs& a, int seq_len) {
+    const int tokens = a.topk != nullptr ? a.listed << a.page_shift : min(max(seq_len, 0), a.max_pages << a.page_shift);
+    return max((tokens + kTile - 1) / kTile, 1);
   }
-  int before = 0;
-  for (int base = 0; base < a.batch; base += kWave) {
-    if (a.batch > kWave || a.most_units == 0) read(base);
-    const int parts = base + lane < a.batch ? max(1, (int)(((int64_t)tiles + chunk - 1) / chunk)) : 0;
-    const int end = up_to_lane(parts, lane) + before;
-    const unsigned long long behind = __ballot(end > unit);
-    if (behind != 0) {
-      const int at = __builtin_ctzll(behind);
-      u.b = base + at;
-      u.seq_len = min(max(__builtin_amdgcn_readlane(seq_len, at), 0), a.max_pages << a.page_shift);
-      u.parts = __builtin_amdgcn_readlane(parts, at);
-      u.part = unit - (__builtin_amdgcn_readlane(end, at) - u.parts);
-      const int all = __builtin_amdgcn_readlane(tiles, at);
-      u.first_tile = u.part * (u.parts > 1 ? chunk : 0);
-      u.end_tile = u.part + 1 < u.parts ? u.first_tile + chunk : all;
+  template <int kTile>
+  __device__ __forceinline__ void at(const DecodeArgs& a, int sequence) {
+    b = sequence;
+    seq_len = a.seq_lens[b];
+    tiles = tiles_of<kTile>(a, seq_len);
+  }
+  // Where share `share` begins; false: behind the line's end.
+  template <int kTile>
+  __device__ __forceinline__ bool find(const DecodeArgs& a, int share, int lane) {
+    if (a.shares == 0) {
+      if (share >= a.batch) return false;
+      length = INT32_MAX;
+      first = 0;
+      at<kTile>(a, share);
       return true;
     }
-    before = __builtin_amdgcn_readlane(end, kWave - 1);
+    if (a.batch == 1) {
+      at<kTile>(a, 0);
+      first = 0;
+      length = share_length(a, tiles, tiles);
+      return (int64_t)share * length < tiles;
+    }
+    int mine = 0, total = 0, longest = 0;
+    auto read = [&](int base) {
+      seq_len = a.seq_lens[min(base + lane, a.batch - 1)];
+      mine = base + lane < a.batch ? tiles_of<kTile>(a, seq_len) : 0;
+    };
+    for (int base = 0; base < a.batch; base += kWave) {
+      read(base);
+      total += __builtin_amdgcn_readlane(up_to_lane(mine, lane), kWave - 1);
+      longest = max(longest, largest_of_wave(mine));
+    }
+    length = share_length(a, total, longest);
+    const int64_t begin = (int64_t)share * length;
+    if (begin >= total) return false;
+    first = 0;
+    for (int base = 0; base < a.batch; base += kWave) {
+      if (a.batch > kWave) read(base);
+      const int end = up_to_lane(mine, lane) + first;
+      const unsigned long long behind = __ballot(end > begin);
+      if (behind != 0) {
+        const int l = __builtin_ctzll(behind);
+        b = base + l;
+        seq_len = __builtin_amdgcn_readlane(seq_len, l);
+        tiles = __builtin_amdgcn_readlane(mine, l);
+        first = __builtin_amdgcn_readlane(end, l) - tiles;
+        return true;
+      }
+      first = __builtin_amdgcn_readlane(end, kWave - 1);
+    }
+    return false;
   }
-  return false;
+  __device__ __forceinline__ static int share_length(const DecodeArgs& a, int total, int longest) {
+    return max((int)(((int64_t)total + a.shares - 1) / a.shares), (longest + kMostParts - 1) / kMostParts);
+  }
+};
+
+// A buffer of the first `bytes` of a block of eight tokens: what lies behind them is not read, and zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* pool, uint32_t block, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool) + (size_t)block * (8 * kRowBytes8), 0, bytes, 0x00020000);
 }
+__device__ __forceinline__ uint4 row16(__amdgpu_buffer_rsrc_t rows, int lane) {
+  const auto v = __builtin_amdgcn_raw_buffer_load_b128(rows, lane * 16, 0, 2);   // (non-temporal)
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// Where the eights of tokens of a wave's steps lie, kEights lanes a step.
+struct Places {
+  int block, bytes;     // bytes: of the tokens that there are, 0 to 1024
+  float2 scale;
+};
 
 // One query head: lane l has channels 16 (l % 8) ..+15 of tokens l / 8 of every eight.
 struct OneHead {
   static constexpr int kSlots = 1, kStride = kHeadDim;
+  static constexpr int kEights = 2, kRing = 4;   // of a step; steps under way
   static constexpr float kMove = 8.f;
   uint32_t q[8];
   float m, l, limit, acc[16];   // limit: m + kMove, -3e38 while no token has counted
@@ -110,12 +137,6 @@ struct OneHead {
     l = 0.f;
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-  }
-  __device__ __forceinline__ static void load(Regs& r, const char* k, const char* v, size_t first, size_t second, int lane) {
-    r.k[0] = ld16_stream(k + first + lane * 16);
-    r.k[1] = ld16_stream(k + second + lane * 16);
-    r.v[0] = ld16_stream(v + first + lane * 16);
-    r.v[1] = ld16_stream(v + second + lane * 16);
   }
   __device__ __forceinline__ float logit(uint4 k, float scale) const {
     const uint4 a = halves_of(make_uint2(k.x, k.y), scale), b = halves_of(make_uint2(k.z, k.w), scale);
@@ -141,16 +162,14 @@ struct OneHead {
       acc[4 * i + 3] = __builtin_fmaf(p, b[1], acc[4 * i + 3]);
     }
   }
-  // left: tokens of the two eights that there are (anything from below zero to above eight).
-  __device__ __forceinline__ void fold(Regs& r, const int (&left)[2], const float2 (&scale)[2], float scale_log2, int lane) {
-    float z[2];
+  __device__ __forceinline__ void fold(const Regs& r, const Places& p, int step, float scale_log2, int lane) {
+    float z[2], v_scale[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      z[i] = logit(r.k[i], scale[i].x) * scale_log2;
-      if (left[i] < 8 && (lane >> 3) >= left[i]) {   // stale slots contribute nothing, whatever they hold
-        z[i] = -INFINITY;
-        r.v[i] = make_uint4(0, 0, 0, 0);
-      }
+      z[i] = logit(r.k[i], from_lane(p.scale.x, 2 * step + i)) * scale_log2;
+      v_scale[i] = from_lane(p.scale.y, 2 * step + i);
+      const int bytes = __builtin_amdgcn_readlane(p.bytes, 2 * step + i);
+      if (bytes < 1024 && lane * 16 >= bytes) z[i] = -INFINITY;   // stale slots contribute nothing
     }
     const float top = fmaxf(z[0], z[1]);
     const bool move = top > limit;
@@ -165,257 +184,466 @@ struct OneHead {
     }
     const float p0 = __builtin_amdgcn_exp2f(z[0] - m), p1 = __builtin_amdgcn_exp2f(z[1] - m);
     l += p0 + p1;
-    add(r.v[0], p0, scale[0].y);
-    add(r.v[1], p1, scale[1].y);
+    add(r.v[0], p0, v_scale[0]);
+    add(r.v[1], p1, v_scale[1]);
   }
-  // The wave's result: acc[channel], m, l in LDS.
-  template <class Pair>
-  __device__ __forceinline__ void join(Pair pair) {
-    const LanePair a = pair(as_u(m)), b = pair(as_u(l));
-    const float la = as_f(b.first), lb = as_f(b.second);
-    const float ma = la > 0.f ? as_f(a.first) : kNegBig, mb = lb > 0.f ? as_f(a.second) : kNegBig;
-    const float top = fmaxf(ma, mb);
-    const float wa = __builtin_amdgcn_exp2f(ma - top), wb = __builtin_amdgcn_exp2f(mb - top);
-    l = la * wa + lb * wb;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const LanePair p = pair(as_u(acc[j]));
-      acc[j] = as_f(p.first) * wa + as_f(p.second) * wb;
-    }
-    m = top;
+  // The wave's result: acc[channel], m, l in LDS.  Eight lanes have each channel: of two that meet, each keeps half of the
+  // channels (16, then 8, 4 and 2 a lane).
+  struct Meeting {
+    float mine, others;   // weights
+  };
+  __device__ __forceinline__ Meeting meet(float other_m, float other_l) {
+    const float a = l != 0.f ? m : kNegBig, b = other_l != 0.f ? other_m : kNegBig;   // (NaN counts)
+    m = fmaxf(a, b);
+    const Meeting w = {__builtin_amdgcn_exp2f(a - m), __builtin_amdgcn_exp2f(b - m)};
+    l = l * w.mine + other_l * w.others;
+    return w;
   }
   __device__ __forceinline__ void finish(float* to, float* to_m, float* to_l, int lane) {
-    join([&](uint32_t v) {
-      const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false);   // lane ^ 8
-      return (lane & 8) ? LanePair{other, v} : LanePair{v, other};
-    });
-    join([](uint32_t v) { return pair_across16(v); });
-    join([](uint32_t v) { return pair_across32(v); });
-    if (lane < 8) {
+    auto across8 = [](float v) { return as_f((uint32_t)__builtin_amdgcn_update_dpp(0, (int)as_u(v), 0x128, 0xf, 0xf, false)); };
+    Meeting w = meet(across8(m), across8(l));
+    const bool high = lane & 8;
+    float a8[8], a4[4], a2[2];
 #pragma unroll
-      for (int j = 0; j < 16; j += 4)
-        *reinterpret_cast<float4*>(to + lane * 16 + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
-      if (lane == 0) *to_m = m, *to_l = l;
+    for (int j = 0; j < 8; ++j) {
+      const float keep = high ? acc[j + 8] : acc[j], give = high ? acc[j] : acc[j + 8];
+      a8[j] = keep * w.mine + across8(give) * w.others;
     }
+    // (the swaps bring the pair in the order first row, second row of the two, whichever of them a lane is in)
+    auto rows = [&](auto swap, bool odd) {
+      const auto pm = swap(as_u(m), as_u(m)), pl = swap(as_u(l), as_u(l));
+      const Meeting x = meet(as_f(odd ? pm.first : pm.second), as_f(odd ? pl.first : pl.second));
+      return odd ? Meeting{x.others, x.mine} : x;   // of the first, of the second
+    };
+    auto swap16 = [](uint32_t x, uint32_t y) {
+      const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+      return LanePair{r[0], r[1]};
+    };
+    auto swap32 = [](uint32_t x, uint32_t y) {
+      const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+      return LanePair{r[0], r[1]};
+    };
+    w = rows(swap16, lane & 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const LanePair p = swap16(as_u(a8[j]), as_u(a8[j + 4]));
+      a4[j] = as_f(p.first) * w.mine + as_f(p.second) * w.others;
+    }
+    w = rows(swap32, lane & 32);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const LanePair p = swap32(as_u(a4[j]), as_u(a4[j + 2]));
+      a2[j] = as_f(p.first) * w.mine + as_f(p.second) * w.others;
+    }
+    const int channel = (lane & 7) * 16 + (lane & 8) + ((lane >> 2) & 4) + ((lane >> 4) & 2);
+    *reinterpret_cast<float2*>(to + channel) = make_float2(a2[0], a2[1]);
+    if (lane == 0) *to_m = m, *to_l = l;
   }
 };
 
-// Up to eight query heads: lane l has channels 8 (l % 16) ..+7 of tokens l / 16 of every four.
+// Up to eight query heads, 32 tokens a step, on the matrix cores (v_mfma_f32_16x16x32_f16; lane l: c = l % 16, g = l / 16).
+// Keys and values lie in LDS as they came, rows of 128 bytes whose chunks of 16 are exclusive-ored with place().  Columns are those of
+// GroupState: column n is head n % 8, columns 0-7 carry 2^14 times a weight rounded to fp16, columns 8-15 2^12 times what that leaves.
+//   logits   first operand: row m of product t = 0, 1 is token 8 (m / 4) + 4 t + m % 4, so that a lane's results are the
+//            tokens 8 g + 4 t + 0..3 of its column; a lane has the 32 channels from 32 g on, eight for each of four products.
+//   values   first operand: channels 16 d + c of the tokens 8 g ..+7, turned by ds_read_b64_tr_b8; the weights that a lane has are the
+//            second operand.  Nothing moves between lanes.
+// A key's scale is multiplied onto its logit, a value's onto the value where it becomes an fp16 number.
 struct ManyHeads {
   static constexpr int kSlots = kGroupHeads, kStride = kGroupStride;
-  GroupState st;
+  static constexpr int kEights = 4, kRing = 2;
+  typedef int int2_t __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) int2_t lds_int2_t;
+  char* stage;      // 2 * 32 rows of this wave
+  uint4 q[4];       // of column c: channels 32 g + 8 j ..+7
+  f32x4_t acc[8];   // [d]: channels 16 d + 4 g + i of column c
+  float ref, l;     // exponent reference of the column (log2), this lane's share of its sum
 
   struct Regs {
-    uint2 k[4], v[4];
+    uint4 k[4], v[4];
   };
-  __device__ __forceinline__ void init(char* stage, const char* query, int heads, int lane) {
-    group_init(st, stage, query, heads, lane);
+  __device__ __forceinline__ static int place(int token, int chunk) {
+    return token * kRowBytes8 + ((chunk ^ ((token >> 1) & 7) ^ ((token >> 3) & 2)) << 4);
   }
-  __device__ __forceinline__ static uint2 ld8(const char* p) {
-    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-    const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p));
-    return make_uint2(v.x, v.y);
-  }
-  __device__ __forceinline__ static void load(Regs& r, const char* k, const char* v, size_t first, size_t second, int lane) {
+  __device__ __forceinline__ void init(char* lds, const char* query, int heads, int lane) {
+    stage = lds;
+    const int head = lane & (kGroupHeads - 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.k[i] = ld8(k + (i < 2 ? first : second) + (i & 1) * 512 + lane * 8);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[i] = ld8(v + (i < 2 ? first : second) + (i & 1) * 512 + lane * 8);
-  }
-  __device__ __forceinline__ void fold(Regs& r, const int (&left)[2], const float2 (&scale)[2], float scale_log2, int lane) {
-    GroupRegs g;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      g.k[i] = halves_of(r.k[i], scale[i >> 1].x);
-      g.v[i] = halves_of(r.v[i], scale[i >> 1].y);
+    for (int j = 0; j < 4; ++j) {
+      const uint4 v = ld16(query + (head < heads ? head : 0) * kRowBytes + (lane >> 4) * 64 + j * 16);
+      q[j] = head < heads ? v : make_uint4(0, 0, 0, 0);
     }
-    g.first = left[0];
-    g.second = left[1];
-    group_fold(st, g, scale_log2, lane);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) acc[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    ref = kNegBig;
+    l = 0.f;
   }
-  __device__ __forceinline__ void finish(float* to, float* to_m, float* to_l, int lane) { group_finish(st, to, to_m, to_l, lane); }
+  __device__ __forceinline__ static half8_t eight(uint32_t x, uint32_t y, float scale) {
+    return __builtin_bit_cast(half8_t, halves_of(make_uint2(x, y), scale));
+  }
+  __device__ __forceinline__ void fold(const Regs& r, const Places& p, int step, float scale_log2, int lane) {
+    const int c = lane & 15, g = lane >> 4;
+    char* k = stage;
+    char* v = stage + 32 * kRowBytes8;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = place(8 * e + (lane >> 3), lane & 7);
+      st16(k + at, r.k[e]);
+      st16(v + at, r.v[e]);
+    }
+    const int from = (step * 4 + g) * 4;
+    const float k_scale = as_f((uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)as_u(p.scale.x))) * scale_log2;
+    const float v_scale = as_f((uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)as_u(p.scale.y)));
+    const int there = __builtin_amdgcn_ds_bpermute(from, p.bytes) >> 7;   // tokens of the lane's eight
+    lds_in_order();
+    float z[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int token = 8 * (c >> 2) + 4 * t + (c & 3);
+      const uint4 a = ld16(k + place(token, 2 * g)), b = ld16(k + place(token, 2 * g + 1));
+      f32x4_t s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+      auto product = [&](uint32_t x, uint32_t y, int j, f32x4_t s) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(eight(x, y, 1.f), __builtin_bit_cast(half8_t, q[j]), s, 0, 0, 0);
+      };
+      s0 = product(a.x, a.y, 0, s0);
+      s1 = product(b.x, b.y, 2, s1);
+      s0 = product(a.z, a.w, 1, s0);
+      s1 = product(b.z, b.w, 3, s1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[4 * t + i] = (s0[i] + s1[i]) * k_scale;
+    }
+    if (__ballot(there < 8)) {   // stale slots contribute nothing
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= there) z[i] = -INFINITY;
+    }
+    float top = z[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
+    LanePair p2 = pair_across16(as_u(top));
+    p2 = pair_across32(as_u(fmaxf(as_f(p2.first), as_f(p2.second))));
+    top = fmaxf(as_f(p2.first), as_f(p2.second));
+    // weights stay at or below 2: the reference moves only when a logit passes that
+    const bool move = top > ref + 1.f;
+    if (__ballot(move)) {
+      const float to = move ? top : ref;
+      const float alpha = __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) acc[d] *= alpha;
+    }
+    half8_t w;
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = __builtin_amdgcn_exp2f(z[i] - ref);
+      sum[i & 1] += x;
+      const float scaled = x * kWeightScale;
+      const _Float16 part = (_Float16)scaled;
+      w[i] = (lane & 8) ? (_Float16)((scaled - (float)part) * kRestScale) : part;
+    }
+    l += sum[0] + sum[1];
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      const int2_t codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2_t*)(v + place(8 * g + (c >> 1), d) + (c & 1) * 8));
+      acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight((uint32_t)codes.x, (uint32_t)codes.y, v_scale), w, acc[d], 0, 0, 0);
+    }
+    lds_in_order();
+  }
+  __device__ __forceinline__ void finish(float* to, float* to_m, float* to_l, int lane) {
+    LanePair s = pair_across16(as_u(l));
+    s = pair_across32(as_u(as_f(s.first) + as_f(s.second)));
+    const int head = lane & 15, g = lane >> 4;
+    const float unscale = (lane & 8) ? 1.f / (kWeightScale * kRestScale) : 1.f / kWeightScale;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      float o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = row_ror_add<8>(acc[d][i] * unscale);   // the two parts of the weights
+      if (head < kGroupHeads)
+        *reinterpret_cast<float4*>(to + head * kStride + 16 * d + 4 * g) = make_float4(o[0], o[1], o[2], o[3]);
+    }
+    if (lane < kGroupHeads) {
+      to_m[lane] = ref;
+      to_l[lane] = as_f(s.first) + as_f(s.second);
+    }
+  }
 };
+
+__device__ __forceinline__ float lse_of(float top, float sum) {
+  return sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
 
 template <class Head>
 __global__ __launch_bounds__(kWaves* kWave, 2) void decode_e4m3_kernel(const DecodeArgs a) {
-  constexpr int kSlots = Head::kSlots, kStride = Head::kStride;
-  __shared__ __align__(16) float acc_lds[kWaves][kSlots * kStride];
+  constexpr int kSlots = Head::kSlots, kStride = Head::kStride, kEights = Head::kEights, kRing = Head::kRing;
+  constexpr int kTile = kWaves * kEights * 8;
+  constexpr int kStage = kSlots > 1 ? 2 * 32 * kRowBytes8 / 4 : 0, kResult = kSlots * kStride;
+  __shared__ __align__(16) float acc_lds[kWaves][kStage > kResult ? kStage : kResult];
   __shared__ float m_lds[kWaves][kSlots], l_lds[kWaves][kSlots];
   __shared__ uint32_t arrived;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
-  const int columns = a.kv_heads * a.subs;
-  const int column = blockIdx.x % columns, index = blockIdx.x / columns;
+  const int columns = a.kv_heads * a.subs;   // KV heads, in parts of up to eight query heads
+  // Work-groups go to the eight dies by turns: a share's columns are all on one, where what they read at a time is adjacent (heads of
+  // the same pages).
+  const int column = blockIdx.x / 8 % columns, index = blockIdx.x / 8 / columns * 8 + blockIdx.x % 8;
   const int hk = column / a.subs, head0 = column % a.subs * kSlots;
   const int n_heads = min(kSlots, a.group - head0);
-  Unit u;
-  if (!find_unit(u, a, index, lane)) return;
-  const size_t out_row = (size_t)u.b * a.num_heads + (size_t)hk * a.group + head0;
-
-  Head st;
-  st.init(reinterpret_cast<char*>(acc_lds[wave]), a.q + out_row * kRowBytes, n_heads, lane);
-  const int32_t* table = a.page_table + (size_t)u.b * a.max_pages;
-  const int32_t* list = a.topk != nullptr ? a.topk + ((size_t)u.b * a.kv_heads + hk) * a.k_pages : nullptr;
+  Line line;
+  if (!line.find<kTile>(a, index, lane)) return;
+  const int64_t begin = a.shares > 0 ? (int64_t)index * line.length : 0;
   const int eights_shift = a.page_shift - 3;   // log2 of a page's eights of tokens
-  const int seq_pages = (u.seq_len + (1 << a.page_shift) - 1) >> a.page_shift;
-  const int steps = u.end_tile - u.first_tile;
 #pragma unroll 1
-  for (int base = 0; base < steps; base += kWalkSteps) {
-    const int n = min(steps - base, kWalkSteps);
-    int block = 0, left = 0;
-    float2 scale = make_float2(1.f, 1.f);
-    {
-      const int eight = ((u.first_tile + base + (lane >> 1)) * kWaves + wave) * 2 + (lane & 1);
-      const int entry = eight >> eights_shift, in_page = eight & ((1 << eights_shift) - 1);
-      int page = entry;
-      if (list != nullptr) page = entry < a.listed ? list[entry] : -1;
-      if ((lane >> 1) < n && page >= 0 && page < seq_pages) {
-        const size_t at = (size_t)table[page] * a.kv_heads + hk;
-        scale = a.scales[at];
-        block = (int)((at << eights_shift) + in_page);
-        left = u.seq_len - (page << a.page_shift) - in_page * 8;
-      }
-    }
-    block = settled(block);
-    left = settled(left);
-    scale.x = as_f((uint32_t)settled((int)as_u(scale.x)));
-    scale.y = as_f((uint32_t)settled((int)as_u(scale.y)));
-    typename Head::Regs r[kSteps];
-    auto load = [&](typename Head::Regs& to, int i) {
-      i = min(i, n - 1);
-      const size_t first = (size_t)(uint32_t)__builtin_amdgcn_readlane(block, 2 * i) * (8 * kRowBytes8);
-      const size_t second = (size_t)(uint32_t)__builtin_amdgcn_readlane(block, 2 * i + 1) * (8 * kRowBytes8);
-      Head::load(to, a.k_pool, a.v_pool, first, second, lane);
-    };
-    auto fold = [&](typename Head::Regs& from, int i) {
-      const int there[2] = {__builtin_amdgcn_readlane(left, 2 * i), __builtin_amdgcn_readlane(left, 2 * i + 1)};
-      const float2 by[2] = {make_float2(from_lane(scale.x, 2 * i), from_lane(scale.y, 2 * i)),
-                            make_float2(from_lane(scale.x, 2 * i + 1), from_lane(scale.y, 2 * i + 1))};
-      st.fold(from, there, by, a.scale_log2, lane);
-    };
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) load(r[j], j);
-    int i = 0;
-#pragma unroll 1
-    for (; i + 2 * kSteps <= n; i += kSteps)
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        fold(r[j], i + j);
-        load(r[j], i + j + kSteps);
-      }
-    if (i + kSteps < n) {
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        fold(r[j], i + j);
-        load(r[j], i + j + kSteps);
-      }
-      i += kSteps;
-    }
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j)
-      if (i + j < n) fold(r[j], i + j);
-  }
+  for (;;) {
+    // The share's part of sequence b: its tiles [first_tile, end_tile), the whole or one of `parts`.
+    const int b = line.b, seq_len = min(max(line.seq_len, 0), a.max_pages << a.page_shift);
+    const int first_tile = (int)max(begin - line.first, (int64_t)0);
+    const int end_tile = (int)min(begin + line.length - line.first, (int64_t)line.tiles);
+    const int share0 = line.first / line.length, parts = (line.first + line.tiles - 1) / line.length - share0 + 1;
+    const size_t out_row = (size_t)b * a.num_heads + (size_t)hk * a.group + head0;
 
-  st.finish(acc_lds[wave], m_lds[wave], l_lds[wave], lane);
-  __syncthreads();
-  // Head `slot`, channels 2 lane and 2 lane + 1, over the four waves.
-  auto joined = [&](int slot, float2& ml) {
-    float w[kWaves], top = kNegBig, sum = 0.f;
+    Head st;
+    st.init(reinterpret_cast<char*>(acc_lds[wave]), a.q + out_row * kRowBytes, n_heads, lane);
+    const int32_t* table = a.page_table + (size_t)b * a.max_pages;
+    const int32_t* list = a.topk != nullptr ? a.topk + ((size_t)b * a.kv_heads + hk) * a.k_pages : nullptr;
+    const int seq_pages = (seq_len + (1 << a.page_shift) - 1) >> a.page_shift;
+    // Places of kPlaceSteps steps at a time, those of the next in three parts while the wave is at these: the list's and the page
+    // table's entries two ahead, the scales one.
+    constexpr int kPlaceSteps = kWave / kEights, kTurns = kPlaceSteps / kRing;   // turns: of the ring
+    const int steps = end_tile - first_tile, turns = (steps + kRing - 1) / kRing;
+    struct Found {
+      int at, eight, bytes;   // (page, head); eight tokens in it; 0 bytes: nothing
+    };
+    auto find = [&](int base) {
+      const int step = base + lane / kEights;
+      const int eight = ((first_tile + step) * kWaves + wave) * kEights + lane % kEights;
+      const int entry = eight >> eights_shift, in_page = eight & ((1 << eights_shift) - 1);
+      bool there = step < steps;
+      int page = entry;
+      if (list != nullptr) {
+        there = there && entry < a.listed;
+        page = list[there ? entry : 0];
+      }
+      there = there && page >= 0 && page < seq_pages;
+      Found f;
+      f.at = table[there ? page : 0] * a.kv_heads + hk;
+      f.eight = in_page;
+      f.bytes = there ? min(max(seq_len - (page << a.page_shift) - in_page * 8, 0), 8) * kRowBytes8 : 0;
+      return f;
+    };
+    auto settle = [](Found& f) {
+      f.at = settled(f.at);
+      f.bytes = settled(f.bytes);
+    };
+    auto scale_at = [&](const Found& f) { return a.scales[f.bytes > 0 ? f.at : 0]; };
+    auto places = [&](const Found& f, float2 scale) {
+      Places p;
+      p.block = (int)((uint32_t)f.at << eights_shift) + f.eight;
+      p.bytes = f.bytes;
+      scale.x = as_f((uint32_t)settled((int)as_u(scale.x)));
+      scale.y = as_f((uint32_t)settled((int)as_u(scale.y)));
+      p.scale = f.bytes > 0 ? scale : make_float2(1.f, 1.f);   // (a page without tokens may have any)
+      return p;
+    };
+    typename Head::Regs r[kRing];
+    auto load = [&](typename Head::Regs& to, int block, int bytes, int step) {
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, l_lds[i][slot] > 0.f ? m_lds[i][slot] : kNegBig);
-    float2 o = make_float2(0.f, 0.f);
+      for (int e = 0; e < kEights; ++e) {
+        const int at = step * kEights + e;
+        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane(block, at);
+        const int n = __builtin_amdgcn_readlane(bytes, at);
+        to.k[e] = row16(rows_at(a.k_pool, first, n), lane);
+        to.v[e] = row16(rows_at(a.v_pool, first, n), lane);
+      }
+    };
+    Found next = find(0);
+    settle(next);
+    float2 scale = scale_at(next);
+    Places now;
+    now.block = (int)((uint32_t)next.at << eights_shift) + next.eight;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      w[i] = l_lds[i][slot] != 0.f ? __builtin_amdgcn_exp2f(m_lds[i][slot] - top) : 0.f;   // (NaN counts)
-      sum += w[i] * l_lds[i][slot];
-      const float2 x = *reinterpret_cast<const float2*>(&acc_lds[i][slot * kStride + lane * 2]);
-      o.x += w[i] * x.x;
-      o.y += w[i] * x.y;
-    }
-    ml = make_float2(top, sum);
-    return o;
-  };
-  if (u.parts > 1) {
-    const size_t part0 = ((size_t)index * columns + column) * kSlots;
-    for (int slot = wave; slot < n_heads; slot += kWaves) {
-      float2 ml;
-      const float2 o = joined(slot, ml);
-      dev_st2(a.part_acc + (part0 + slot) * kHeadDim + lane * 2, o);
-      if (lane == 0) dev_st2(a.part_ml + (part0 + slot) * 2, ml);
-    }
-    wait_stores();
-    __syncthreads();
-    uint32_t* counter = reinterpret_cast<uint32_t*>(a.counters + ((size_t)u.b * columns + column) * kTeamWordStride);
-    if (threadIdx.x == 0) arrived = team_arrive(counter, a.device_fences);
-    __syncthreads();
-    if (arrived != (uint32_t)u.parts - 1) return;
-    team_acquire(a.device_fences);
-    if (threadIdx.x == 0) team_reset(counter);
-    // Parts wave, wave + 4, .. of every head; the weights a part a lane.
-    const size_t first = ((size_t)(index - u.part + wave) * columns + column) * kSlots;
-    const size_t step = (size_t)kWaves * columns * kSlots;
-    const int mine = (u.parts - wave + kWaves - 1) / kWaves;
-    for (int slot = 0; slot < n_heads; ++slot) {
-      float top = kNegBig, sum = 0.f;
-      float2 o = make_float2(0.f, 0.f);
-      for (int base = 0; base < mine; base += kWave) {
-        float2 ml = make_float2(kNegBig, 0.f);
-        if (base + lane < mine) ml = dev_ld2(a.part_ml + (first + slot + (base + lane) * step) * 2);
-        float next = ml.y > 0.f ? ml.x : kNegBig;
-#pragma unroll
-        for (int i = 1; i < kWave; i <<= 1) next = fmaxf(next, __shfl_xor(next, i));
-        next = fmaxf(next, top);
-        const float alpha = __builtin_amdgcn_exp2f(top - next);
-        const float weight = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - next) : 0.f;
-        float add = weight * ml.y;
-#pragma unroll
-        for (int i = 1; i < kWave; i <<= 1) add += __shfl_xor(add, i);
-        sum = sum * alpha + add;
-        o.x *= alpha, o.y *= alpha;
-        top = next;
-        const int n = min(mine - base, kWave);
+    for (int j = 0; j < kRing; ++j) load(r[j], now.block, next.bytes, j);
+    now = places(next, scale);
+    if (turns >= kTurns) next = find(kPlaceSteps);
 #pragma unroll 1
-        for (int i = 0; i < n; i += 16) {
-          float2 x[16];
+    for (int turn0 = 0; turn0 < turns; turn0 += kTurns) {
+      const int n = min(turns - turn0, kTurns);
+      Found after = next;
+      if (n == kTurns) {
+        settle(next);
+        scale = scale_at(next);
+        after = find((turn0 + 2 * kTurns) * kRing);
+      }
+      auto ring = [&](int turn, const Places& from) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            x[j] = dev_ld2(a.part_acc + (first + slot + (size_t)(base + min(i + j, n - 1)) * step) * kHeadDim + lane * 2);
+        for (int j = 0; j < kRing; ++j) {
+          if ((turn0 + turn) * kRing + j < steps) st.fold(r[j], now, turn * kRing + j, a.scale_log2, lane);
+          load(r[j], from.block, from.bytes, (turn * kRing + j + kRing) & (kPlaceSteps - 1));
+        }
+      };
+      int turn = 0;
+#pragma unroll 1
+      do {
+        ring(turn, now);
+      } while (++turn < min(n, kTurns - 1));
+      if (n == kTurns) {
+        const Places then = places(next, scale);
+        ring(kTurns - 1, then);
+        now = then;
+        next = after;
+      }
+    }
+
+    st.finish(acc_lds[wave], m_lds[wave], l_lds[wave], lane);
+    __syncthreads();
+    // Head `slot`, channels 2 lane and 2 lane + 1, over the four waves.
+    auto joined = [&](int slot, float2& ml) {
+      float w[kWaves], top = kNegBig, sum = 0.f;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float w = i + j < n ? from_lane(weight, i + j) : 0.f;
-            o.x += w * x[j].x;
-            o.y += w * x[j].y;
+      for (int i = 0; i < kWaves; ++i) top = fmaxf(top, l_lds[i][slot] > 0.f ? m_lds[i][slot] : kNegBig);
+      float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        w[i] = l_lds[i][slot] != 0.f ? __builtin_amdgcn_exp2f(m_lds[i][slot] - top) : 0.f;   // (NaN counts)
+        sum += w[i] * l_lds[i][slot];
+        const float2 x = *reinterpret_cast<const float2*>(&acc_lds[i][slot * kStride + lane * 2]);
+        o.x += w[i] * x.x;
+        o.y += w[i] * x.y;
+      }
+      ml = make_float2(top, sum);
+      return o;
+    };
+    bool done = false;   // the outputs are somebody else's, or written
+    if (parts > 1) {
+      // A share has two places: for what began in a share before, and for what goes on in the next.
+      auto place = [&](int part) { return (((size_t)(share0 + part) * 2 + (part == 0)) * columns + column) * kSlots; };
+      const size_t mine = place(index - share0);
+      for (int slot = wave; slot < n_heads; slot += kWaves) {
+        float2 ml;
+        const float2 o = joined(slot, ml);
+        dev_st2(a.part_acc + (mine + slot) * kHeadDim + lane * 2, o);
+        if (lane == 0) dev_st2(a.part_ml + (mine + slot) * 2, ml);
+      }
+      wait_stores();
+      __syncthreads();
+      uint32_t* counter = reinterpret_cast<uint32_t*>(a.counters + ((size_t)b * columns + column) * kTeamWordStride);
+      if (threadIdx.x == 0) arrived = team_arrive(counter, a.device_fences);
+      __syncthreads();
+      done = arrived != (uint32_t)parts - 1;
+      if (!done) {
+        team_acquire(a.device_fences);
+        if (threadIdx.x == 0) team_reset(counter);
+        // Half a wave, four channels a lane, has a head's parts (one head: every eighth part).
+        constexpr int kClasses = kSlots > 1 ? 1 : 2 * kWaves, kHalf = kWave / 2;
+        const int half = lane >> 5, l = lane & (kHalf - 1), which = wave * 2 + half;
+        const int slot = kSlots > 1 ? min(which, n_heads - 1) : 0, from = kSlots > 1 ? 0 : which;
+        const int count = (parts - from + kClasses - 1) / kClasses, most = (parts + kClasses - 1) / kClasses;   // (most: whole wave)
+        auto row = [&](int i) { return place(min(from + i * kClasses, parts - 1)) + slot; };
+        float top = kNegBig, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int base = 0; base < most; base += kHalf) {
+          float2 ml = dev_ld2(a.part_ml + row(base + l) * 2);
+          constexpr int kAhead = 8;
+          float2 x[kAhead][2];
+          auto ask = [&](int i) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+              const float* at = a.part_acc + row(base + i + j) * kHeadDim + l * 4;
+              x[j][0] = dev_ld2(at);
+              x[j][1] = dev_ld2(at + 2);
+            }
+          };
+          ask(0);
+          if (base + l >= count) ml = make_float2(kNegBig, 0.f);
+          float next = row16_max(ml.y != 0.f ? ml.x : kNegBig);   // (NaN counts)
+          const LanePair m2 = pair_across16(as_u(next));
+          next = fmaxf(fmaxf(as_f(m2.first), as_f(m2.second)), top);
+          const float alpha = __builtin_amdgcn_exp2f(top - next);
+          const float weight = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - next) : 0.f;
+          const float add = row16_sum(weight * ml.y);
+          const LanePair s2 = pair_across16(as_u(add));
+          sum = sum * alpha + (as_f(s2.first) + as_f(s2.second));
+          o.x *= alpha, o.y *= alpha, o.z *= alpha, o.w *= alpha;
+          top = next;
+          const int n = min(most - base, kHalf);
+#pragma unroll 1
+          for (int i = 0; i < n; i += kAhead) {
+            if (i > 0) ask(i);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+              const float w = as_f((uint32_t)__builtin_amdgcn_ds_bpermute(((lane & kHalf) + min(i + j, kHalf - 1)) * 4, (int)as_u(weight)));
+              const float by = i + j < n ? w : 0.f;
+              o.x += by * x[j][0].x, o.y += by * x[j][0].y;
+              o.z += by * x[j][1].x, o.w += by * x[j][1].y;
+            }
           }
         }
+        if constexpr (kSlots > 1) {
+          if (which < n_heads) {
+            const float factor = sum != 0.f ? 1.f / sum : 0.f;
+            const size_t at = (out_row + slot) * kHeadDim + l * 4;
+            o = make_float4(o.x * factor, o.y * factor, o.z * factor, o.w * factor);
+            if (a.out_is_fp16)
+              store_halves((_Float16*)a.out + at, o);
+            else
+              *reinterpret_cast<float4*>((float*)a.out + at) = o;
+            if (a.lse != nullptr && l == 0) a.lse[out_row + slot] = lse_of(top, sum);
+          }
+          done = true;
+        } else {
+          const LanePair m2 = pair_across32(as_u(top)), s2 = pair_across32(as_u(sum));
+          const float to = fmaxf(as_f(m2.first), as_f(m2.second));
+          const float wa = __builtin_amdgcn_exp2f(as_f(m2.first) - to), wb = __builtin_amdgcn_exp2f(as_f(m2.second) - to);
+          auto both = [&](float v) {
+            const LanePair p = pair_across32(as_u(v));
+            return as_f(p.first) * wa + as_f(p.second) * wb;
+          };
+          o = make_float4(both(o.x), both(o.y), both(o.z), both(o.w));
+          if (lane < kHalf) *reinterpret_cast<float4*>(&acc_lds[wave][l * 4]) = o;
+          if (lane == 0) m_lds[wave][0] = to, l_lds[wave][0] = as_f(s2.first) * wa + as_f(s2.second) * wb;
+          __syncthreads();
+        }
       }
-      *reinterpret_cast<float2*>(&acc_lds[wave][slot * kStride + lane * 2]) = o;
-      if (lane == 0) m_lds[wave][slot] = top, l_lds[wave][slot] = sum;
     }
+    if (!done) {
+      for (int slot = wave; slot < n_heads; slot += kWaves) {
+        float2 ml;
+        const float2 o = joined(slot, ml);
+        const float factor = ml.y != 0.f ? 1.f / ml.y : 0.f;
+        const size_t at = (out_row + slot) * kHeadDim + lane * 2;
+        if (a.out_is_fp16)
+          *reinterpret_cast<half2_t*>((_Float16*)a.out + at) = half2_t{half_of(o.x * factor), half_of(o.y * factor)};
+        else
+          *reinterpret_cast<float2*>((float*)a.out + at) = make_float2(o.x * factor, o.y * factor);
+        if (a.lse != nullptr && lane == 0) a.lse[out_row + slot] = lse_of(ml.x, ml.y);
+      }
+    }
+    // The next sequence, if the share goes on in it.
+    const int64_t end = (int64_t)line.first + line.tiles;
+    if (a.shares == 0 || end >= begin + line.length || b + 1 >= a.batch) return;
+    line.first = (int)end;
+    line.at<kTile>(a, b + 1);
     __syncthreads();
-  }
-  for (int slot = wave; slot < n_heads; slot += kWaves) {
-    float2 ml;
-    const float2 o = joined(slot, ml);
-    const float factor = ml.y != 0.f ? 1.f / ml.y : 0.f;
-    const size_t at = (out_row + slot) * kHeadDim + lane * 2;
-    if (a.out_is_fp16)
-      *reinterpret_cast<half2_t*>((_Float16*)a.out + at) = half2_t{half_of(o.x * factor), half_of(o.y * factor)};
-    else
-      *reinterpret_cast<float2*>((float*)a.out + at) = make_float2(o.x * factor, o.y * factor);
-    if (a.lse != nullptr && lane == 0)
-      a.lse[out_row + slot] = ml.y == 0.f ? -INFINITY : (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2;
   }
 }
 
 bool many_heads(const quest_cache& c) { return group_size(c) > 1; }
+int tile_tokens(const quest_cache& c) { return kWaves * 8 * (many_heads(c) ? ManyHeads::kEights : OneHead::kEights); }
 int columns_of(const quest_cache& c) { return kv_heads(c) * attention_subs(c); }
-// Units of a column that are asked for: two work-groups on every compute unit.
-int most_units_of(const quest_cache& c) {
-  const int most = 512 / columns_of(c);
-  return most > c.batch ? std::max(most, c.batch + 1) : 0;
+// Shares of a column: a work-group on every compute unit, or one a sequence.  (More of them for few sequences leave more to join and no
+// more bytes under way: 128 pages of each of 32 heads 9.0 us, with twice as many 10.4; 590k tokens of 16 sequences and 8 KV heads
+// 196 us and 201.)  None where the (sequence, KV head) pairs are more than two for a compute unit: the units then even out what
+// sequences differ by (256 sequences of 10 to 2000 tokens and 8 KV heads 94 us, in shares 132; 64 sequences 56 and 56).
+int most_shares(const quest_cache& c) {
+  const int columns = columns_of(c);
+  const int64_t tiles = ((int64_t)c.max_pages_per_seq * c.page_size / tile_tokens(c) + 1) * c.batch;
+  return (int64_t)c.batch * columns <= 512 && tiles <= INT32_MAX ? std::max(256 / columns, c.batch) : 0;
 }
-size_t unit_bytes(const quest_cache& c) {
-  return (size_t)columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * (kHeadDim + 2) * sizeof(float);
+size_t share_bytes(const quest_cache& c) {
+  return (size_t)2 * columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * (kHeadDim + 2) * sizeof(float);
 }
 // (The counters' part is as long as that of an fp16 cache of the shape, so that one workspace serves both.)
 size_t counter_bytes(const quest_cache& c) { return decode_counter_bytes(c); }
@@ -423,12 +651,12 @@ size_t counter_bytes(const quest_cache& c) { return decode_counter_bytes(c); }
 }  // namespace
 
 size_t decode_e4m3_workspace_bytes(const quest_cache& c) {
-  const int units = most_units_of(c);
-  return units > 0 ? counter_bytes(c) + units * unit_bytes(c) : 0;
+  const int shares = most_shares(c);
+  return shares > 0 ? counter_bytes(c) + shares * share_bytes(c) : 0;
 }
 
 bool decode_e4m3_fits_a_launch(const quest_cache& c) {
-  return (int64_t)std::max(most_units_of(c), c.batch) * columns_of(c) < (1 << 24) - 1;   // 2^32 threads
+  return ((int64_t)std::max(most_shares(c), c.batch) + 8) * columns_of(c) < 1 << 24;   // 2^32 threads
 }
 
 int launch_decode_e4m3(const quest_cache& c, const void* q, const int32_t* topk_idx, int k_pages, float sm_scale, void* out,
@@ -439,14 +667,14 @@ int launch_decode_e4m3(const quest_cache& c, const void* q, const int32_t* topk_
   a.topk = topk_idx;
   a.k_pages = k_pages;
   a.listed = topk_idx != nullptr ? std::min(k_pages, c.max_pages_per_seq) : 0;
-  a.most_units = most_units_of(c);
   const size_t counters = counter_bytes(c);
-  const size_t room = workspace != nullptr && workspace_bytes > counters ? (workspace_bytes - counters) / unit_bytes(c) : 0;
-  if (room < (size_t)a.most_units) a.most_units = room > (size_t)c.batch ? (int)room : 0;   // as far as it goes
+  const size_t room = workspace != nullptr && workspace_bytes > counters ? (workspace_bytes - counters) / share_bytes(c) : 0;
+  a.shares = most_shares(c);
+  if (room < (size_t)a.shares) a.shares = room >= (size_t)c.batch ? (int)room : 0;   // as far as it goes
   a.counters = (uint64_t*)workspace;
   a.part_acc = (float*)((char*)workspace + counters);
-  const int units = std::max(a.most_units, c.batch);
-  a.part_ml = a.part_acc + (size_t)units * columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * kHeadDim;
+  a.part_ml = a.part_acc + (size_t)a.shares * 2 * columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * kHeadDim;
+  const int units = ((a.shares > 0 ? a.shares : c.batch) + 7) / 8 * 8;
   const dim3 grid((unsigned)((int64_t)units * columns_of(c))), block(kWaves * kWave);
   if (many_heads(c))
     hipLaunchKernelGGL(decode_e4m3_kernel<ManyHeads>, grid, block, 0, s, a);
