@@ -103,15 +103,6 @@ struct Line {
   }
 };
 
-// A buffer of the first `bytes` of a block of eight tokens: what lies behind them is not read, and zero.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* pool, uint32_t block, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool) + (size_t)block * (8 * kRowBytes8), 0, bytes, 0x00020000);
-}
-__device__ __forceinline__ uint4 row16(__amdgpu_buffer_rsrc_t rows, int lane) {
-  const auto v = __builtin_amdgcn_raw_buffer_load_b128(rows, lane * 16, 0, 2);   // (non-temporal)
-  return make_uint4(v[0], v[1], v[2], v[3]);
-}
-
 // Where the eights of tokens of a wave's steps lie, kEights lanes a step.
 struct Places {
   int block, bytes;     // bytes: of the tokens that there are, 0 to 1024

@@ -61,6 +61,15 @@ __device__ __forceinline__ int exponent_for(uint32_t bits) {
 __device__ __forceinline__ float scale_of(int exponent) { return __builtin_bit_cast(float, (uint32_t)(exponent + 127) << 23); }
 __device__ __forceinline__ int exponent_of(float scale) { return (int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127; }
 
+// A buffer of the first `bytes` of a block of eight tokens: what lies behind them is not read, and zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* pool, uint32_t block, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool) + (size_t)block * (8 * kRowBytes8), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ uint4 row16(__amdgpu_buffer_rsrc_t rows, int lane) {
+  const auto v = __builtin_amdgcn_raw_buffer_load_b128(rows, lane * 16, 0, 2);   // (non-temporal)
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 #endif  // __HIPCC__
 
 }  // namespace quest

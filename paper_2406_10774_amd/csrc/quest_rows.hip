@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     walk.load8(a, w.stream, w.hk, step, wave * 8, lane, key8, value8);
   };
   auto put8 = [&](int step) {
-    if (step < steps) walk.put8(step, wave * 8, lane, key8, value8, keys(step), values(step));
+    if (step < steps) walk.put8(walk.scales8(), step, wave * 8, lane, key8, value8, keys(step), values(step));
   };
   if constexpr (k8) {
     walk.find8(a, w.stream, w.hk, 0, lane);
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     ask8(0);
     const uint4 key0 = key8, value0 = value8;
     ask8(1);
-    walk.put8(0, wave * 8, lane, key0, value0, keys(0), values(0));
+    walk.put8(walk.scales8(), 0, wave * 8, lane, key0, value0, keys(0), values(0));
     put8(1);
     ask8(2);
     st.ready(a.q_sign);
@@ -251,7 +251,7 @@ template <bool kTree, bool kHalfOut, bool k8>
 __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
-  constexpr int kTokens = 32, kEach = k8 ? 8 : 4, kLoads = kTokens / kEach;   // kEach: tokens of a wave-wide load
+  constexpr int kTokens = 32, kLoads = kTokens / 4;
   constexpr int kStride = kHeadDim + 4;
   constexpr int kStage = 2 * kTokens * kRowBytes, kJoin = kFewRows * kStride * 4;
   __shared__ __align__(16) char lds[kWaves * (kStage > kJoin ? kStage : kJoin)];
@@ -277,48 +277,84 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   uint64_t held = 0, held_next = 0;
   uint4 k[kLoads], v[kLoads];
   bool token_there[kLoads];
-  auto find = [&](int step) {
-    if constexpr (k8)
-      walk.find8(a, w.stream, w.hk, step, lane);
-    else
-      walk.find(w.stream, step, lane);
-  };
   auto load = [&](int step) {
-    if (!walk.knows(step)) find(step);
-    if constexpr (k8) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) walk.load8(a, w.stream, w.hk, step, i * 8, lane, k[i], v[i]);
-      return;
-    }
+    if (!walk.knows(step)) walk.find(w.stream, step, lane);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) token_there[i] = walk.load(a, w.stream, w.hk, step, i * 4, lane, k[i], v[i]);
     if (kTree) held_next = walk.held(step, lane);
   };
-  if (steps > 0) find(0);
-  st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
-  if (steps > 0) load(0);
-  st.ready(a.q_sign);
-  for (int step = 0; step < steps; ++step) {
-    held = held_next;
-    if constexpr (k8) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) walk.put8(step, i * 8, lane, k[i], v[i], stage_k, stage_v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = i * 4 + (lane >> 4);
-        st16(stage_k + k_place(at, lane & 15), k[i]);
-        st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
-      }
-    }
-    lds_in_order();
-    if (step + 1 < steps) load(step + 1);
+  auto fold = [&](int step) {
     const bool masked = !walk.whole(w.stream, held, step, first_position);
     uint64_t allow = ~0ull;
     if (masked)
       allow = walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words, a.mask_words);
     st.template fold<1>(stage_k, stage_v, a, masked, allow, lane);
     lds_in_order();
+  };
+  if constexpr (k8) {
+    // Pages of 8 bits: two steps on their way in the registers of one.  (No load of the loop is ever skipped, so that the compiler knows
+    // how many are under way.)
+    constexpr int kEights = kTokens / 8;
+    struct Step {
+      uint4 k[kEights], v[kEights];
+      typename Walk<kTree, kTokens, k8>::Scales8 scales;
+    } at[2];
+    auto load8 = [&](Step& to, int step) {
+      if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
+#pragma unroll
+      for (int i = 0; i < kEights; ++i) walk.load8(a, w.stream, w.hk, step, i * 8, lane, to.k[i], to.v[i]);
+      to.scales = walk.scales8();
+    };
+    walk.find8(a, w.stream, w.hk, 0, lane);
+    st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+    load8(at[0], 0);
+    if (steps > 1) load8(at[1], 1);
+    st.ready(a.q_sign);
+    auto put8 = [&](const Step& from, int step) {
+#pragma unroll
+      for (int i = 0; i < kEights; ++i) walk.put8(from.scales, step, i * 8, lane, from.k[i], from.v[i], stage_k, stage_v);
+      lds_in_order();
+    };
+    int step = 0;
+#pragma unroll 1
+    for (; step + 3 < steps; step += 2)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        put8(at[j], step + j);
+        load8(at[j], step + j + 2);
+        fold(step + j);
+      }
+    const int rest = steps - step;   // 0 to 3
+    if (rest > 0) {
+      put8(at[0], step);
+      if (rest > 2) load8(at[0], step + 2);
+      fold(step);
+    }
+    if (rest > 1) {
+      put8(at[1], step + 1);
+      fold(step + 1);
+    }
+    if (rest > 2) {
+      put8(at[0], step + 2);
+      fold(step + 2);
+    }
+  } else {
+    if (steps > 0) walk.find(w.stream, 0, lane);
+    st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
+    if (steps > 0) load(0);
+    st.ready(a.q_sign);
+    for (int step = 0; step < steps; ++step) {
+      held = held_next;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = i * 4 + (lane >> 4);
+        st16(stage_k + k_place(at, lane & 15), k[i]);
+        st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
+      }
+      lds_in_order();
+      if (step + 1 < steps) load(step + 1);
+      fold(step);
+    }
   }
 
   // Join the waves' results: eight threads a row, 16 channels each.
@@ -554,8 +590,11 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   const int r = check_launch(who);
   if (r != QUEST_OK || p.most_units == 0) return r;
   const unsigned tiles = (unsigned)(p.row_tiles * a.kv_heads);
-  if (p.rows == kFewRows)
+  if (p.rows == kFewRows && tiles <= 64)
     hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 4>), dim3(tiles * (kFewRows / 4)), dim3(256), 0, s, a, a.cu,
+                       a.seq_lens, topk);
+  else if (p.rows == kFewRows)
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 16>), dim3(tiles * (kFewRows / 16)), dim3(256), 0, s, a, a.cu,
                        a.seq_lens, topk);
   else if (tiles <= 32)
     hipLaunchKernelGGL((merge_rows_kernel<kTree, kSharedRows, 4>), dim3(tiles * (kSharedRows / 4)), dim3(256), 0, s, a,

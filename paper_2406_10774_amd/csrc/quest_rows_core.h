@@ -524,21 +524,31 @@ struct Walk {
     scale = make_float2(1.f, 1.f);   // (a page without tokens may have any)
     if (left > 0) scale = a.scales[(size_t)phys * a.kv_heads + hk];
   }
-  // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15.
-  __device__ __forceinline__ void load8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int eight, int lane, uint4& key,
-                                        uint4& value) const {
-    const int page = __builtin_amdgcn_readlane(phys, ((step - first_step) << per_step_log2) + (eight >> shift));
-    const int at = start + step * stride + eight;
-    const int64_t row = (((int64_t)page * a.kv_heads + hk) << s.page_shift) + (at & ((1 << s.page_shift) - 1));
-    key = ld16(a.k_pool + row * kRowBytes8 + lane * 16);   // eight rows of 128 bytes
-    value = ld16(a.v_pool + row * kRowBytes8 + lane * 16);
-  }
-  // What load8 brought, as fp16 numbers into LDS (k, v: the tile); before another find8.  A value that is not there is zero.
-  __device__ __forceinline__ void put8(int step, int eight, int lane, uint4 key, uint4 value, char* k, char* v) const {
+  // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15; zeros where there
+  // is no token.
+  __device__ __forceinline__ void load8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int eight, int lane,
+                                        uint4& key, uint4& value) const {
     const int from = ((step - first_step) << per_step_log2) + (eight >> shift);
-    const float k_scale = from_lane(scale.x, from), v_scale = from_lane(scale.y, from);
-    const int sub = lane >> 3, token = eight + sub, slot = (lane & 7) * 2;
-    if ((eight & ((1 << shift) - 1)) + sub >= __builtin_amdgcn_readlane(left, from)) value = make_uint4(0, 0, 0, 0);
+    const int page = __builtin_amdgcn_readlane(phys, from);
+    const int at = (start + step * stride + eight) & ((1 << s.page_shift) - 1);
+    const uint32_t block = ((uint32_t)(page * a.kv_heads + hk) << (s.page_shift - 3)) + (at >> 3);
+    const int tokens = min(max(__builtin_amdgcn_readlane(left, from) - (eight & ((1 << shift) - 1)), 0), 8);
+    // (the same in all lanes, which the compiler does not see)
+    const uint32_t of_wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)block);
+    const int bytes = __builtin_amdgcn_readfirstlane(tokens * kRowBytes8);
+    key = row16(rows_at(a.k_pool, of_wave, bytes), lane);
+    value = row16(rows_at(a.v_pool, of_wave, bytes), lane);
+  }
+  // What load8 brought, as fp16 numbers into LDS (k, v: the tile).  `of`: the scales as they were then.
+  struct Scales8 {
+    float2 scale;
+    int first_step;
+  };
+  __device__ __forceinline__ Scales8 scales8() const { return {scale, first_step}; }
+  __device__ __forceinline__ void put8(const Scales8& of, int step, int eight, int lane, uint4 key, uint4 value, char* k, char* v) const {
+    const int from = ((step - of.first_step) << per_step_log2) + (eight >> shift);
+    const float k_scale = from_lane(of.scale.x, from), v_scale = from_lane(of.scale.y, from);
+    const int token = eight + (lane >> 3), slot = (lane & 7) * 2;
     st16(k + k_place(token, slot), halves_of(make_uint2(key.x, key.y), k_scale));
     st16(k + k_place(token, slot + 1), halves_of(make_uint2(key.z, key.w), k_scale));
     st16(v + v_place(token, slot), halves_of(make_uint2(value.x, value.y), v_scale));
