@@ -8,8 +8,10 @@
 // 8 bits: the scale of a page belongs to all of its tokens, so a wave has a whole (page, head) in registers before it rounds the first
 // number.  A page that held tokens before keeps its scale unless the new ones need a larger one; then its old numbers are rounded again.
 //
-// Bound by memory: every number is read once and written once.  A wave has one (page, head), the waves of a work-group adjacent
-// heads; queries follow in the same launch, a wave having four tokens (whose table rows it then reads once) of kQHeads heads.
+// Bound by memory: every number is read once and written once.  The waves of a work-group have adjacent heads; queries follow in the
+// same launch, a wave having four tokens (whose table rows it then reads once) of kQHeads heads.  32749 tokens, pages of 16: 32 query / 8
+// KV heads turned into pages of 8 bits 143 us (763 MB, 5.3 TB/s; a large copy 5.3), 32 heads into pages of 8 bits as they are 154 us (5.4).
+// One token each of 16 sequences 4.5 us: lengths -> page -> data -> store.
 //
 // Without any length on the host: the pages of sequence b start at unit floor(cu[b] / S) + 2 b, which leaves
 // room for the floor((n + S - 2) / S) + 1 pages that n >= 1 tokens can touch.
@@ -20,7 +22,8 @@ namespace quest {
 
 namespace {
 
-constexpr int kInsertWaves = 4;
+constexpr int kPairsOf = 4;     // (page, head) pairs of a work-group: adjacent heads
+constexpr int kRowWaves = 4;    // of a work-group that turns rows alone
 constexpr int kQHeads = 4;
 
 struct InsertArgs {
@@ -38,7 +41,7 @@ struct InsertArgs {
   char* q_out;
   int64_t new_stride, q_stride, q_out_stride;   // bytes between tokens
   int batch, kv_heads, q_heads, max_pages, total;
-  int64_t num_phys_pages, waves;                // waves: of the insertion
+  int64_t num_phys_pages, pairs;                // pairs: (page, head) pairs at most
   int64_t insert_blocks;
   const float* table;
   const int32_t* positions;
@@ -107,9 +110,15 @@ __device__ __forceinline__ uint4 turn(const InsertArgs& a, uint4 v, const Turn& 
   } else {
     const int by = a.rotary >> 4;   // lanes between the channels of a pair
     const bool second = chunk >= by;
-    const int from = (stays ? lane : second ? lane - by : lane + by) * 4;
-    const uint4 o = make_uint4(__builtin_amdgcn_ds_bpermute(from, v.x), __builtin_amdgcn_ds_bpermute(from, v.y),
-                               __builtin_amdgcn_ds_bpermute(from, v.z), __builtin_amdgcn_ds_bpermute(from, v.w));
+    uint4 o;
+    if (by == 8) {   // half a row of lanes away
+      auto across = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false); };
+      o = make_uint4(across(v.x), across(v.y), across(v.z), across(v.w));
+    } else {
+      const int from = (stays ? lane : second ? lane - by : lane + by) * 4;
+      o = make_uint4(__builtin_amdgcn_ds_bpermute(from, v.x), __builtin_amdgcn_ds_bpermute(from, v.y),
+                     __builtin_amdgcn_ds_bpermute(from, v.z), __builtin_amdgcn_ds_bpermute(from, v.w));
+    }
     const float sign = second ? 1.f : -1.f;
     auto two = [&](uint32_t own, uint32_t other, float c0, float s0, float c1, float s1) {
       return two_halves(turned(half_lo(own), c0, half_lo(other), sign * s0), turned(half_hi(own), c1, half_hi(other), sign * s1));
@@ -156,10 +165,13 @@ __device__ __forceinline__ void turn_rows(const InsertArgs& a, int64_t at, int l
   }
 }
 
-__global__ __launch_bounds__(kInsertWaves* kWave) void rotate_rows_kernel(const InsertArgs a) {
-  turn_rows(a, (int64_t)blockIdx.x * kInsertWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane_id());
+__global__ __launch_bounds__(kRowWaves* kWave) void rotate_rows_kernel(const InsertArgs a) {
+  turn_rows(a, (int64_t)blockIdx.x * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane_id());
 }
 
+__device__ __forceinline__ uint32_t magnitude8(uint4 v) {
+  return key_max2(key_max2(magnitude2(v.x), magnitude2(v.y)), key_max2(magnitude2(v.z), magnitude2(v.w)));
+}
 // The largest 16-bit magnitude of the wave.
 __device__ __forceinline__ uint32_t largest_half(uint32_t m2) {
   m2 = key_max2(m2, m2 >> 16);
@@ -170,111 +182,165 @@ __device__ __forceinline__ uint32_t largest_half(uint32_t m2) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)rows_key_max2(m2)) & 0xffffu;
 }
 
-// The page's numbers (keys or values) to 8 bits; x: slots 4 i + sub, channels 8 chunk ..+7.  Returns the scale.
+// A wave's part of a page (keys or values) to 8 bits, with scale 2^e: slots first + 4 i + sub, channels 8 chunk ..+7 of x are new
+// from slot `from` to slot `to`; those before hold numbers of scale `old`.
 template <int kLoads>
-__device__ __forceinline__ float round_page(char* block, const uint4 (&x)[kLoads], int from, int to, float old, int lane) {
+__device__ __forceinline__ void round_part(char* block, const uint4 (&x)[kLoads], int first, int from, int to, float old, float scale,
+                                           int lane) {
   const int sub = lane >> 4, chunk = lane & 15;
-  uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int slot = 4 * i + sub;
-    if (slot >= from && slot < to)
-      most = key_max2(key_max2(key_max2(most, magnitude2(x[i].x)), key_max2(magnitude2(x[i].y), magnitude2(x[i].z))),
-                      magnitude2(x[i].w));
-  }
-  int e = exponent_for(largest_half(most));
-  if (from > 0) e = max(e, exponent_of(old));
-  const float scale = scale_of(e);
-  if (from > 0 && scale != old) {
-    for (int slot = sub; slot < from; slot += 4) {
-      uint2* at = reinterpret_cast<uint2*>(block + slot * kRowBytes8 + chunk * 8);
+    const int slot = first + 4 * i + sub;
+    uint2* at = reinterpret_cast<uint2*>(block + slot * kRowBytes8 + chunk * 8);
+    if (slot >= from) {
+      if (slot < to) *at = codes_of(at_most8(x[i]), scale);
+    } else if (scale != old) {
       *at = codes_of(halves_of(*at, old), scale);
     }
   }
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int slot = 4 * i + sub;
-    if (slot >= from && slot < to)
-      *reinterpret_cast<uint2*>(block + slot * kRowBytes8 + chunk * 8) = codes_of(at_most8(x[i]), scale);
-  }
-  return scale;
 }
 
+// How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their numbers in
+// registers: one wave's too, or, turned (which takes registers of its own, and from the queries' waves as well), 16 tokens a wave, and what
+// belongs to the page goes through LDS.  32k tokens of 32 / 8 heads in pages of 32 (64): one wave 170 (207) us, parts 165 (169);
+// without rotation, 32 heads, one wave 153 (158), parts 176 (177).
 template <int kS, bool k8, bool kRotate>
-__global__ __launch_bounds__(kInsertWaves* kWave) void insert_kernel(const InsertArgs a) {
-  constexpr int kLoads = kS / 4;   // wave-wide loads of four tokens each
+struct Shape {
+  static constexpr int kParts = k8 && kRotate && kS > 16 ? kS / 16 : 1;   // waves of a page
+  static constexpr int kTokens = kS / kParts;                             // of a wave
+  static constexpr int kPairs = kParts == 4 ? 1 : kPairsOf;               // of a work-group
+  static constexpr int kWaves = kPairs * kParts;
+  static constexpr int kEach = k8 ? kTokens : kTokens < 16 ? kTokens : 16;   // tokens at a time
+};
+
+template <int kS, bool k8, bool kRotate>
+__global__ __launch_bounds__((Shape<kS, k8, kRotate>::kWaves * kWave)) void insert_kernel(const InsertArgs a) {
+  using Of = Shape<kS, k8, kRotate>;
+  constexpr int kParts = Of::kParts, kWaves = Of::kWaves, kEach = Of::kEach;
+  constexpr int kLoads = kEach / 4;   // wave-wide loads of four tokens each
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (kRotate && blockIdx.x >= a.insert_blocks) {
-    turn_rows(a, (blockIdx.x - a.insert_blocks) * kInsertWaves + wave, lane);
+    turn_rows(a, (blockIdx.x - a.insert_blocks) * kWaves + wave, lane);
     return;
   }
-  const int64_t at = (int64_t)blockIdx.x * kInsertWaves + wave;
-  if (at >= a.waves) return;
-  const int unit = (int)(at / a.kv_heads);
-  const int head = (int)(at - (int64_t)unit * a.kv_heads);
+  const int64_t at = (int64_t)blockIdx.x * Of::kPairs + wave / kParts;
+  const int part = wave % kParts;
+  bool there = at < a.pairs;
+  const int unit = there ? (int)(at / a.kv_heads) : 0;
+  const int head = there ? (int)(at - (int64_t)unit * a.kv_heads) : 0;
   const int b = sequence_at(a, unit, lane, [&](int i) { return a.cu[i] / kS + 2 * i; });
   const int first_row = a.cu[b];
   const int tokens = a.cu[b + 1] - first_row;
   const int seq_len = a.seq_lens[b];
   const int first = seq_len - tokens;                              // position of the first new token
   const int page = first / kS + unit - (first_row / kS + 2 * b);
-  if (tokens <= 0 || first < 0 || page > (seq_len - 1) / kS || page >= a.max_pages) return;   // (no page behind the row)
+  there = there && tokens > 0 && first >= 0 && page <= (seq_len - 1) / kS && page < a.max_pages;   // (no page behind the row)
+  if (kParts == 1 && !there) return;
   const int from = max(first - page * kS, 0), to = min(seq_len - page * kS, kS);   // the page's new slots
-  const int phys = a.page_table[(size_t)b * a.max_pages + page];
+  const int phys = there ? a.page_table[(size_t)b * a.max_pages + page] : 0;
   const size_t block = (size_t)phys * a.kv_heads + head;
   const int sub = lane >> 4, chunk = lane & 15;
 
   uint4 k[kLoads], v[kLoads];
-  int row[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int slot = 4 * i + sub;
-    const bool here = slot >= from && slot < to;
-    row[i] = first_row + (here ? page * kS + slot - first : 0);
-    int source = row[i];
-    if (a.rows != nullptr) source = a.rows[source];
-    const int64_t off = source * a.new_stride + (int64_t)head * kRowBytes + chunk * 16;
-    k[i] = ld16_stream(a.k_new + off);
-    v[i] = ld16_stream(a.v_new + off);
-  }
-  float2 old = make_float2(0.f, 0.f);
-  if (k8 && from > 0) old = a.scales[block];
-  if constexpr (kRotate) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      Turn t;
-      t.load(a, a.positions != nullptr ? a.positions[row[i]] : first + row[i] - first_row, chunk);
-      k[i] = turn(a, k[i], t, chunk, lane);
-    }
-  }
-
   uint4 mn = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
   uint4 mx = make_uint4(0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u);
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int slot = 4 * i + sub;
-    if (slot >= from && slot < to) {
-      const uint4 key = order_key8(k[i]);
-      mn = key_min8(mn, key);
-      mx = key_max8(mx, key);
-    }
-  }
-  if constexpr (k8) {
-    const float k_scale = round_page<kLoads>(a.k_pool + block * (kS * kRowBytes8), k, from, to, old.x, lane);
-    const float v_scale = round_page<kLoads>(a.v_pool + block * (kS * kRowBytes8), v, from, to, old.y, lane);
-    if (lane == 0) a.scales[block] = make_float2(k_scale, v_scale);
-  } else {
+  uint32_t most[2] = {0, 0};
+  // Values asked for when the keys are turned leave registers for more waves (pages of 16 tokens 147 us, else 153; not where a
+  // wave has several times 16 tokens one after the other, 163 and 159).
+  constexpr bool kLate = kRotate && (kS <= 16 || kParts > 1);
+  // The new tokens from slot first_slot on, turned, and what the page's metadata and scales need of them.
+  auto take = [&](int first_slot) {
+    int row[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int slot = 4 * i + sub;
+      const int slot = first_slot + 4 * i + sub;
+      const bool here = slot >= from && slot < to;
+      row[i] = first_row + (here ? page * kS + slot - first : 0);
+      int source = row[i];
+      if (!kRotate && a.rows != nullptr) source = a.rows[source];
+      const int64_t off = source * a.new_stride + (int64_t)head * kRowBytes + chunk * 16;
+      k[i] = ld16_stream(a.k_new + off);
+      if (!kLate) v[i] = ld16_stream(a.v_new + off);
+    }
+    if constexpr (kRotate) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        Turn t;
+        t.load(a, a.positions != nullptr ? a.positions[row[i]] : first + row[i] - first_row, chunk);
+        k[i] = turn(a, k[i], t, chunk, lane);
+      }
+      if (kLate) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+          v[i] = ld16_stream(a.v_new + row[i] * a.new_stride + (int64_t)head * kRowBytes + chunk * 16);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int slot = first_slot + 4 * i + sub;
       if (slot >= from && slot < to) {
-        const size_t off = block * (kS * kRowBytes) + (size_t)slot * kRowBytes + chunk * 16;
-        st16(a.k_pool + off, k[i]);
-        st16(a.v_pool + off, v[i]);
+        const uint4 key = order_key8(k[i]);
+        mn = key_min8(mn, key);
+        mx = key_max8(mx, key);
+        if constexpr (k8) {
+          most[0] = key_max2(most[0], magnitude8(k[i]));
+          most[1] = key_max2(most[1], magnitude8(v[i]));
+        }
+      }
+    }
+  };
+  if constexpr (k8) {
+    const int first_slot = part * Of::kTokens;
+    float2 old = make_float2(0.f, 0.f);
+    if (there && from > 0) old = a.scales[block];
+    if (there && first_slot + Of::kTokens > from && first_slot < to) take(first_slot);
+    most[0] = largest_half(most[0]);
+    most[1] = largest_half(most[1]);
+    if constexpr (kParts > 1) {
+      __shared__ uint4 bounds[kWaves][2][16];
+      __shared__ uint32_t largest[kWaves][2];
+      mn = rows_key_min8(mn);
+      mx = rows_key_max8(mx);
+      if (lane < 32) bounds[wave][sub][chunk] = sub == 0 ? mn : mx;
+      if (lane == 0) largest[wave][0] = most[0], largest[wave][1] = most[1];
+      __syncthreads();
+      if (!there) return;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        const int of = wave - part + i;
+        most[0] = max(most[0], largest[of][0]);
+        most[1] = max(most[1], largest[of][1]);
+        if (part == 0) {
+          mn = key_min8(mn, bounds[of][0][chunk]);
+          mx = key_max8(mx, bounds[of][1][chunk]);
+        }
+      }
+    }
+    int e[2] = {exponent_for(most[0]), exponent_for(most[1])};
+    if (from > 0) e[0] = max(e[0], exponent_of(old.x)), e[1] = max(e[1], exponent_of(old.y));
+    const float2 scale = make_float2(scale_of(e[0]), scale_of(e[1]));
+    round_part<kLoads>(a.k_pool + block * (kS * kRowBytes8), k, first_slot, from, to, old.x, scale.x, lane);
+    round_part<kLoads>(a.v_pool + block * (kS * kRowBytes8), v, first_slot, from, to, old.y, scale.y, lane);
+    if (part == 0 && lane == 0) a.scales[block] = scale;
+  } else {
+#pragma unroll 1
+    for (int first_slot = 0; first_slot < kS; first_slot += kEach) {
+      if (first_slot + kEach <= from || first_slot >= to) continue;
+      take(first_slot);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int slot = first_slot + 4 * i + sub;
+        if (slot >= from && slot < to) {
+          const size_t off = block * (kS * kRowBytes) + (size_t)slot * kRowBytes + chunk * 16;
+          st16(a.k_pool + off, k[i]);
+          st16(a.v_pool + off, v[i]);
+        }
       }
     }
   }
+  if (part != 0) return;
   mn = rows_key_min8(mn);
   mx = rows_key_max8(mx);
   if (lane < 32) {
@@ -290,17 +356,18 @@ __global__ __launch_bounds__(kInsertWaves* kWave) void insert_kernel(const Inser
 
 int64_t waves_of_rows(const InsertArgs& a) { return ((int64_t)a.total + 3) / 4 * ((a.q_heads + kQHeads - 1) / kQHeads); }
 
-template <int kS>
-int launch_insert_for(const InsertArgs& a, bool pages8, bool rotate, const char* who, hipStream_t s) {
-  const int64_t rows = rotate && a.q != nullptr ? (waves_of_rows(a) + kInsertWaves - 1) / kInsertWaves : 0;
-  const dim3 grid((unsigned)(a.insert_blocks + rows)), block(kInsertWaves * kWave);
-  if (!pages8)
-    hipLaunchKernelGGL((insert_kernel<kS, false, true>), grid, block, 0, s, a);
-  else if (rotate)
-    hipLaunchKernelGGL((insert_kernel<kS, true, true>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((insert_kernel<kS, true, false>), grid, block, 0, s, a);
+template <int kS, bool k8, bool kRotate>
+int launch_insert_as(InsertArgs& a, const char* who, hipStream_t s) {
+  using Of = Shape<kS, k8, kRotate>;
+  a.insert_blocks = (a.pairs + Of::kPairs - 1) / Of::kPairs;
+  const int64_t rows = kRotate && a.q != nullptr ? (waves_of_rows(a) + Of::kWaves - 1) / Of::kWaves : 0;
+  hipLaunchKernelGGL((insert_kernel<kS, k8, kRotate>), dim3((unsigned)(a.insert_blocks + rows)), dim3(Of::kWaves * kWave), 0, s, a);
   return check_launch(who);
+}
+template <int kS>
+int launch_insert_for(InsertArgs& a, bool pages8, bool rotate, const char* who, hipStream_t s) {
+  if (!pages8) return launch_insert_as<kS, false, true>(a, who, s);
+  return rotate ? launch_insert_as<kS, true, true>(a, who, s) : launch_insert_as<kS, true, false>(a, who, s);
 }
 
 InsertArgs rotation_args(const quest_cache& c, const PackedTokens& p, const quest_rotation* r) {
@@ -342,8 +409,7 @@ int launch_insert(const quest_cache& c, const PackedTokens& p, const quest_rotat
   a.q_heads = c.num_heads;
   a.max_pages = c.max_pages_per_seq;
   a.num_phys_pages = c.num_phys_pages;
-  a.waves = ((int64_t)p.total / c.page_size + 2 * (int64_t)c.batch) * a.kv_heads;
-  a.insert_blocks = (a.waves + kInsertWaves - 1) / kInsertWaves;
+  a.pairs = ((int64_t)p.total / c.page_size + 2 * (int64_t)c.batch) * a.kv_heads;
   const bool pages8 = e4m3_pages(c), rotate = rotation != nullptr;
   switch (c.page_size) {
     case 8: return launch_insert_for<8>(a, pages8, rotate, who, s);
@@ -361,8 +427,8 @@ int launch_rotate_rows(const quest_cache& c, const PackedTokens& p, const quest_
   a.q_stride = x_stride * 2;
   a.q_out_stride = out_stride * 2;
   a.q_heads = heads;
-  const int64_t blocks = (waves_of_rows(a) + kInsertWaves - 1) / kInsertWaves;
-  hipLaunchKernelGGL(rotate_rows_kernel, dim3((unsigned)blocks), dim3(kInsertWaves * kWave), 0, s, a);
+  const int64_t blocks = (waves_of_rows(a) + kRowWaves - 1) / kRowWaves;
+  hipLaunchKernelGGL(rotate_rows_kernel, dim3((unsigned)blocks), dim3(kRowWaves * kWave), 0, s, a);
   return check_launch("quest_rotate_tokens");
 }
 
