@@ -152,6 +152,10 @@ int check_rotation(const quest_rotation* r, const char* who) {
 int attend_e4m3(const quest_cache& c, const void* q, const float* scores, const int32_t* topk_idx, int32_t* topk_out,
                 int32_t* k_eff, int32_t k_pages, float sm_scale, void* out, int32_t out_is_fp16, float* lse, void* workspace,
                 size_t bytes, const char* who, hipStream_t s) {
+  if ((uintptr_t)workspace % 16 != 0) {
+    set_error("%s: workspace must lie on 16 bytes", who);
+    return QUEST_ERR_SHAPE;
+  }
   if (workspace == nullptr) bytes = 0;
   const size_t attention = std::min(bytes, attention_e4m3_bytes(c));
   if (scores != nullptr) {

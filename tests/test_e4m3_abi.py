@@ -131,6 +131,12 @@ def test_steps_of_8_bits_need_scales():
     assert binding.load().quest_decode_step(ctypes.byref(c), None, None, 0, P, 8, 1.0, P, P, None, P, 0, None, None, 0, None) == -1
 
 
+def test_workspaces_off_their_alignment():
+    c, lib = make_cache(flags=E8, scales=P), binding.load()
+    assert lib.quest_sparse_decode(ctypes.byref(c), P, None, 0, 1.0, P, 0, None, P + 8, 1 << 20, None) == -2
+    assert lib.quest_select_decode(ctypes.byref(c), P, P, 8, 1.0, P, None, P, 0, None, P + 4, 1 << 20, None) == -2
+
+
 def test_too_many_heads_and_sequences_for_a_launch():
     c = make_cache(flags=E8, scales=P, batch=65535, num_heads=4096, num_kv_heads=4096)
     assert every_call(c)["quest_sparse_decode"]() == -2

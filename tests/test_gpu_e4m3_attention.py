@@ -215,6 +215,33 @@ def test_selection_and_steps(S, pages, K, heads, kv_heads):
                 assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (8, 2)])
+def test_lengths_past_the_page_table_row(heads, kv_heads):
+    """A sequence is as long as its page-table row at most, whatever its length says."""
+    p = one_query([16 * 30, 700], heads=heads, kv_heads=kv_heads, seed=6)
+    p.table = p.table[:, :30].contiguous()
+    p.describe()
+    p.lens = [480, 480]
+    lists = torch.tensor([3, 29, 30, 31, 1000, 7], dtype=torch.int32, device=p.dev).expand(2, kv_heads, 6).contiguous()
+    for length in (480, 481, 700, 2 ** 31 - 1):
+        p.seq_lens.fill_(length)
+        for these in (None, lists):
+            for ws in ("full", None):
+                check_decode(p, *run_decode(p, False, these, workspace=ws), False, these, what=length)
+    p.seq_lens.fill_(-5)
+    out, lse = run_decode(p, False)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+def test_sequences_that_share_pages():
+    """A common beginning, held once."""
+    p = one_query([900, 900, 500], heads=4, kv_heads=2, seed=8)
+    p.table[1, :40] = p.table[0, :40]
+    p.table[2] = p.table[0, :p.table.shape[1]]
+    p.table_np = p.table.cpu().numpy()
+    check_decode(p, *run_decode(p, False), False)
+
+
 # ---- prompts
 
 def run_prompt(p, half, scale=SCALE, workspace="full"):
@@ -288,8 +315,49 @@ def test_prompt_scales(scale):
             check_prompt(p, *run_prompt(p, half, scale), half, scale, scale)
 
 
-def test_prompt_lengths_past_the_page_table_row():
-    """A sequence is as long as its row at most; one that is shorter than its new tokens spoils nothing else."""
+def test_prompt_workspaces_of_any_size():
+    for new in ([3, 2], [60, 100]):
+        p = Packed8([6000, 3500], new, heads=8, kv_heads=2, seed=4)
+        full = Q.quest_tokens_workspace_bytes(p.cache, p.total)
+        for size in (16, 1 << 20, 5 << 20, full // 2, full):
+            ws = torch.full((size // 4 + 64,), 5.0, device=p.dev)
+            out, lse = p.results(False)
+            Q.quest_prompt_attention(p.cache, p.q, p.cu, SCALE, out, lse=lse, workspace=ws[:size // 4])
+            check_prompt(p, out, lse, False, SCALE, size)
+            assert bool((ws[size // 4:] == 5).all())
+
+
+def test_prompt_of_more_sequences_than_lanes():
+    new = [int(x) for x in np.random.default_rng(0).integers(0, 40, 150)]
+    lens = [n + (7 * i) % 50 + 1 for i, n in enumerate(new)]
+    lens[77] += 3000
+    p = Packed8(lens, new, heads=4, kv_heads=1, seed=6)
+    check_prompt(p, *run_prompt(p, True), True, SCALE)
+
+
+@pytest.mark.parametrize("new", [70, 3])
+def test_prompt_lengths_past_the_row(new):
+    """Queries whose positions lie past the page-table row attend to all that the row has room for."""
+    p = Packed8([480, 900], [new, new], heads=4, kv_heads=2, seed=6)
+    p.table = p.table[:, :30].contiguous()
+    p.describe()
+    want = []
+    for length in (480 + new, 5000):                # the first position is 480 or later
+        p.seq_lens.fill_(length)
+        for half in (True, False):
+            for ws in ("full", None):
+                out, lse = run_prompt(p, half, workspace=ws)
+                p.lens = [480, 480]
+                for b in range(2):
+                    at = p.rows(b)
+                    sees = torch.ones(new, 480, dtype=torch.bool, device=p.dev)
+                    for h in range(4):
+                        k, v = p.cached(b, h // 2)
+                        check(out[at, h], lse[at, h], attention64(p.q[at, h].double(), k, v, sees, SCALE), half, (length, half, ws))
+
+
+def test_prompt_lengths_below_the_new_tokens():
+    """A sequence that is shorter than its new tokens spoils nothing else."""
     p = Packed8([200, 300], [70, 80], heads=4, kv_heads=2, seed=3)
     want = run_prompt(p, False)
     p.seq_lens[0] = 60

@@ -184,12 +184,23 @@ def test_pools_beyond_32_bits():
     x = torch.randn(S + 5, Hkv, D, device=dev).half()
     cu = torch.tensor([0, S + 5], dtype=torch.int32, device=dev)
     Q.quest_append_tokens(cache, x, x, cu)
-    out = torch.empty(1, Hkv, D, device=dev)
-    Q.quest_sparse_decode(cache, torch.zeros(1, Hkv, D, device=dev, dtype=torch.float16), None, 0, 1.0, out)
     scale = cache.scales[[N - 1, N - 2], :, 1].double()
     rows = torch.from_numpy(VALUES).to(dev)[v[[N - 1, N - 2]].long()] * scale[..., None, None]
-    want = torch.cat([rows[0], rows[1, :, :5]], 1).mean(1)
-    assert bool(((rows[0] - x[:S].double().transpose(0, 1)).abs() <= 2.0 ** -4 * x[:S].double().transpose(0, 1).abs() + 2.0 ** -10 * scale[0][:, None, None]).all())
-    size = torch.cat([rows[0], rows[1, :, :5]], 1).abs().mean(1)   # all weights are 1: 69 additions, each off by 2^-24 of a part of the sum
-    assert bool(((out[0].double() - want).abs() <= 69 * 2.0 ** -24 * size + 2.0 ** -24).all())
+    held = torch.cat([rows[0], rows[1, :, :5]], 1)                 # [Hkv][69][D]
+    want, size = held.mean(1), held.abs().mean(1)                  # all weights are 1: 69 additions, each off by 2^-24 of a part of the sum
+    one, last = torch.tensor([0, 1], dtype=torch.int32, device=dev), []
+    for heads in (Hkv, 2 * Hkv):
+        c = Q.Cache(k, v, cache.meta, table, cache.seq_lens, num_heads=heads, scales=cache.scales)
+        q = torch.zeros(1, heads, D, device=dev, dtype=torch.float16)
+        for call in ("decode", "prompt", "listed"):
+            out = torch.full((1, heads, D), 77.0, device=dev)
+            if call == "prompt":
+                Q.quest_prompt_attention(c, q, one, 1.0, out)
+            else:
+                lists = torch.tensor([1, 0], dtype=torch.int32, device=dev).expand(1, Hkv, 2).contiguous()
+                Q.quest_sparse_decode(c, q, lists if call == "listed" else None, 2, 1.0, out)
+            off = (out[0].double().view(Hkv, -1, D) - want[:, None]).abs()
+            assert bool((off <= 69 * 2.0 ** -24 * size[:, None] + 2.0 ** -24).all()), (heads, call)
+    x64 = x.double().transpose(0, 1)
+    assert bool(((rows[0] - x64[:, :S]).abs() <= 2.0 ** -4 * x64[:, :S].abs() + 2.0 ** -10 * scale[0][:, None, None]).all())
     assert int((k != 0).flatten(1).any(1).sum()) == 2
