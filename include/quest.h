@@ -144,8 +144,8 @@ typedef struct quest_cache {
  * pages are selected as with the fp16 cache.
  * Calls on such a cache: quest_append_tokens and quest_rotate_append_tokens fill it (a decode step's token
  * too); quest_estimate and quest_topk as on any cache; quest_sparse_decode, quest_select_decode,
- * quest_decode_step and quest_prompt_attention read it (select and step as launches of
- * their own for each phase).  QUEST_ERR_UNSUPPORTED: quest_build_meta, quest_tree_attention, quest_decode_step_static, and
+ * quest_decode_step, quest_prompt_attention and quest_tree_attention (drafted nodes in fp16) read it (select and step as
+ * launches of their own for each phase).  QUEST_ERR_UNSUPPORTED: quest_build_meta, quest_decode_step_static, and
  * a token's insertion by the single-token calls (k_pool_write != 0).  quest_sparse_decode and its like take any workspace, or
  * NULL, without a refusal: a smaller one makes fewer splits, slower.  Nothing is split where the batch times the KV heads (times parts of eight query
  * heads) is more than 512: a sequence much longer than the others is faster in a call of its own there. */

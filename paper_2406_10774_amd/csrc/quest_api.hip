@@ -542,8 +542,7 @@ int quest_tree_attention(const quest_cache* cache, const void* q, int64_t q_stri
                          int32_t out_is_fp16, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   const char* who = "quest_tree_attention";
   int r = check_packed(cache, cu_tokens, total_tokens, who);
-  if (r != QUEST_OK) return r;
-  if ((r = refuse_e4m3(*cache, "the call", who)) != QUEST_OK || total_tokens == 0) return r;
+  if (r != QUEST_OK || total_tokens == 0) return r;
   if ((r = check_rows(q, q_stride, cache->num_heads, "q", who)) != QUEST_OK) return r;
   if ((r = check_rows(k_new, new_stride, kv_heads(*cache), "k_new", who)) != QUEST_OK) return r;
   if ((r = check_rows(v_new, new_stride, kv_heads(*cache), "v_new", who)) != QUEST_OK) return r;
@@ -560,6 +559,7 @@ int quest_tree_attention(const quest_cache* cache, const void* q, int64_t q_stri
     set_error("%s: mask_words, and k_pages with a page list, must be >= 1 (got %d, %d)", who, mask_words, k_pages);
     return QUEST_ERR_SHAPE;
   }
+  if ((r = check_e4m3(*cache, who)) != QUEST_OK) return r;
   return launch_tree(*cache, {cu_tokens, total_tokens}, q, q_stride, k_new, v_new, new_stride, tree_mask, mask_words, topk_idx,
                      k_pages, sm_scale, out, out_is_fp16 != 0, lse, workspace, workspace_bytes, (hipStream_t)stream);
 }

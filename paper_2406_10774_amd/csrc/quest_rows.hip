@@ -80,7 +80,8 @@ struct Part {
 // ahead changed it by less than 1 %.  (All before the sum of the weights as rounded, 16 instructions of the softmax, which adds 3 to 4 %.)
 //
 // k8: pages of 8 bits.  A wave has eight tokens of a tile, which are on their way to its registers for a whole step: in its turn of
-// softmax of tile t it puts its share of tile t + 2 into LDS as fp16 numbers and asks for that of tile t + 3.
+// softmax of tile t it puts its share of tile t + 2 into LDS as fp16 numbers and asks for that of tile t + 3.  Tiles of drafted nodes, which
+// come last, go straight to LDS as without k8.
 template <bool kTree, bool kExact, bool k8>
 __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -115,26 +116,59 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     return kTree ? walk.held(step, lane) : 0;
   };
   // k8: a wave's eight tokens of a tile, asked for and put into LDS
-  static_assert(!k8 || (!kTree && kTileTokens == 8 * kSharedWaves), "eight tokens a wave");
+  static_assert(!k8 || kTileTokens == 8 * kSharedWaves, "eight tokens a wave");
   uint4 key8, value8;
+  uint64_t held8 = 0;
+  bool under_way = false;   // straight to LDS
+  auto drafted = [&](int step) { return kTree && (w.first_tile + step) * kTileTokens >= w.stream.context; };
   auto ask8 = [&](int step) {
-    if (step >= steps) return;
+    if (step >= steps || drafted(step)) return;
     if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
     walk.load8(a, w.stream, w.hk, step, wave * 8, lane, key8, value8);
+    if (kTree) held8 = walk.held(step, lane);
   };
-  auto put8 = [&](int step) {
-    if (step < steps) walk.put8(walk.scales8(), step, wave * 8, lane, key8, value8, keys(step), values(step));
+  auto put8 = [&](int step) -> uint64_t {
+    if (step >= steps) return 0;
+    if (drafted(step)) {
+      under_way = true;
+      return fetch(step);
+    }
+    walk.put8(walk.scales8(), step, wave * 8, lane, key8, value8, keys(step), values(step));
+    return held8;
+  };
+  auto arrived = [&] {
+    if constexpr (!k8) {
+      dma_arrived<0>();
+    } else if (kTree && under_way) {
+      dma_arrived<0>();
+      under_way = false;
+    }
+  };
+  auto next = [&](int step) -> uint64_t {
+    if constexpr (k8) {
+      const uint64_t of_step = put8(step);
+      ask8(step + 1);
+      return of_step;
+    } else {
+      return fetch(step);
+    }
   };
   if constexpr (k8) {
     walk.find8(a, w.stream, w.hk, 0, lane);
     st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
     ask8(0);
-    const uint4 key0 = key8, value0 = value8;
-    ask8(1);
-    walk.put8(walk.scales8(), 0, wave * 8, lane, key0, value0, keys(0), values(0));
-    put8(1);
+    if constexpr (kTree) {
+      held = put8(0);
+      ask8(1);
+    } else {
+      const uint4 key0 = key8, value0 = value8;
+      ask8(1);
+      walk.put8(walk.scales8(), 0, wave * 8, lane, key0, value0, keys(0), values(0));
+    }
+    held1 = put8(1);
     ask8(2);
     st.ready(a.q_sign);
+    arrived();
   } else {
     walk.find(w.stream, 0, lane);
     st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
@@ -143,18 +177,6 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
     st.ready(a.q_sign);
     dma_arrived<0>();
   }
-  auto arrived = [] {
-    if constexpr (!k8) dma_arrived<0>();
-  };
-  auto next = [&](int step) -> uint64_t {
-    if constexpr (k8) {
-      put8(step);
-      ask8(step + 1);
-      return 0;
-    } else {
-      return fetch(step);
-    }
-  };
   __syncthreads();
   const bool second = wave >= kSharedWaves / 2;
   if (second) __syncthreads();
@@ -283,6 +305,15 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     for (int i = 0; i < kLoads; ++i) token_there[i] = walk.load(a, w.stream, w.hk, step, i * 4, lane, k[i], v[i]);
     if (kTree) held_next = walk.held(step, lane);
   };
+  auto put = [&] {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = i * 4 + (lane >> 4);
+      st16(stage_k + k_place(at, lane & 15), k[i]);
+      st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
+    }
+    lds_in_order();
+  };
   auto fold = [&](int step) {
     const bool masked = !walk.whole(w.stream, held, step, first_position);
     uint64_t allow = ~0ull;
@@ -298,33 +329,38 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     struct Step {
       uint4 k[kEights], v[kEights];
       typename Walk<kTree, kTokens, k8>::Scales8 scales;
+      uint64_t held;
     } at[2];
+    // (the steps over cached tokens, which come before those over drafted nodes)
+    const int cached = kTree ? min(max((w.stream.context - walk.start + walk.stride - 1) / walk.stride, 0), max(steps, 0)) : steps;
     auto load8 = [&](Step& to, int step) {
       if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
 #pragma unroll
       for (int i = 0; i < kEights; ++i) walk.load8(a, w.stream, w.hk, step, i * 8, lane, to.k[i], to.v[i]);
       to.scales = walk.scales8();
+      to.held = kTree ? walk.held(step, lane) : 0;
     };
     walk.find8(a, w.stream, w.hk, 0, lane);
     st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
-    load8(at[0], 0);
-    if (steps > 1) load8(at[1], 1);
+    if (!kTree || cached > 0) load8(at[0], 0);
+    if (cached > 1) load8(at[1], 1);
     st.ready(a.q_sign);
     auto put8 = [&](const Step& from, int step) {
+      held = from.held;
 #pragma unroll
       for (int i = 0; i < kEights; ++i) walk.put8(from.scales, step, i * 8, lane, from.k[i], from.v[i], stage_k, stage_v);
       lds_in_order();
     };
     int step = 0;
 #pragma unroll 1
-    for (; step + 3 < steps; step += 2)
+    for (; step + 3 < cached; step += 2)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         put8(at[j], step + j);
         load8(at[j], step + j + 2);
         fold(step + j);
       }
-    const int rest = steps - step;   // 0 to 3
+    const int rest = cached - step;   // 0 to 3
     if (rest > 0) {
       put8(at[0], step);
       if (rest > 2) load8(at[0], step + 2);
@@ -338,6 +374,13 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
       put8(at[0], step + 2);
       fold(step + 2);
     }
+    if constexpr (kTree)
+      for (step = cached; step < steps; ++step) {
+        load(step);
+        held = held_next;
+        put();
+        fold(step);
+      }
   } else {
     if (steps > 0) walk.find(w.stream, 0, lane);
     st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
@@ -345,13 +388,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     st.ready(a.q_sign);
     for (int step = 0; step < steps; ++step) {
       held = held_next;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = i * 4 + (lane >> 4);
-        st16(stage_k + k_place(at, lane & 15), k[i]);
-        st16(stage_v + v_place(at, lane & 15), token_there[i] ? v[i] : make_uint4(0, 0, 0, 0));
-      }
-      lds_in_order();
+      put();
       if (step + 1 < steps) load(step + 1);
       fold(step);
     }
@@ -670,7 +707,8 @@ int launch_tree(const quest_cache& c, const PackedTokens& p, const void* q, int6
   a.mask = mask;
   a.mask_words = mask_words;
   a.k_pages = k_pages;
-  const auto launch = out_is_fp16 ? launch_rows<true, false> : launch_rows<true, true>;
+  const auto launch = e4m3_pages(c) ? (out_is_fp16 ? launch_rows<true, false, true> : launch_rows<true, true, true>)
+                                    : (out_is_fp16 ? launch_rows<true, false> : launch_rows<true, true>);
   return launch(c, a, p.total, topk_idx, workspace, workspace_bytes, "quest_tree_attention", s);
 }
 

@@ -481,7 +481,7 @@ struct Stream {
 // is in is looked up for many steps at a time, one page (or part of one, where a page is longer than a step) a lane:
 // lane e of the first step's, then the next step's, ..  The lookups' latency, twice a memory access with a list, is
 // then paid once in 16 to 64 steps, and nothing waits for a lookup behind the keys and values under way.
-// k8: pages of 8 bits, whose numbers become fp16 numbers on the way from registers to LDS (prompts only).
+// k8: pages of 8 bits, whose numbers become fp16 numbers on the way from registers to LDS (drafted nodes are fp16 as ever).
 template <bool kTree, int kPlaces, bool k8 = false>
 struct Walk {
   int start, stride;
@@ -521,8 +521,9 @@ struct Walk {
   }
   __device__ __forceinline__ void find8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int lane) {
     find(s, step, lane);
+    const int at = start + (step + (lane >> per_step_log2)) * stride + ((lane & ((1 << per_step_log2) - 1)) << shift);
     scale = make_float2(1.f, 1.f);   // (a page without tokens may have any)
-    if (left > 0) scale = a.scales[(size_t)phys * a.kv_heads + hk];
+    if (left > 0 && (!kTree || at < s.context)) scale = a.scales[(size_t)phys * a.kv_heads + hk];
   }
   // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15; zeros where there
   // is no token.

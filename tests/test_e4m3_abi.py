@@ -110,7 +110,7 @@ def every_call(c):
 
 
 @pytest.mark.parametrize("name", ["quest_build_meta", "quest_append_meta", "quest_append_estimate", "quest_decode_step",
-                                  "quest_decode_step_static", "quest_tree_attention"])
+                                  "quest_decode_step_static"])
 def test_calls_that_know_fp16_pages_only(name):
     assert every_call(make_cache(flags=E8, scales=P))[name]() == -3
     message = binding.load().quest_last_error()
@@ -118,7 +118,7 @@ def test_calls_that_know_fp16_pages_only(name):
 
 
 @pytest.mark.parametrize("name", ["quest_append_tokens", "quest_rotate_append_tokens", "quest_prompt_attention",
-                                  "quest_sparse_decode", "quest_select_decode"])
+                                  "quest_tree_attention", "quest_sparse_decode", "quest_select_decode"])
 @pytest.mark.parametrize("cache,status", [(dict(scales=None), -1), (dict(scales=P + 4), -2), (dict(scales=P, k_pool=P + 8), -2),
                                           (dict(scales=P, v_pool=P + 1), -2)])
 def test_pools_of_8_bits(name, cache, status):
