@@ -181,10 +181,7 @@ class Cache:
             num_kv_heads=0 if H == Hkv else Hkv, scales=None if scales is None else scales.data_ptr())
         self.heads, self.kv_heads, self.batch, self.head_dim = H, Hkv, page_table.shape[0], D
         self.device = k_pool.get_device()
-
-    @property
-    def ref(self):
-        return ctypes.byref(self.c)
+        self.ref = ctypes.byref(self.c)
 
 
 class Rotation:
@@ -205,10 +202,7 @@ class Rotation:
         self.device = table.get_device()
         self.c = quest_rotation(table=table.data_ptr(), positions=_ptr(positions), num_positions=table.shape[0],
                                 rotary_dim=table.shape[1], interleaved=int(bool(interleaved)))
-
-    @property
-    def ref(self):
-        return ctypes.byref(self.c)
+        self.ref = ctypes.byref(self.c)
 
 
 def quest_workspace_bytes(cache: Cache, k_pages: int) -> int:
@@ -306,12 +300,17 @@ def _types_of_torch():
 
 def _rows_of(cache, shape, t, heads, other=None):
     """Elements between the rows of t (its shape, t), and of `other`: fp16 rows whose heads lie next to each other."""
-    stride, dim, device = t.stride(), cache.head_dim, cache.device
-    if (t.dtype is _half and len(shape) == 3 and shape[1] == heads and shape[2] == dim and stride[2] == 1
-            and (stride[1] == dim or heads == 1) and t.get_device() == device
-            and (other is None or other.dtype is _half and other.stride() == stride and other.shape == shape
-                 and other.get_device() == device)):
-        return stride[0] if shape[0] > 1 else heads * dim
+    dim, device = cache.head_dim, cache.device
+    if len(shape) == 3 and shape[1] == heads and shape[2] == dim and t.dtype is _half and t.get_device() == device:
+        if t.is_contiguous() and (other is None or other.dtype is _half and other.is_contiguous() and other.shape == shape
+                                  and other.get_device() == device):
+            return heads * dim
+        stride = t.stride()
+        if stride[2] == 1 and (stride[1] == dim or heads == 1) and (
+                other is None or other.dtype is _half and other.stride() == stride and other.shape == shape
+                and other.get_device() == device):
+            return stride[0] if shape[0] > 1 else heads * dim
+    stride = t.stride()
     what = "" if other is None else f", {tuple(other.shape)} and {other.stride()} ({other.dtype}, {other.device})"
     raise QuestError(-2, f"packed rows of shape {tuple(shape)} and strides {stride} ({t.dtype}, {t.device}){what}: they have to "
                          f"be fp16 [rows][{heads}][{dim}] on the cache's device, heads next to each other, keys as values")
@@ -423,13 +422,13 @@ def quest_rotate_append_tokens(cache: Cache, rotation: Rotation, q, k_new, v_new
     shape = k_new.shape
     stride = _rows_of(cache, shape, k_new, cache.kv_heads, v_new)
     total, q_stride, out_stride = shape[0], 0, 0
-    if (q is None) != (q_out is None):
-        raise QuestError(-1, "q and q_out: both or neither")
-    if q is not None:
-        q_shape, out_shape = q.shape, q_out.shape
-        q_stride, out_stride = _rows_of(cache, q_shape, q, cache.heads), _rows_of(cache, out_shape, q_out, cache.heads)
+    if q is not None and q_out is not None:
+        q_shape, out_shape, heads = q.shape, q_out.shape, cache.heads
+        q_stride, out_stride = _rows_of(cache, q_shape, q, heads), _rows_of(cache, out_shape, q_out, heads)
         if q_shape[0] < total or out_shape[0] < total:
             raise QuestError(-2, f"{q_shape[0]} rows of queries and {out_shape[0]} of results for {total} of keys")
+    elif q is not None or q_out is not None:
+        raise QuestError(-1, "q and q_out: both or neither")
     _rotation_of(cache, rotation, total)
     _plain(cache, cu_tokens, i32, cache.batch + 1, "cu_tokens")
     _check(load().quest_rotate_append_tokens(
