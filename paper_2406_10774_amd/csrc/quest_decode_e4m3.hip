@@ -445,8 +445,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_e4m3_kernel(const Dec
         const int at = step * kEights + e;
         const uint32_t first = (uint32_t)__builtin_amdgcn_readlane(block, at);
         const int n = __builtin_amdgcn_readlane(bytes, at);
-        to.k[e] = row16(rows_at(a.k_pool, first, n), lane);
-        to.v[e] = row16(rows_at(a.v_pool, first, n), lane);
+        to.k[e] = row16<true>(rows_at(a.k_pool, first, n), lane);
+        to.v[e] = row16<true>(rows_at(a.v_pool, first, n), lane);
       }
     };
     Found next = find(0);

@@ -65,8 +65,10 @@ __device__ __forceinline__ int exponent_of(float scale) { return (int)(__builtin
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* pool, uint32_t block, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool) + (size_t)block * (8 * kRowBytes8), 0, bytes, 0x00020000);
 }
+// kOnce: non-temporal, for what a launch reads once.
+template <bool kOnce>
 __device__ __forceinline__ uint4 row16(__amdgpu_buffer_rsrc_t rows, int lane) {
-  const auto v = __builtin_amdgcn_raw_buffer_load_b128(rows, lane * 16, 0, 2);   // (non-temporal)
+  const auto v = __builtin_amdgcn_raw_buffer_load_b128(rows, lane * 16, 0, kOnce ? 2 : 0);
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kSharedWaves* kWave, 2) void shared_rows_kernel(
   auto ask8 = [&](int step) {
     if (step >= steps || drafted(step)) return;
     if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
-    walk.load8(a, w.stream, w.hk, step, wave * 8, lane, key8, value8);
+    walk.template load8<false>(a, w.stream, w.hk, step, wave * 8, lane, key8, value8);
     if (kTree) held8 = walk.held(step, lane);
   };
   auto put8 = [&](int step) -> uint64_t {
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     auto load8 = [&](Step& to, int step) {
       if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
 #pragma unroll
-      for (int i = 0; i < kEights; ++i) walk.load8(a, w.stream, w.hk, step, i * 8, lane, to.k[i], to.v[i]);
+      for (int i = 0; i < kEights; ++i) walk.template load8<true>(a, w.stream, w.hk, step, i * 8, lane, to.k[i], to.v[i]);
       to.scales = walk.scales8();
       to.held = kTree ? walk.held(step, lane) : 0;
     };

@@ -526,7 +526,9 @@ struct Walk {
     if (left > 0 && (!kTree || at < s.context)) scale = a.scales[(size_t)phys * a.kv_heads + hk];
   }
   // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15; zeros where there
-  // is no token.
+  // is no token.  kOnce: past the caches (few rows: one token a head at 32k of 32 heads 55 us, else 61; many row tiles, which read the same
+  // tokens at about the same time: 32k of 32 / 8 heads 8.9 ms, else 9.0).
+  template <bool kOnce>
   __device__ __forceinline__ void load8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int eight, int lane,
                                         uint4& key, uint4& value) const {
     const int from = ((step - first_step) << per_step_log2) + (eight >> shift);
@@ -537,8 +539,8 @@ struct Walk {
     // (the same in all lanes, which the compiler does not see)
     const uint32_t of_wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)block);
     const int bytes = __builtin_amdgcn_readfirstlane(tokens * kRowBytes8);
-    key = row16(rows_at(a.k_pool, of_wave, bytes), lane);
-    value = row16(rows_at(a.v_pool, of_wave, bytes), lane);
+    key = row16<kOnce>(rows_at(a.k_pool, of_wave, bytes), lane);
+    value = row16<kOnce>(rows_at(a.v_pool, of_wave, bytes), lane);
   }
   // What load8 brought, as fp16 numbers into LDS (k, v: the tile).  `of`: the scales as they were then.
   struct Scales8 {
@@ -552,8 +554,12 @@ struct Walk {
     const int token = eight + (lane >> 3), slot = (lane & 7) * 2;
     st16(k + k_place(token, slot), halves_of(make_uint2(key.x, key.y), k_scale));
     st16(k + k_place(token, slot + 1), halves_of(make_uint2(key.z, key.w), k_scale));
-    st16(v + v_place(token, slot), halves_of(make_uint2(value.x, value.y), v_scale));
-    st16(v + v_place(token, slot + 1), halves_of(make_uint2(value.z, value.w), v_scale));
+    // (two tokens' values go to LDS at a time: their even chunks and their odd ones, so that all banks are met)
+    const int odd = token & 1;
+    const uint2 a = odd ? make_uint2(value.z, value.w) : make_uint2(value.x, value.y);
+    const uint2 b = odd ? make_uint2(value.x, value.y) : make_uint2(value.z, value.w);
+    st16(v + v_place(token, slot + odd), halves_of(a, v_scale));
+    st16(v + v_place(token, slot + 1 - odd), halves_of(b, v_scale));
   }
   // 16 bytes of the key and of the value of the step's place `four` + lane / 16 (`four`: a multiple of 4).  Returns whether
   // there is a token; if not, the value has to be zeroed when it has arrived: stale slots may hold anything, and
