@@ -11,6 +11,7 @@
 // leaves partial results, which merge_rows_kernel joins (a launch of its own: 4 to 7 us, and up to 95 splits are
 // joined by as many work-groups as there are rows, not by the last one to arrive).
 #include <algorithm>
+#include <type_traits>
 
 #include "quest_common.h"
 #include "quest_decode_core.h"
@@ -274,8 +275,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     const RowsArgs a, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ topk, const int64_t* __restrict__ mask) {
   constexpr int kTokens = 32, kLoads = kTokens / 4;
-  constexpr int kStride = kHeadDim + 4;
-  constexpr int kStage = 2 * kTokens * kRowBytes, kJoin = kFewRows * kStride * 4;
+  constexpr int kPasses = k8 && !kTree ? 2 : 1;   // of the waves' join
+  constexpr int kStride = kHeadDim / kPasses + 4;
+  constexpr int kStage = 2 * kTokens * (k8 && !kTree ? kRowBytes8 : kRowBytes), kJoin = kFewRows * kStride * 4;
   __shared__ __align__(16) char lds[kWaves * (kStage > kJoin ? kStage : kJoin)];
   __shared__ float ml[2][kWaves][kFewRows];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -323,56 +325,54 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     lds_in_order();
   };
   if constexpr (k8) {
-    // Pages of 8 bits: two steps on their way in the registers of one.  (No load of the loop is ever skipped, so that the compiler knows
-    // how many are under way.)
+    // Pages of 8 bits: tiles lie in LDS as they came and become fp16 numbers on the way to a product, each number once, as a wave has all of
+    // a tile's rows: half the LDS traffic of fp16 tiles.  26 tokens at 32k of 32 heads 57 us, with fp16 tiles 64 (40 heads, 9 to 77 tokens behind 35 to 2600:
+    // 38.6 and 44.2); two steps under way 64 (registers spill); three work-groups on a compute unit, with queries in LDS, 63.
+    // (No load of the loop is ever skipped, so that the compiler knows how many are under way.)
     constexpr int kEights = kTokens / 8;
-    struct Step {
-      uint4 k[kEights], v[kEights];
-      typename Walk<kTree, kTokens, k8>::Scales8 scales;
-      uint64_t held;
-    } at[2];
     // (the steps over cached tokens, which come before those over drafted nodes)
     const int cached = kTree ? min(max((w.stream.context - walk.start + walk.stride - 1) / walk.stride, 0), max(steps, 0)) : steps;
-    auto load8 = [&](Step& to, int step) {
+    char* stage_v8 = stage_k + kTokens * kRowBytes8;
+    auto load8 = [&](int step) {
       if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
 #pragma unroll
-      for (int i = 0; i < kEights; ++i) walk.template load8<true>(a, w.stream, w.hk, step, i * 8, lane, to.k[i], to.v[i]);
-      to.scales = walk.scales8();
-      to.held = kTree ? walk.held(step, lane) : 0;
+      for (int i = 0; i < kEights; ++i) walk.template load8<true>(a, w.stream, w.hk, step, i * 8, lane, k[i], v[i]);
+    };
+    float k_scale, v_scale[2];   // of the lane's key, of its values
+    auto put8 = [&](int step) {
+#pragma unroll
+      for (int i = 0; i < kEights; ++i) walk.put_codes(i * 8, lane, k[i], v[i], stage_k, stage_v8);
+      k_scale = walk.scale_of_lane(walk.scale.x, step, st.token8(lane & 31) & 24);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v_scale[i] = walk.scale_of_lane(walk.scale.y, step, 16 * i + (lane >> 5) * 8);
+      if (kTree) held = walk.held(step, lane);
+      lds_in_order();
+    };
+    auto fold8 = [&](int step) {
+      f32x16_t s[1];
+      st.logits8(s, stage_k, k_scale, lane);
+      if (!walk.whole(w.stream, held, step, first_position))
+        st.hide8(s, (uint32_t)walk.allow(w.stream, held, step, w.past + token, mask + (int64_t)(w.s.first + token) * a.mask_words,
+                                         a.mask_words), lane);
+      typename RowState<true, false>::template Weights<1> p;
+      st.template weigh<1>(p, s, a);
+      st.add8(p, stage_v8, v_scale, lane);
+      lds_in_order();
     };
     walk.find8(a, w.stream, w.hk, 0, lane);
     st.init(a.q + (int64_t)(w.s.first + token) * a.q_stride + (int64_t)head * kRowBytes, lane);
-    if (!kTree || cached > 0) load8(at[0], 0);
-    if (cached > 1) load8(at[1], 1);
+    if (!kTree || cached > 0) load8(0);
     st.ready(a.q_sign);
-    auto put8 = [&](const Step& from, int step) {
-      held = from.held;
-#pragma unroll
-      for (int i = 0; i < kEights; ++i) walk.put8(from.scales, step, i * 8, lane, from.k[i], from.v[i], stage_k, stage_v);
-      lds_in_order();
-    };
     int step = 0;
 #pragma unroll 1
-    for (; step + 3 < cached; step += 2)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        put8(at[j], step + j);
-        load8(at[j], step + j + 2);
-        fold(step + j);
-      }
-    const int rest = cached - step;   // 0 to 3
-    if (rest > 0) {
-      put8(at[0], step);
-      if (rest > 2) load8(at[0], step + 2);
-      fold(step);
+    for (; step + 1 < cached; ++step) {
+      put8(step);
+      load8(step + 1);
+      fold8(step);
     }
-    if (rest > 1) {
-      put8(at[1], step + 1);
-      fold(step + 1);
-    }
-    if (rest > 2) {
-      put8(at[0], step + 2);
-      fold(step + 2);
+    if (step < cached) {
+      put8(step);
+      fold8(step);
     }
     if constexpr (kTree)
       for (step = cached; step < steps; ++step) {
@@ -399,53 +399,61 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   float* join = reinterpret_cast<float*>(lds);
   const float total = st.total();
   float* mine = join + (wave * kFewRows + (lane & 31)) * kStride;
-  st.each4(RowState<true, false>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + d) = o; });
   if (lane < kFewRows) {
     ml[0][wave][lane] = total > 0.f ? st.base : kNegBig;
     ml[1][wave][lane] = total;
   }
-  __syncthreads();
-  const int in_tile = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * 16;
+  constexpr int kFours = 4 / kPasses;
+  const int in_tile = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * (4 * kFours);
   const int row = w.row0 + in_tile;
-  if (row >= w.rows) return;
-  float top = kNegBig, sum = 0.f, weight[kWaves];
+  auto pass = [&](auto which) {
+    constexpr int kFirst = decltype(which)::value * (kHeadDim / kPasses);
+    if (kFirst > 0) __syncthreads();
+    st.template each4<kFirst / 32, (kFirst + kHeadDim / kPasses) / 32>(
+        RowState<true, false>::kUnscale, lane, [&](int d, float4 o) { *reinterpret_cast<float4*>(mine + (d - kFirst)) = o; });
+    __syncthreads();
+    if (row >= w.rows) return;
+    float top = kNegBig, sum = 0.f, weight[kWaves];
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[0][i][in_tile]);
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    weight[i] = __builtin_amdgcn_exp2f((ml[0][i][in_tile] - top) * a.scale);
-    sum += weight[i] * ml[1][i][in_tile];
-  }
-  float4 o[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[0][i][in_tile]);
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      const float4 x = *reinterpret_cast<const float4*>(join + (i * kFewRows + in_tile) * kStride + d0 + 4 * j);
-      o[j].x += weight[i] * x.x, o[j].y += weight[i] * x.y, o[j].z += weight[i] * x.z, o[j].w += weight[i] * x.w;
+      weight[i] = __builtin_amdgcn_exp2f((ml[0][i][in_tile] - top) * a.scale);
+      sum += weight[i] * ml[1][i][in_tile];
     }
-  }
-  if (!w.whole()) {
-    const size_t part = w.part_row(a, in_tile);
+    float4 o[kFours];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + d0 + 4 * j) = o[j];
-    if (d0 == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(top, sum);
-    return;
-  }
-  const int tok = row / a.group;
-  const size_t out_row = (size_t)(w.s.first + tok) * (a.kv_heads * a.group) + w.hk * a.group + (row - tok * a.group);
-  const float factor = sum > 0.f ? 1.f / sum : 0.f;
+    for (int j = 0; j < kFours; ++j) {
+      o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float4 v = make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor);
-    const size_t at = out_row * kHeadDim + d0 + 4 * j;
-    if constexpr (kHalfOut)
-      store_halves((_Float16*)a.out + at, v);
-    else
-      *reinterpret_cast<float4*>((float*)a.out + at) = v;
-  }
-  if (a.lse != nullptr && d0 == 0) a.lse[out_row] = st.lse(top, sum, a.scale);
+      for (int i = 0; i < kWaves; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(join + (i * kFewRows + in_tile) * kStride + d0 + 4 * j);
+        o[j].x += weight[i] * x.x, o[j].y += weight[i] * x.y, o[j].z += weight[i] * x.z, o[j].w += weight[i] * x.w;
+      }
+    }
+    if (!w.whole()) {
+      const size_t part = w.part_row(a, in_tile);
+#pragma unroll
+      for (int j = 0; j < kFours; ++j) *reinterpret_cast<float4*>(a.part_acc + part * kHeadDim + kFirst + d0 + 4 * j) = o[j];
+      if (kFirst == 0 && d0 == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(top, sum);
+      return;
+    }
+    const int tok = row / a.group;
+    const size_t out_row = (size_t)(w.s.first + tok) * (a.kv_heads * a.group) + w.hk * a.group + (row - tok * a.group);
+    const float factor = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int j = 0; j < kFours; ++j) {
+      const float4 v = make_float4(o[j].x * factor, o[j].y * factor, o[j].z * factor, o[j].w * factor);
+      const size_t at = out_row * kHeadDim + kFirst + d0 + 4 * j;
+      if constexpr (kHalfOut)
+        store_halves((_Float16*)a.out + at, v);
+      else
+        *reinterpret_cast<float4*>((float*)a.out + at) = v;
+    }
+    if (a.lse != nullptr && kFirst == 0 && d0 == 0) a.lse[out_row] = st.lse(top, sum, a.scale);
+  };
+  pass(std::integral_constant<int, 0>());
+  if constexpr (kPasses > 1) pass(std::integral_constant<int, 1>());
 }
 
 // The partial results: a wave has some rows, one after the other, a lane a split for the weights, then two channels a

@@ -218,6 +218,9 @@ __device__ __forceinline__ bool find_sequence(Sequence& s, const RowsArgs& a, co
   return false;
 }
 
+// Where the 16-byte chunk `slot` of a token's 8-bit key or value lies in its LDS tile.
+__device__ __forceinline__ int place8(int token, int slot) { return token * kRowBytes8 + ((slot ^ ((token >> 1) & 7)) << 4); }
+
 // Attention state of a wave's 32 rows; lane l: row l % 32.  Weights are 2^(scale (s - base)), s the logit before the scale
 // and base close below the largest one: the difference first, which is exact near it, so that logits of any size keep
 // their order.  kShifted: the products that make the logits start at -base, which costs 16 registers and no instruction.
@@ -380,6 +383,44 @@ struct RowState {
     add(p, v, lane);
   }
 
+  // The same for 32 tokens that lie in LDS as 8-bit numbers, rows of 128 bytes (place8).  Row m = 8 i + 4 h + j of the first product is
+  // token 16 (i / 2) + 8 h + 4 (i % 2) + j, so that a lane's weights are of tokens 8 h ..+7 and 16 + 8 h ..+7: eight of one page each, whose values
+  // (turned by the LDS read, eight tokens of a channel) have one scale.
+  __device__ __forceinline__ static int token8(int row) { return (row & 16) | ((row & 4) << 1) | ((row & 8) >> 1) | (row & 3); }
+  __device__ __forceinline__ void logits8(f32x16_t (&s)[1], const char* k, float scale, int lane) const {
+    const int token = token8(lane & 31);
+    const char* k_lane = k + (lane >> 5) * 8;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint2 codes = *reinterpret_cast<const uint2*>(k_lane + place8(token, i));
+      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, halves_of(codes, scale)), q[i], s[0], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ static void hide8(f32x16_t (&s)[1], uint32_t allow, int lane) {
+    const uint32_t bits = allow >> ((lane >> 5) * 8);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (!(bits >> (16 * (r / 8) + r % 8) & 1)) s[0][r] = -INFINITY;
+  }
+  __device__ __forceinline__ void add8(const Weights<1>& p, const char* v, const float (&scale)[2], int lane) {
+    typedef int int2_t __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) int2_t lds_int2_t;
+    const int token = (lane >> 5) * 8 + ((lane & 15) >> 1), slot = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const int2_t codes =
+            __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2_t*)(v + place8(16 * i + token, 2 * d + slot) + (lane & 1) * 8));
+        const half8_t value =
+            __builtin_bit_cast(half8_t, halves_of(make_uint2((uint32_t)codes.x, (uint32_t)codes.y), scale[i]));
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, p.w[i], acc[d], 0, 0, 0);
+        if constexpr (kExact) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, p.rest[i], acc[d], 0, 0, 0);
+      }
+  }
+
   // The row's whole sum, and that of the weights that its values met.
   __device__ __forceinline__ float total() const { return both_halves(l); }
   __device__ __forceinline__ float total_met() const { return both_halves(kExact ? l : met); }
@@ -393,11 +434,11 @@ struct RowState {
   }
   static constexpr float kUnscale = kExact ? 1.f / kWeightScale : 1.f;
 
-  // Channels of the lane's accumulators, four at a time: f(channel, four values).
-  template <class F>
+  // Channels 32 kFrom to 32 kTo of the lane's accumulators, four at a time: f(channel, four values).
+  template <int kFrom = 0, int kTo = 4, class F>
   __device__ __forceinline__ void each4(float factor, int lane, F f) const {
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int d = kFrom; d < kTo; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
         f(d * 32 + 2 * r + (lane >> 5) * 4,
@@ -481,7 +522,8 @@ struct Stream {
 // is in is looked up for many steps at a time, one page (or part of one, where a page is longer than a step) a lane:
 // lane e of the first step's, then the next step's, ..  The lookups' latency, twice a memory access with a list, is
 // then paid once in 16 to 64 steps, and nothing waits for a lookup behind the keys and values under way.
-// k8: pages of 8 bits, whose numbers become fp16 numbers on the way from registers to LDS (drafted nodes are fp16 as ever).
+// k8: pages of 8 bits, whose numbers become fp16 numbers on the way from registers to LDS (many row tiles) or from LDS to the products (few);
+// drafted nodes are fp16 as ever.
 template <bool kTree, int kPlaces, bool k8 = false>
 struct Walk {
   int start, stride;
@@ -527,7 +569,7 @@ struct Walk {
   }
   // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15; zeros where there
   // is no token.  kOnce: past the caches (few rows: one token a head at 32k of 32 heads 55 us, else 61; many row tiles, which read the same
-  // tokens at about the same time: 32k of 32 / 8 heads 8.9 ms, else 9.0).
+  // tokens at about the same time: 32k of 32 / 8 heads 8.8 ms, else 9.0).
   template <bool kOnce>
   __device__ __forceinline__ void load8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int eight, int lane,
                                         uint4& key, uint4& value) const {
@@ -542,12 +584,22 @@ struct Walk {
     key = row16<kOnce>(rows_at(a.k_pool, of_wave, bytes), lane);
     value = row16<kOnce>(rows_at(a.v_pool, of_wave, bytes), lane);
   }
-  // What load8 brought, as fp16 numbers into LDS (k, v: the tile).  `of`: the scales as they were then.
+  // What load8 brought, into LDS (k, v: the tile), as it is or as fp16 numbers.  `of`: the scales as they were then.
   struct Scales8 {
     float2 scale;
     int first_step;
   };
   __device__ __forceinline__ Scales8 scales8() const { return {scale, first_step}; }
+  __device__ __forceinline__ static void put_codes(int eight, int lane, uint4 key, uint4 value, char* k, char* v) {
+    const int at = place8(eight + (lane >> 3), lane & 7);
+    st16(k + at, key);
+    st16(v + at, value);
+  }
+  // The scale (`of`: the keys' or the values') of the step's place `eight`, a lane's own.
+  __device__ __forceinline__ float scale_of_lane(float of, int step, int eight) const {
+    const int from = ((step - first_step) << per_step_log2) + (eight >> shift);
+    return as_f((uint32_t)__builtin_amdgcn_ds_bpermute(from * 4, (int)as_u(of)));
+  }
   __device__ __forceinline__ void put8(const Scales8& of, int step, int eight, int lane, uint4 key, uint4 value, char* k, char* v) const {
     const int from = ((step - of.first_step) << per_step_log2) + (eight >> shift);
     const float k_scale = from_lane(of.scale.x, from), v_scale = from_lane(of.scale.y, from);
