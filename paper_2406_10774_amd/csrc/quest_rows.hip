@@ -635,8 +635,14 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   const int r = check_launch(who);
   if (r != QUEST_OK || p.most_units == 0) return r;
   const unsigned tiles = (unsigned)(p.row_tiles * a.kv_heads);
-  if (p.rows == kFewRows && tiles <= 64)
+  // Few rows: work-groups of as few of them as the compute units take at once, 2048 work-groups, so that a wave has one row, two or four.
+  // Four times 16 nodes over 128 listed pages of 32 / 8 heads (96 row tiles) 22.9 us with four rows, 26.0 with 16; 40 heads, 77 tokens behind 2600
+  // (280 row tiles) 50.2 with four rows, 47.5 with eight, 48.7 with 16.
+  if (p.rows == kFewRows && tiles <= 256)
     hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 4>), dim3(tiles * (kFewRows / 4)), dim3(256), 0, s, a, a.cu,
+                       a.seq_lens, topk);
+  else if (p.rows == kFewRows && tiles <= 512)
+    hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 8>), dim3(tiles * (kFewRows / 8)), dim3(256), 0, s, a, a.cu,
                        a.seq_lens, topk);
   else if (p.rows == kFewRows)
     hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 16>), dim3(tiles * (kFewRows / 16)), dim3(256), 0, s, a, a.cu,
