@@ -136,7 +136,7 @@ __device__ __forceinline__ void turn_rows(const InsertArgs& a, int64_t at, int l
   const int64_t four = at / groups;
   const int head0 = (int)(at - four * groups) * kQHeads;
   if (four * 4 >= a.total) return;
-  const int row0 = (int)four * 4, rows_there = a.cu[a.batch];
+  const int row0 = (int)four * 4, rows_there = min(a.cu[a.batch], a.total);
   if (row0 >= rows_there) return;
   const int row = min(row0 + sub, rows_there - 1);
   const bool mine = row0 + sub < rows_there;
