@@ -36,21 +36,29 @@ struct DecodeArgs : AttnArgs {
 };
 
 // The tiles of all sequences, one after the other, are one line that is cut into shares of `length` tiles.  A sequence has a tile at
-// least.
+// least.  A list is taken to have as many entries as its sequence has pages at most (more only if it names a page twice: the last
+// share sees to those).
+// A share that ends one sequence and begins the next does two lookups and leaves two results, which takes longer than a few
+// tiles: where shares up to kMore tiles longer are enough for every sequence to begin a share of its own, the line has gaps and they do
+// (up to 16 sequences; five of 831 to 1066 tokens by 8 KV heads 11.5 -> 8.9 us, of 16 / 8 heads 13.3 -> 10.3, 12 of 525 to 2763 of 32 / 8 heads 19.2 -> 15.6, four
+// of 16k 32.0 -> 28.8).
 struct Line {
+  static constexpr int kMore = 3;
   int length;
   int b, seq_len, first, tiles;   // the sequence that the share begins in: its first tile on the line, and how many it has
+  int span;                       // its tiles with the gap behind them
 
   template <int kTile>
   __device__ __forceinline__ static int tiles_of(const DecodeArgs& a, int seq_len) {
-    const int tokens = a.topk != nullptr ? a.listed << a.page_shift : min(max(seq_len, 0), a.max_pages << a.page_shift);
+    int tokens = min(max(seq_len, 0), a.max_pages << a.page_shift);
+    if (a.topk != nullptr) tokens = min((tokens + (1 << a.page_shift) - 1) >> a.page_shift, a.listed) << a.page_shift;
     return max((tokens + kTile - 1) / kTile, 1);
   }
   template <int kTile>
   __device__ __forceinline__ void at(const DecodeArgs& a, int sequence) {
     b = sequence;
     seq_len = a.seq_lens[b];
-    tiles = tiles_of<kTile>(a, seq_len);
+    tiles = span = tiles_of<kTile>(a, seq_len);
   }
   // Where share `share` begins; false: behind the line's end.
   template <int kTile>
@@ -79,19 +87,34 @@ struct Line {
       longest = max(longest, largest_of_wave(mine));
     }
     length = share_length(a, total, longest);
+    int spans = mine;
+    if (a.batch <= 16) {   // lane 16 j + b: shares that sequence b takes if they are j tiles longer
+      const int tiles_here = __builtin_amdgcn_ds_bpermute((lane & 15) * 4, mine), longer = length + (lane >> 4);
+      const float needed = row16_sum((float)((tiles_here + longer - 1) / longer));
+      const unsigned long long enough = __ballot(needed <= (float)a.shares && (lane >> 4) <= kMore);
+      if (enough != 0) {
+        length += __builtin_ctzll(enough) >> 4;
+        spans = (mine + length - 1) / length * length;
+        total = __builtin_amdgcn_readlane(up_to_lane(spans, lane), kWave - 1);
+      }
+    }
     const int64_t begin = (int64_t)share * length;
     if (begin >= total) return false;
     first = 0;
     for (int base = 0; base < a.batch; base += kWave) {
-      if (a.batch > kWave) read(base);
-      const int end = up_to_lane(mine, lane) + first;
+      if (a.batch > kWave) {
+        read(base);
+        spans = mine;
+      }
+      const int end = up_to_lane(spans, lane) + first;
       const unsigned long long behind = __ballot(end > begin);
       if (behind != 0) {
         const int l = __builtin_ctzll(behind);
         b = base + l;
         seq_len = __builtin_amdgcn_readlane(seq_len, l);
         tiles = __builtin_amdgcn_readlane(mine, l);
-        first = __builtin_amdgcn_readlane(end, l) - tiles;
+        span = __builtin_amdgcn_readlane(spans, l);
+        first = __builtin_amdgcn_readlane(end, l) - span;
         return true;
       }
       first = __builtin_amdgcn_readlane(end, kWave - 1);
@@ -391,7 +414,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_e4m3_kernel(const Dec
     // The share's part of sequence b: its tiles [first_tile, end_tile), the whole or one of `parts`.
     const int b = line.b, seq_len = min(max(line.seq_len, 0), a.max_pages << a.page_shift);
     const int first_tile = (int)max(begin - line.first, (int64_t)0);
-    const int end_tile = (int)min(begin + line.length - line.first, (int64_t)line.tiles);
+    int end_tile = (int)min(begin + line.length - line.first, (int64_t)line.tiles);
     const int share0 = line.first / line.length, parts = (line.first + line.tiles - 1) / line.length - share0 + 1;
     const size_t out_row = (size_t)b * a.num_heads + (size_t)hk * a.group + head0;
 
@@ -400,6 +423,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_e4m3_kernel(const Dec
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
     const int32_t* list = a.topk != nullptr ? a.topk + ((size_t)b * a.kv_heads + hk) * a.k_pages : nullptr;
     const int seq_pages = (seq_len + (1 << a.page_shift) - 1) >> a.page_shift;
+    if (list != nullptr && end_tile == line.tiles) {   // entries that are not counted in the sequence's tiles
+      bool more = false;
+      for (int base = (end_tile * kTile) >> a.page_shift; base < a.listed; base += 4 * kWave)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int page = list[min(base + i * kWave + lane, a.listed - 1)];
+          more = more || (base + i * kWave + lane < a.listed && page >= 0 && page < seq_pages);
+        }
+      if (__ballot(more)) end_tile = ((a.listed << a.page_shift) + kTile - 1) / kTile;
+    }
     // Places of kPlaceSteps steps at a time, those of the next in three parts while the wave is at these: the list's and the page
     // table's entries two ahead, the scales one.
     constexpr int kPlaceSteps = kWave / kEights, kTurns = kPlaceSteps / kRing;   // turns: of the ring
@@ -613,7 +646,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_e4m3_kernel(const Dec
       }
     }
     // The next sequence, if the share goes on in it.
-    const int64_t end = (int64_t)line.first + line.tiles;
+    const int64_t end = (int64_t)line.first + line.span;
     if (a.shares == 0 || end >= begin + line.length || b + 1 >= a.batch) return;
     line.first = (int)end;
     line.at<kTile>(a, b + 1);

@@ -94,6 +94,35 @@ def test_lists(S, K, heads, kv_heads):
                 check_decode(p, *run_decode(p, half, t, workspace=ws), half, t, what=(S, K, half, ws))
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (8, 2)])
+@pytest.mark.parametrize("batch", [1, 4, 17, 300])
+def test_lists_with_more_entries_than_pages(batch, heads, kv_heads):
+    """Every entry a page of its sequence, most of them many times; only the last one; only those behind the first 64."""
+    rng = np.random.default_rng(batch)
+    lens = [int(rng.integers(1, 200)) for _ in range(batch)]
+    K = 333
+    p = one_query(lens, heads=heads, kv_heads=kv_heads, S=8, seed=batch, room=8 * K)
+    full = np.stack([rng.integers(0, -(-n // 8), (kv_heads, K)) for n in lens]).astype(np.int32)
+    last, behind = np.full_like(full, -1), full.copy()
+    last[:, :, -1] = full[:, :, -1]
+    behind[:, :, :64] = -1
+    for these in (full, last, behind):
+        t = torch.from_numpy(these).to(p.dev)
+        for ws in ("full", None):
+            check_decode(p, *run_decode(p, False, t, workspace=ws), False, t, what=(batch, ws))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (8, 8), (16, 2), (40, 40)])
+@pytest.mark.parametrize("batch", [2, 3, 5, 8, 12, 15, 16, 17])
+def test_batches_of_like_and_unlike_lengths(batch, heads, kv_heads):
+    """Where every sequence begins a share of its own, and where shares go on from one to the next."""
+    rng = np.random.default_rng(batch * heads)
+    for longest, shortest in ((700, 650), (2000, 1), (5000, 4990), (64, 64), (9000, 300)):
+        lens = [int(rng.integers(shortest, longest + 1)) for _ in range(batch)]
+        p = one_query(lens, heads=heads, kv_heads=kv_heads, seed=longest)
+        check_decode(p, *run_decode(p, False), False, what=(batch, heads, longest))
+
+
 @pytest.mark.parametrize("scale", [SCALE, -SCALE, 0.0, 1.0])
 def test_scales_of_the_softmax(scale):
     for heads, kv_heads in ((2, 2), (6, 2)):
