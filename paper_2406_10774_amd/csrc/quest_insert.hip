@@ -200,15 +200,17 @@ __device__ __forceinline__ void round_part(char* block, const uint4 (&x)[kLoads]
   }
 }
 
-// How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their numbers in
-// registers: one wave's too, or, turned (which takes registers of its own, and from the queries' waves as well), 16 tokens a wave, and what
-// belongs to the page goes through LDS.  32k tokens of 32 / 8 heads in pages of 32 (64): one wave 170 (207) us, parts 165 (169);
-// without rotation, 32 heads, one wave 153 (158), parts 176 (177).
+// How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their keys in registers, and all of their
+// values: one wave's too, but for pages of 64 tokens, turned, of which a wave has 16 and what belongs to the page goes through LDS.  Of a turned page of
+// 32 tokens the keys are written before the values are asked for.
+//   21722 tokens of 32 / 32 heads, 32 channels turned (32k of 32 / 8 heads, 128), pages of 32: so 182 (148) us; values asked for with the keys 170 in
+//   the latter; in parts of 16 tokens 205 (157).  Pages of 64: in parts 212 (163), as pages of 32 242 (203), in parts of 32 235 (174).  (Pages of 16: 172 (141).)
+//   Without rotation, 32k tokens of 32 heads in pages of 32 (64): one wave 153 (158), parts 176 (177).
 template <int kS, bool k8, bool kRotate>
 struct Shape {
-  static constexpr int kParts = k8 && kRotate && kS > 16 ? kS / 16 : 1;   // waves of a page
+  static constexpr int kParts = k8 && kRotate && kS > 32 ? kS / 16 : 1;   // waves of a page
   static constexpr int kTokens = kS / kParts;                             // of a wave
-  static constexpr int kPairs = kParts == 4 ? 1 : kPairsOf;               // of a work-group
+  static constexpr int kPairs = kParts == 1 ? kPairsOf : 4 / kParts;      // of a work-group
   static constexpr int kWaves = kPairs * kParts;
   static constexpr int kEach = k8 ? kTokens : kTokens < 16 ? kTokens : 16;   // tokens at a time
 };
@@ -246,12 +248,18 @@ __global__ __launch_bounds__((Shape<kS, k8, kRotate>::kWaves * kWave)) void inse
   uint4 mn = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
   uint4 mx = make_uint4(0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u);
   uint32_t most[2] = {0, 0};
-  // Values asked for when the keys are turned leave registers for more waves (pages of 16 tokens 147 us, else 153; not where a
-  // wave has several times 16 tokens one after the other, 163 and 159).
-  constexpr bool kLate = kRotate && (kS <= 16 || kParts > 1);
-  // The new tokens from slot first_slot on, turned, and what the page's metadata and scales need of them.
+  // Values asked for when the keys are turned leave registers for more waves (pages of 16 tokens 147 us, else 153; not where fp16 pages give a
+  // wave several times 16 tokens one after the other, 163 and 159).
+  constexpr bool kLate = kRotate && (k8 || kS <= 16);
+  constexpr bool kKeysFirst = k8 && kRotate && kParts == 1 && kS > 16;
+  // The new tokens from slot first_slot on: their keys, turned, and values; what the page's metadata and scales need of them.
+  int row[kLoads];
+  auto ask_values = [&] {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      v[i] = ld16_stream(a.v_new + row[i] * a.new_stride + (int64_t)head * kRowBytes + chunk * 16);
+  };
   auto take = [&](int first_slot) {
-    int row[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int slot = first_slot + 4 * i + sub;
@@ -270,11 +278,9 @@ __global__ __launch_bounds__((Shape<kS, k8, kRotate>::kWaves * kWave)) void inse
         t.load(a, a.positions != nullptr ? a.positions[row[i]] : first + row[i] - first_row, chunk);
         k[i] = turn(a, k[i], t, chunk, lane);
       }
-      if (kLate) {
+      if (kLate && !kKeysFirst) {
         asm volatile("" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-          v[i] = ld16_stream(a.v_new + row[i] * a.new_stride + (int64_t)head * kRowBytes + chunk * 16);
+        ask_values();
       }
     }
 #pragma unroll
@@ -284,45 +290,79 @@ __global__ __launch_bounds__((Shape<kS, k8, kRotate>::kWaves * kWave)) void inse
         const uint4 key = order_key8(k[i]);
         mn = key_min8(mn, key);
         mx = key_max8(mx, key);
-        if constexpr (k8) {
-          most[0] = key_max2(most[0], magnitude8(k[i]));
-          most[1] = key_max2(most[1], magnitude8(v[i]));
-        }
+        if constexpr (k8) most[0] = key_max2(most[0], magnitude8(k[i]));
+        if constexpr (k8 && kParts == 1 && !kKeysFirst) most[1] = key_max2(most[1], magnitude8(v[i]));
       }
+    }
+  };
+  auto look_at_values = [&](int first_slot) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int slot = first_slot + 4 * i + sub;
+      if (slot >= from && slot < to) most[1] = key_max2(most[1], magnitude8(v[i]));
     }
   };
   if constexpr (k8) {
     const int first_slot = part * Of::kTokens;
     float2 old = make_float2(0.f, 0.f);
     if (there && from > 0) old = a.scales[block];
-    if (there && first_slot + Of::kTokens > from && first_slot < to) take(first_slot);
+    const bool takes = there && first_slot + Of::kTokens > from && first_slot < to;
+    if (takes) take(first_slot);
+    float2 scale;
+    auto scale_for = [&](uint32_t largest, float before) {
+      const int e = exponent_for(largest);
+      return scale_of(from > 0 ? max(e, exponent_of(before)) : e);
+    };
+    char* const k_block = a.k_pool + block * (kS * kRowBytes8);
+    char* const v_block = a.v_pool + block * (kS * kRowBytes8);
     most[0] = largest_half(most[0]);
-    most[1] = largest_half(most[1]);
     if constexpr (kParts > 1) {
+      // The keys' share of it first: they are written while the values are still on their way, which a barrier that waits for LDS alone
+      // leaves alone.
       __shared__ uint4 bounds[kWaves][2][16];
       __shared__ uint32_t largest[kWaves][2];
+      auto meet = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+      auto largest_of = [&](int which) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) m = max(m, largest[wave - part + i][which]);
+        return m;
+      };
       mn = rows_key_min8(mn);
       mx = rows_key_max8(mx);
       if (lane < 32) bounds[wave][sub][chunk] = sub == 0 ? mn : mx;
-      if (lane == 0) largest[wave][0] = most[0], largest[wave][1] = most[1];
-      __syncthreads();
-      if (!there) return;
+      if (lane == 0) largest[wave][0] = most[0];
+      meet();
+      if (there) {
+        scale.x = scale_for(largest_of(0), old.x);
+        round_part<kLoads>(k_block, k, first_slot, from, to, old.x, scale.x, lane);
+        if (part == 0)
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) {
-        const int of = wave - part + i;
-        most[0] = max(most[0], largest[of][0]);
-        most[1] = max(most[1], largest[of][1]);
-        if (part == 0) {
-          mn = key_min8(mn, bounds[of][0][chunk]);
-          mx = key_max8(mx, bounds[of][1][chunk]);
-        }
+          for (int i = 1; i < kParts; ++i) {
+            mn = key_min8(mn, bounds[wave + i][0][chunk]);
+            mx = key_max8(mx, bounds[wave + i][1][chunk]);
+          }
       }
+      if (takes) look_at_values(first_slot);
+      most[1] = largest_half(most[1]);
+      if (lane == 0) largest[wave][1] = most[1];
+      meet();
+      if (!there) return;
+      scale.y = scale_for(largest_of(1), old.y);
+      round_part<kLoads>(v_block, v, first_slot, from, to, old.y, scale.y, lane);
+    } else {
+      scale.x = scale_for(most[0], old.x);
+      if constexpr (kKeysFirst) {
+        round_part<kLoads>(k_block, k, first_slot, from, to, old.x, scale.x, lane);
+        asm volatile("" ::: "memory");
+        ask_values();
+        look_at_values(first_slot);
+      }
+      most[1] = largest_half(most[1]);
+      scale.y = scale_for(most[1], old.y);
+      if (!kKeysFirst) round_part<kLoads>(k_block, k, first_slot, from, to, old.x, scale.x, lane);
+      round_part<kLoads>(v_block, v, first_slot, from, to, old.y, scale.y, lane);
     }
-    int e[2] = {exponent_for(most[0]), exponent_for(most[1])};
-    if (from > 0) e[0] = max(e[0], exponent_of(old.x)), e[1] = max(e[1], exponent_of(old.y));
-    const float2 scale = make_float2(scale_of(e[0]), scale_of(e[1]));
-    round_part<kLoads>(a.k_pool + block * (kS * kRowBytes8), k, first_slot, from, to, old.x, scale.x, lane);
-    round_part<kLoads>(a.v_pool + block * (kS * kRowBytes8), v, first_slot, from, to, old.y, scale.y, lane);
     if (part == 0 && lane == 0) a.scales[block] = scale;
   } else {
 #pragma unroll 1
