@@ -33,14 +33,16 @@ struct DecodeArgs : AttnArgs {
   const int32_t* topk;
   int k_pages, listed;    // entries of a list, and how many of them count
   int shares;             // of the line of all sequences' tiles; 0: one work-group a sequence
+  int loose;              // more than a share for each compute unit
+  int count, per_die;     // shares or sequences, and (share, column) pairs of a die (0: every eighth sequence's)
 };
 
 // The tiles of all sequences, one after the other, are one line that is cut into shares of `length` tiles.  A sequence has a tile at
 // least.  A list is taken to have as many entries as its sequence has pages at most (more only if it names a page twice: the last
 // share sees to those).
 // A share that ends one sequence and begins the next does two lookups and leaves two results, which takes longer than a few
-// tiles: where shares up to kMore tiles longer are enough for every sequence to begin a share of its own, the line has gaps and they do
-// (up to 16 sequences; five of 831 to 1066 tokens by 8 KV heads 11.5 -> 8.9 us, of 16 / 8 heads 13.3 -> 10.3, 12 of 525 to 2763 of 32 / 8 heads 19.2 -> 15.6, four
+// tiles: where shares up to kMore tiles longer (more than one share a compute unit: up to six tiles or a third) are enough for every sequence to begin a
+// share of its own, the line has gaps and they do (up to 64 sequences; five of 831 to 1066 tokens by 8 KV heads 11.5 -> 8.9 us, of 16 / 8 heads 13.3 -> 10.3, 12 of 525 to 2763 of 32 / 8 heads 19.2 -> 15.6, four
 // of 16k 32.0 -> 28.8).
 struct Line {
   static constexpr int kMore = 3;
@@ -88,12 +90,22 @@ struct Line {
     }
     length = share_length(a, total, longest);
     int spans = mine;
-    if (a.batch <= 16) {   // lane 16 j + b: shares that sequence b takes if they are j tiles longer
-      const int tiles_here = __builtin_amdgcn_ds_bpermute((lane & 15) * 4, mine), longer = length + (lane >> 4);
-      const float needed = row16_sum((float)((tiles_here + longer - 1) / longer));
-      const unsigned long long enough = __ballot(needed <= (float)a.shares && (lane >> 4) <= kMore);
-      if (enough != 0) {
-        length += __builtin_ctzll(enough) >> 4;
+    if (a.batch <= kWave) {
+      const int step = a.loose ? max(length / (3 * kMore), 2) : 1;
+      int longer = 0;
+      if (a.batch <= 16) {   // lane 16 j + b: shares that sequence b takes if they are j steps longer
+        const int tiles_here = __builtin_amdgcn_ds_bpermute((lane & 15) * 4, mine), at = length + (lane >> 4) * step;
+        const float needed = row16_sum((float)((tiles_here + at - 1) / at));
+        const unsigned long long enough = __ballot(needed <= (float)a.shares && (lane >> 4) <= kMore);
+        if (enough != 0) longer = length + (__builtin_ctzll(enough) >> 4) * step;
+      } else {
+        for (int j = 0; j <= kMore && longer == 0; ++j) {
+          const int at = length + j * step;
+          if (__builtin_amdgcn_readlane(up_to_lane((mine + at - 1) / at, lane), kWave - 1) <= a.shares) longer = at;
+        }
+      }
+      if (longer != 0) {
+        length = longer;
         spans = (mine + length - 1) / length * length;
         total = __builtin_amdgcn_readlane(up_to_lane(spans, lane), kWave - 1);
       }
@@ -400,9 +412,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void decode_e4m3_kernel(const Dec
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id();
   const int columns = a.kv_heads * a.subs;   // KV heads, in parts of up to eight query heads
-  // Work-groups go to the eight dies by turns: a share's columns are all on one, where what they read at a time is adjacent (heads of
-  // the same pages).
-  const int column = blockIdx.x / 8 % columns, index = blockIdx.x / 8 / columns * 8 + blockIdx.x % 8;
+  // Work-groups go to the eight dies by turns: a share's columns are on one, where what they read at a time is adjacent (heads of
+  // the same pages), and every die has the same number of work-groups (96 heads have two shares each: 296 us on two dies, 119 on eight).
+  int column, index;
+  if (a.per_die > 0) {
+    const int at = blockIdx.x % 8 * a.per_die + blockIdx.x / 8;
+    index = at / columns, column = at - index * columns;
+    if (index >= a.count) return;
+  } else {
+    column = blockIdx.x / 8 % columns, index = blockIdx.x / 8 / columns * 8 + blockIdx.x % 8;
+  }
   const int hk = column / a.subs, head0 = column % a.subs * kSlots;
   const int n_heads = min(kSlots, a.group - head0);
   Line line;
@@ -659,12 +678,16 @@ int tile_tokens(const quest_cache& c) { return kWaves * 8 * (many_heads(c) ? Man
 int columns_of(const quest_cache& c) { return kv_heads(c) * attention_subs(c); }
 // Shares of a column: a work-group on every compute unit, or one a sequence.  (More of them for few sequences leave more to join and no
 // more bytes under way: 128 pages of each of 32 heads 9.0 us, with twice as many 10.4; 590k tokens of 16 sequences and 8 KV heads
-// 196 us and 201.)  None where the (sequence, KV head) pairs are more than two for a compute unit: the units then even out what
+// 196 us and 201.)  Twice as many where there would be more than one on some units and one on others, or more than a fifth of the units had none: ten
+// sequences of 3000 to 30000 tokens of 32 heads 265 -> 204 us, 40 of 900 to 8000 of 32 / 8 heads 84 -> 69, one of 30000 of 96 heads 119 -> 112.
+// None where the (sequence, KV head) pairs are more than two for a compute unit: the units then even out what
 // sequences differ by (256 sequences of 10 to 2000 tokens and 8 KV heads 94 us, in shares 132; 64 sequences 56 and 56).
 int most_shares(const quest_cache& c) {
   const int columns = columns_of(c);
   const int64_t tiles = ((int64_t)c.max_pages_per_seq * c.page_size / tile_tokens(c) + 1) * c.batch;
-  return (int64_t)c.batch * columns <= 512 && tiles <= INT32_MAX ? std::max(256 / columns, c.batch) : 0;
+  const int64_t pairs = (int64_t)c.batch * columns;
+  if (pairs > 512 || tiles > INT32_MAX) return 0;
+  return std::max((pairs > 256 || 256 / columns * columns < 208 ? 512 : 256) / columns, c.batch);
 }
 size_t share_bytes(const quest_cache& c) {
   return (size_t)2 * columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * (kHeadDim + 2) * sizeof(float);
@@ -698,8 +721,12 @@ int launch_decode_e4m3(const quest_cache& c, const void* q, const int32_t* topk_
   a.counters = (uint64_t*)workspace;
   a.part_acc = (float*)((char*)workspace + counters);
   a.part_ml = a.part_acc + (size_t)a.shares * 2 * columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * kHeadDim;
-  const int units = ((a.shares > 0 ? a.shares : c.batch) + 7) / 8 * 8;
-  const dim3 grid((unsigned)((int64_t)units * columns_of(c))), block(kWaves * kWave);
+  a.count = a.shares > 0 ? a.shares : c.batch;
+  const int64_t blocks = (int64_t)a.count * columns_of(c);
+  a.loose = blocks > 256;
+  // (a few sequences, too, but not many: if they are sorted by length, dies should have one of every eight)
+  a.per_die = a.count % 8 != 0 && (a.shares > 0 || a.count < 24) ? (int)((blocks + 7) / 8) : 0;
+  const dim3 grid((unsigned)(a.per_die > 0 ? a.per_die * 8 : (int64_t)(a.count + 7) / 8 * 8 * columns_of(c))), block(kWaves * kWave);
   if (many_heads(c))
     hipLaunchKernelGGL(decode_e4m3_kernel<ManyHeads>, grid, block, 0, s, a);
   else

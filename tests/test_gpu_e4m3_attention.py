@@ -113,14 +113,26 @@ def test_lists_with_more_entries_than_pages(batch, heads, kv_heads):
 
 
 @pytest.mark.parametrize("heads,kv_heads", [(2, 2), (8, 8), (16, 2), (40, 40)])
-@pytest.mark.parametrize("batch", [2, 3, 5, 8, 12, 15, 16, 17])
+@pytest.mark.parametrize("batch", [2, 3, 5, 8, 12, 15, 16, 17, 40, 64, 65])
 def test_batches_of_like_and_unlike_lengths(batch, heads, kv_heads):
     """Where every sequence begins a share of its own, and where shares go on from one to the next."""
     rng = np.random.default_rng(batch * heads)
+    if batch * kv_heads > 680:
+        return                                                      # 512 pairs and more are not shared out
     for longest, shortest in ((700, 650), (2000, 1), (5000, 4990), (64, 64), (9000, 300)):
         lens = [int(rng.integers(shortest, longest + 1)) for _ in range(batch)]
         p = one_query(lens, heads=heads, kv_heads=kv_heads, seed=longest)
         check_decode(p, *run_decode(p, False), False, what=(batch, heads, longest))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(3, 3), (33, 33), (96, 96), (200, 200), (48, 24)])
+@pytest.mark.parametrize("batch", [1, 2, 9, 19])
+def test_heads_and_batches_that_eight_does_not_divide(batch, heads, kv_heads):
+    rng = np.random.default_rng(batch * heads)
+    p = one_query([int(n) for n in rng.integers(0, 900, batch)], heads=heads, kv_heads=kv_heads, seed=heads)
+    sizes = ("full", None) if batch < 9 else ("full",)
+    for ws in sizes:
+        check_decode(p, *run_decode(p, False, workspace=ws), False, what=(batch, heads, ws))
 
 
 @pytest.mark.parametrize("scale", [SCALE, -SCALE, 0.0, 1.0])
