@@ -201,23 +201,27 @@ __device__ __forceinline__ void round_part(char* block, const uint4 (&x)[kLoads]
 }
 
 // How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their keys in registers, and all of their
-// values: one wave's too, but for pages of 64 tokens, turned, of which a wave has 16 and what belongs to the page goes through LDS.  Of a turned page of
-// 32 tokens the keys are written before the values are asked for.
+// values: one wave's too, or (kApart) 16 tokens a wave, and what belongs to the page goes through LDS: pages of 64 tokens, turned, and pages of 32 and 64 that
+// are no more than the SIMDs, where a wave's latency counts.  Of a turned page of 32 tokens that is one wave's the keys are written before the values are
+// asked for.
 //   21722 tokens of 32 / 32 heads, 32 channels turned (32k of 32 / 8 heads, 128), pages of 32: so 182 (148) us; values asked for with the keys 170 in
-//   the latter; in parts of 16 tokens 205 (157).  Pages of 64: in parts 212 (163), as pages of 32 242 (203), in parts of 32 235 (174).  (Pages of 16: 172 (141).)
-//   Without rotation, 32k tokens of 32 heads in pages of 32 (64): one wave 153 (158), parts 176 (177).
-template <int kS, bool k8, bool kRotate>
+//   the latter; apart 205 (157).  Pages of 64: apart 212 (163), as pages of 32 242 (203), in parts of 32 235 (174).  (Pages of 16: 172 (141).)
+//   Without rotation, 32k tokens of 32 heads in pages of 32 (64): one wave 153 (158), apart 176 (177).
+//   One token each of 16 sequences, 8 KV heads, pages of 64: one wave 6.7, apart 5.4; turned, pages of 32: 7.7 and 6.5.  1180 tokens of 32 heads (850 pairs of page
+//   and head) pages of 64 17.2 and 14.3; (1440 pairs) pages of 32 12.3 and 14.1.
+constexpr int kFewPairs = 1024;
+template <int kS, bool k8, bool kRotate, bool kApart>
 struct Shape {
-  static constexpr int kParts = k8 && kRotate && kS > 32 ? kS / 16 : 1;   // waves of a page
+  static constexpr int kParts = kApart ? kS / 16 : 1;                     // waves of a page
   static constexpr int kTokens = kS / kParts;                             // of a wave
   static constexpr int kPairs = kParts == 1 ? kPairsOf : 4 / kParts;      // of a work-group
   static constexpr int kWaves = kPairs * kParts;
   static constexpr int kEach = k8 ? kTokens : kTokens < 16 ? kTokens : 16;   // tokens at a time
 };
 
-template <int kS, bool k8, bool kRotate>
-__global__ __launch_bounds__((Shape<kS, k8, kRotate>::kWaves * kWave)) void insert_kernel(const InsertArgs a) {
-  using Of = Shape<kS, k8, kRotate>;
+template <int kS, bool k8, bool kRotate, bool kApart>
+__global__ __launch_bounds__((Shape<kS, k8, kRotate, kApart>::kWaves * kWave)) void insert_kernel(const InsertArgs a) {
+  using Of = Shape<kS, k8, kRotate, kApart>;
   constexpr int kParts = Of::kParts, kWaves = Of::kWaves, kEach = Of::kEach;
   constexpr int kLoads = kEach / 4;   // wave-wide loads of four tokens each
   const int lane = lane_id();
@@ -396,18 +400,28 @@ __global__ __launch_bounds__((Shape<kS, k8, kRotate>::kWaves * kWave)) void inse
 
 int64_t waves_of_rows(const InsertArgs& a) { return ((int64_t)a.total + 3) / 4 * ((a.q_heads + kQHeads - 1) / kQHeads); }
 
-template <int kS, bool k8, bool kRotate>
+template <int kS, bool k8, bool kRotate, bool kApart = false>
 int launch_insert_as(InsertArgs& a, const char* who, hipStream_t s) {
-  using Of = Shape<kS, k8, kRotate>;
+  using Of = Shape<kS, k8, kRotate, kApart>;
   a.insert_blocks = (a.pairs + Of::kPairs - 1) / Of::kPairs;
   const int64_t rows = kRotate && a.q != nullptr ? (waves_of_rows(a) + Of::kWaves - 1) / Of::kWaves : 0;
-  hipLaunchKernelGGL((insert_kernel<kS, k8, kRotate>), dim3((unsigned)(a.insert_blocks + rows)), dim3(Of::kWaves * kWave), 0, s, a);
+  hipLaunchKernelGGL((insert_kernel<kS, k8, kRotate, kApart>), dim3((unsigned)(a.insert_blocks + rows)), dim3(Of::kWaves * kWave), 0, s, a);
   return check_launch(who);
+}
+template <int kS, bool kRotate>
+int launch_insert8(InsertArgs& a, const char* who, hipStream_t s) {
+  if constexpr (kRotate && kS > 32) {
+    return launch_insert_as<kS, true, kRotate, true>(a, who, s);
+  } else {
+    if constexpr (kS > 16)
+      if (a.pairs <= kFewPairs) return launch_insert_as<kS, true, kRotate, true>(a, who, s);
+    return launch_insert_as<kS, true, kRotate>(a, who, s);
+  }
 }
 template <int kS>
 int launch_insert_for(InsertArgs& a, bool pages8, bool rotate, const char* who, hipStream_t s) {
   if (!pages8) return launch_insert_as<kS, false, true>(a, who, s);
-  return rotate ? launch_insert_as<kS, true, true>(a, who, s) : launch_insert_as<kS, true, false>(a, who, s);
+  return rotate ? launch_insert8<kS, true>(a, who, s) : launch_insert8<kS, false>(a, who, s);
 }
 
 InsertArgs rotation_args(const quest_cache& c, const PackedTokens& p, const quest_rotation* r) {

@@ -102,6 +102,16 @@ def test_ragged_insertion(S, heads, kv_heads):
         assert torch.equal(p.meta.view(torch.int16), half.meta.view(torch.int16))          # of the keys before they are rounded
 
 
+@pytest.mark.parametrize("S", [32, 64])
+def test_more_pages_than_are_shared_out(S):
+    lens, new = [250, 40, 3 * S, 1, 70, S - 1, 2 * S + 3], [250, 0, S, 1, 65, 2, 2]
+    p = Packed8(lens, new, heads=80, kv_heads=80, S=S, seed=S)
+    assert (sum(new) // S + 2 * len(new)) * 80 > 1024
+    o = Oracle(p)
+    Q.quest_append_tokens(p.cache, p.k_new, p.v_new, p.cu)
+    o.check(p, o.insert(p))
+
+
 @pytest.mark.parametrize("S", [8, 16, 32, 64])
 def test_scales_that_grow_token_by_token(S):
     """One token a call, each larger than the last by up to 2^12, and some smaller: what the page holds is rounded again, down into

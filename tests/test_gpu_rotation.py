@@ -128,6 +128,20 @@ def test_insertion_with_rotation_is_both_calls(bits_of_cache, S, rotary, interle
                 assert torch.equal(raw(t), raw(getattr(b, name))) and torch.equal(raw(t), raw(getattr(c, name))), name
 
 
+@pytest.mark.parametrize("S", [32, 64])
+@pytest.mark.parametrize("rotary,interleaved", [(128, False), (64, True)])
+def test_insertion_of_many_heads_with_rotation_is_both_calls(S, rotary, interleaved):
+    """More (page, head) pairs than large pages of 8 bits are shared out for."""
+    a, b = (Packed8([100, 70, 5, 131, 90, 3, 20], [1, 70, 0, 66, 90, 3, 7], heads=80, kv_heads=80, S=S, seed=S) for _ in range(2))
+    r = Q.Rotation(table_of(150, rotary), interleaved=interleaved)
+    Q.quest_rotate_append_tokens(a.cache, r, None, a.k_new, a.v_new, a.cu)
+    k = torch.zeros(b.total, 80, D, device=b.dev, dtype=torch.float16)
+    Q.quest_rotate_tokens(b.cache, r, b.k_new, b.cu, k)
+    Q.quest_append_tokens(b.cache, k, b.v_new.contiguous(), b.cu)
+    for name, t in cache_of(a, 8).items():
+        assert torch.equal(raw(t), raw(getattr(b, name))), name
+
+
 def test_insertion_in_place_and_repeated():
     """Queries turned where they lie; a second call with the same tokens changes nothing but them."""
     p = Packed([90, 31], [40, 1], heads=4, kv_heads=2, seed=2)
