@@ -333,10 +333,19 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
     // (the steps over cached tokens, which come before those over drafted nodes)
     const int cached = kTree ? min(max((w.stream.context - walk.start + walk.stride - 1) / walk.stride, 0), max(steps, 0)) : steps;
     char* stage_v8 = stage_k + kTokens * kRowBytes8;
+    // Past the caches, unless other row tiles read the same tokens for long enough: one token a head at 32k of 32 heads so 52 us, else 58; 32 times 10
+    // tokens at 4000 of 32 / 8 heads (40 rows, two tiles; a split walks 63 tiles of tokens) 78 and through them 72, twice 33 at 65k of 8 heads (64 tiles) 78 and
+    // 73; but 16 times 16 at 3000 of 32 / 8 heads (24) 35.1 and 35.9, 77 to 9 behind 2600 to 35 of 40 heads (21) 37.4 and 38.2.
+    const bool once = w.s.row_tiles == 1 || w.end_tile - w.first_tile < 32;
     auto load8 = [&](int step) {
       if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
+      if (once) {
 #pragma unroll
-      for (int i = 0; i < kEights; ++i) walk.template load8<true>(a, w.stream, w.hk, step, i * 8, lane, k[i], v[i]);
+        for (int i = 0; i < kEights; ++i) walk.template load8<true>(a, w.stream, w.hk, step, i * 8, lane, k[i], v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kEights; ++i) walk.template load8<false>(a, w.stream, w.hk, step, i * 8, lane, k[i], v[i]);
+      }
     };
     float k_scale, v_scale[2];   // of the lane's key, of its values
     auto put8 = [&](int step) {

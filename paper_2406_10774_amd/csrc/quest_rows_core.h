@@ -568,8 +568,8 @@ struct Walk {
     if (left > 0 && (!kTree || at < s.context)) scale = a.scales[(size_t)phys * a.kv_heads + hk];
   }
   // Key and value of the step's place `eight` + lane / 8 (`eight`: a multiple of 8): channels 16 (lane % 8) ..+15; zeros where there
-  // is no token.  kOnce: past the caches (few rows: one token a head at 32k of 32 heads 52 us, else 58; many row tiles, which read the same
-  // tokens at about the same time: 32k of 32 / 8 heads 8.8 ms, else 9.0).
+  // is no token.  kOnce: past the caches (the large kernel, whose row tiles read the same tokens at about the same time: 32k of 32 / 8
+  // heads through them 8.8 ms, past them 9.0).
   template <bool kOnce>
   __device__ __forceinline__ void load8(const RowsArgs& a, const Stream<kTree>& s, int hk, int step, int eight, int lane,
                                         uint4& key, uint4& value) const {
