@@ -142,13 +142,15 @@ typedef struct quest_cache {
  * e or takes a larger one; what it holds is then rounded to that (exact, but for what becomes an e4m3 subnormal).
  * Metadata is of the keys in fp16, before they are rounded to 8 bits, so that the same
  * pages are selected as with the fp16 cache.
- * Calls on such a cache: quest_append_tokens and quest_rotate_append_tokens fill it (a decode step's token
- * too); quest_estimate and quest_topk as on any cache; quest_sparse_decode, quest_select_decode,
- * quest_decode_step, quest_prompt_attention and quest_tree_attention (drafted nodes in fp16) read it (select and step as
- * launches of their own for each phase).  QUEST_ERR_UNSUPPORTED: quest_build_meta, quest_decode_step_static, and
- * a token's insertion by the single-token calls (k_pool_write != 0).  quest_sparse_decode and its like take any workspace, or
- * NULL, without a refusal: a smaller one makes fewer splits, slower.  Nothing is split where the batch times the KV heads (times parts of eight query
- * heads) is more than 512: a sequence much longer than the others is faster in a call of its own there. */
+ * Calls on such a cache: quest_append_tokens and quest_rotate_append_tokens fill it (a decode step's
+ * token too); quest_estimate and quest_topk as on any cache; quest_sparse_decode, quest_select_decode,
+ * quest_decode_step, quest_prompt_attention and quest_tree_attention (drafted nodes in fp16) read it
+ * (select and step as launches of their own for each phase).  QUEST_ERR_UNSUPPORTED: quest_build_meta,
+ * quest_decode_step_static, and a token's insertion by the single-token calls (k_pool_write != 0).
+ * quest_sparse_decode and its like take any workspace, or NULL, without a refusal: a smaller one makes
+ * fewer splits, slower.  Nothing is split where the batch times the KV heads (times parts of eight query
+ * heads) is more than 512: a sequence much longer than the others is faster in a call of its own there.
+ * Lists are fastest as quest_topk leaves them, with no more entries than their sequence has pages. */
 
 /* Bytes of device workspace for quest_sparse_decode, quest_select_decode and
  * quest_decode_step on this cache: one size for every call on the cache shape
@@ -370,7 +372,8 @@ typedef struct quest_rotation {
 } quest_rotation;
 
 /* Packed rows of `heads` heads, turned: out[row] = rotation of x[row] for rows below cu_tokens[batch].  Of the cache only its
- * shape and seq_lens are used.  Strides in elements, as above; out may be x itself with the same stride, and must not overlap it otherwise. */
+ * shape and seq_lens are used.  Strides in elements, as above; out may be x itself with the same stride, and
+ * must not overlap it otherwise. */
 int quest_rotate_tokens(const quest_cache* cache, const quest_rotation* rotation, const void* x, int64_t x_stride,
                         int32_t heads, const int32_t* cu_tokens, int32_t total_tokens, void* out, int64_t out_stride,
                         void* stream);

@@ -1,8 +1,8 @@
 // Attention of one query a sequence over pages of 8 bits: listed pages, or all.
 //
 // Bound by memory: a token's key and value of a head are 256 bytes, read once.  The tokens of a sequence are cut into tiles of
-// 64 (128 where query heads share a KV head), a quarter for each of a work-group's four waves; a lane looks up the page of eight tokens, ahead of
-// the keys and values, which are on their way to a wave 16 KiB at a time, and go on across the lookups.
+// 64 (128 where query heads share a KV head), a quarter for each of a work-group's four waves; a lane looks up the page of eight tokens,
+// ahead of the keys and values, which are on their way to a wave 16 KiB at a time, and go on across the lookups.
 //
 // The host knows no lengths: the tiles of all sequences are one line that is cut into equal shares, a work-group each, however ragged
 // the batch.  A share that ends inside a sequence leaves a partial result; the share of a (sequence, KV head) that arrives last joins
@@ -41,9 +41,9 @@ struct DecodeArgs : AttnArgs {
 // least.  A list is taken to have as many entries as its sequence has pages at most (more only if it names a page twice: the last
 // share sees to those).
 // A share that ends one sequence and begins the next does two lookups and leaves two results, which takes longer than a few
-// tiles: where shares up to kMore tiles longer (more than one share a compute unit: up to six tiles or a third) are enough for every sequence to begin a
-// share of its own, the line has gaps and they do (up to 64 sequences; five of 831 to 1066 tokens by 8 KV heads 11.5 -> 8.9 us, of 16 / 8 heads 13.3 -> 10.3, 12 of 525 to 2763 of 32 / 8 heads 19.2 -> 15.6, four
-// of 16k 32.0 -> 28.8).
+// tiles: where shares up to kMore tiles longer (more than one share a compute unit: up to six tiles or a third) are enough for every
+// sequence to begin a share of its own, the line has gaps and they do (up to 64 sequences; five of 831 to 1066 tokens by 8 KV heads 11.5
+// -> 8.9 us, of 16 / 8 heads 13.3 -> 10.3, 12 of 525 to 2763 of 32 / 8 heads 19.2 -> 15.6, four of 16k 32.0 -> 28.8).
 struct Line {
   static constexpr int kMore = 3;
   int length;
@@ -678,9 +678,9 @@ int tile_tokens(const quest_cache& c) { return kWaves * 8 * (many_heads(c) ? Man
 int columns_of(const quest_cache& c) { return kv_heads(c) * attention_subs(c); }
 // Shares of a column: a work-group on every compute unit, or one a sequence.  (More of them for few sequences leave more to join and no
 // more bytes under way: 128 pages of each of 32 heads 9.0 us, with twice as many 10.4; 590k tokens of 16 sequences and 8 KV heads
-// 196 us and 201.)  Twice as many where there would be more than one on some units and one on others, or more than a fifth of the units had none: ten
-// sequences of 3000 to 30000 tokens of 32 heads 265 -> 204 us, 40 of 900 to 8000 of 32 / 8 heads 84 -> 69, one of 30000 of 96 heads 119 -> 112.
-// None where the (sequence, KV head) pairs are more than two for a compute unit: the units then even out what
+// 196 us and 201.)  Twice as many where there would be more than one on some units and one on others, or more than a fifth of the units
+// had none: ten sequences of 3000 to 30000 tokens of 32 heads 265 -> 204 us, 40 of 900 to 8000 of 32 / 8 heads 84 -> 69, one of 30000 of
+// 96 heads 119 -> 112. None where the (sequence, KV head) pairs are more than two for a compute unit: the units then even out what
 // sequences differ by (256 sequences of 10 to 2000 tokens and 8 KV heads 94 us, in shares 132; 64 sequences 56 and 56).
 int most_shares(const quest_cache& c) {
   const int columns = columns_of(c);

@@ -200,15 +200,15 @@ __device__ __forceinline__ void round_part(char* block, const uint4 (&x)[kLoads]
   }
 }
 
-// How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their keys in registers, and all of their
-// values: one wave's too, or (kApart) 16 tokens a wave, and what belongs to the page goes through LDS: pages of 64 tokens, turned, and pages of 32 and 64 that
-// are no more than the SIMDs, where a wave's latency counts.  Of a turned page of 32 tokens that is one wave's the keys are written before the values are
-// asked for.
-//   21722 tokens of 32 / 32 heads, 32 channels turned (32k of 32 / 8 heads, 128), pages of 32: so 182 (148) us; values asked for with the keys 170 in
-//   the latter; apart 205 (157).  Pages of 64: apart 212 (163), as pages of 32 242 (203), in parts of 32 235 (174).  (Pages of 16: 172 (141).)
-//   Without rotation, 32k tokens of 32 heads in pages of 32 (64): one wave 153 (158), apart 176 (177).
-//   One token each of 16 sequences, 8 KV heads, pages of 64: one wave 6.7, apart 5.4; turned, pages of 32: 7.7 and 6.5.  1180 tokens of 32 heads (850 pairs of page
-//   and head) pages of 64 17.2 and 14.3; (1440 pairs) pages of 32 12.3 and 14.1.
+// How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their keys in registers, and
+// all of their values: one wave's too, or (kApart) 16 tokens a wave, and what belongs to the page goes through LDS: pages of 64 tokens,
+// turned, and pages of 32 and 64 that are no more than the SIMDs, where a wave's latency counts.  Of a turned page of 32 tokens that is
+// one wave's the keys are written before the values are asked for.
+//   21722 tokens of 32 / 32 heads, 32 channels turned (32k of 32 / 8 heads, 128), pages of 32: so 182 (148) us; values asked for with the
+//   keys 170 in the latter; apart 205 (157).  Pages of 64: apart 212 (163), as pages of 32 242 (203), in parts of 32 235 (174).  (Pages
+//   of 16: 172 (141).) Without rotation, 32k tokens of 32 heads in pages of 32 (64): one wave 153 (158), apart 176 (177). One token each
+//   of 16 sequences, 8 KV heads, pages of 64: one wave 6.7, apart 5.4; turned, pages of 32: 7.7 and 6.5.  1180 tokens of 32 heads (850
+//   pairs of page and head) pages of 64 17.2 and 14.3; (1440 pairs) pages of 32 12.3 and 14.1.
 constexpr int kFewPairs = 1024;
 template <int kS, bool k8, bool kRotate, bool kApart>
 struct Shape {
@@ -252,8 +252,8 @@ __global__ __launch_bounds__((Shape<kS, k8, kRotate, kApart>::kWaves * kWave)) v
   uint4 mn = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
   uint4 mx = make_uint4(0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u);
   uint32_t most[2] = {0, 0};
-  // Values asked for when the keys are turned leave registers for more waves (pages of 16 tokens 147 us, else 153; not where fp16 pages give a
-  // wave several times 16 tokens one after the other, 163 and 159).
+  // Values asked for when the keys are turned leave registers for more waves (pages of 16 tokens 147 us, else 153; not where fp16 pages
+  // give a wave several times 16 tokens one after the other, 163 and 159).
   constexpr bool kLate = kRotate && (k8 || kS <= 16);
   constexpr bool kKeysFirst = k8 && kRotate && kParts == 1 && kS > 16;
   // The new tokens from slot first_slot on: their keys, turned, and values; what the page's metadata and scales need of them.

@@ -326,16 +326,17 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void few_rows_kernel(
   };
   if constexpr (k8) {
     // Pages of 8 bits: tiles lie in LDS as they came and become fp16 numbers on the way to a product, each number once, as a wave has all of
-    // a tile's rows: half the LDS traffic of fp16 tiles.  26 tokens at 32k of 32 heads 57 us, with fp16 tiles 64 (40 heads, 9 to 77 tokens behind 35 to 2600:
-    // 38.6 and 44.2); two steps under way 64 (registers spill); three work-groups on a compute unit, with queries in LDS, 63.
-    // (No load of the loop is ever skipped, so that the compiler knows how many are under way.)
+    // a tile's rows: half the LDS traffic of fp16 tiles.  26 tokens at 32k of 32 heads 57 us, with fp16 tiles 64 (40 heads, 9 to 77
+    // tokens behind 35 to 2600: 38.6 and 44.2); two steps under way 64 (registers spill); three work-groups on a compute unit, with
+    // queries in LDS, 63. (No load of the loop is ever skipped, so that the compiler knows how many are under way.)
     constexpr int kEights = kTokens / 8;
     // (the steps over cached tokens, which come before those over drafted nodes)
     const int cached = kTree ? min(max((w.stream.context - walk.start + walk.stride - 1) / walk.stride, 0), max(steps, 0)) : steps;
     char* stage_v8 = stage_k + kTokens * kRowBytes8;
-    // Past the caches, unless other row tiles read the same tokens for long enough: one token a head at 32k of 32 heads so 52 us, else 58; 32 times 10
-    // tokens at 4000 of 32 / 8 heads (40 rows, two tiles; a split walks 63 tiles of tokens) 78 and through them 72, twice 33 at 65k of 8 heads (64 tiles) 78 and
-    // 73; but 16 times 16 at 3000 of 32 / 8 heads (24) 35.1 and 35.9, 77 to 9 behind 2600 to 35 of 40 heads (21) 37.4 and 38.2.
+    // Past the caches, unless other row tiles read the same tokens for long enough: one token a head at 32k of 32 heads so 52 us, else
+    // 58; 32 times 10 tokens at 4000 of 32 / 8 heads (40 rows, two tiles; a split walks 63 tiles of tokens) 78 and through them 72, twice
+    // 33 at 65k of 8 heads (64 tiles) 78 and 73; but 16 times 16 at 3000 of 32 / 8 heads (24) 35.1 and 35.9, 77 to 9 behind 2600 to 35 of
+    // 40 heads (21) 37.4 and 38.2.
     const bool once = w.s.row_tiles == 1 || w.end_tile - w.first_tile < 32;
     auto load8 = [&](int step) {
       if (!walk.knows(step)) walk.find8(a, w.stream, w.hk, step, lane);
@@ -563,10 +564,10 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 
 // How a call is cut up, from what the host knows.  The figures are of 820 calls, from 6 to 12000 rows a sequence over contexts
 // up to 60000 tokens by 1 to 64 heads, each with both kernels, with and without splits: the rules take 1 % longer than the
-// best of the four on average.  (The lengths of a batch were from half or a quarter of the longest, page-table rows ended with it, and the small
-// kernel rounded the weights of fp16 outputs, 1.00 to 1.12 times as fast as it is.)  The row of the page table is taken for the longest
-// length: in wide tables short prompts have the large kernel and splits that find nothing to split (77 tokens of 32 heads in rows of 2048
-// pages 13.4 us, in rows of their own length 6.7).
+// best of the four on average.  (The lengths of a batch were from half or a quarter of the longest, page-table rows ended with it, and
+// the small kernel rounded the weights of fp16 outputs, 1.00 to 1.12 times as fast as it is.)  The row of the page table is taken for the
+// longest length: in wide tables short prompts have the large kernel and splits that find nothing to split (77 tokens of 32 heads in rows
+// of 2048 pages 13.4 us, in rows of their own length 6.7).
 //   Splits: where the row tiles leave compute units idle for long enough.  Idle is the share of the units without
 //   a row tile times the row's tiles of tokens; a join costs as much as 8 to 12 of them (60 drafts of 8 heads at 600
 //   tokens 12 us with splits and 15 without), 20 to 25 where more than a third of the units have a row tile (sixteen
@@ -645,8 +646,8 @@ int launch_rows(const quest_cache& c, RowsArgs& a, int total_tokens, const int32
   if (r != QUEST_OK || p.most_units == 0) return r;
   const unsigned tiles = (unsigned)(p.row_tiles * a.kv_heads);
   // Few rows: work-groups of as few of them as the compute units take at once, 2048 work-groups, so that a wave has one row, two or four.
-  // Four times 16 nodes over 128 listed pages of 32 / 8 heads (96 row tiles) 22.9 us with four rows, 26.0 with 16; 40 heads, 77 tokens behind 2600
-  // (280 row tiles) 50.2 with four rows, 47.5 with eight, 48.7 with 16.
+  // Four times 16 nodes over 128 listed pages of 32 / 8 heads (96 row tiles) 22.9 us with four rows, 26.0 with 16; 40 heads, 77 tokens
+  // behind 2600 (280 row tiles) 50.2 with four rows, 47.5 with eight, 48.7 with 16.
   if (p.rows == kFewRows && tiles <= 256)
     hipLaunchKernelGGL((merge_rows_kernel<kTree, kFewRows, 4>), dim3(tiles * (kFewRows / 4)), dim3(256), 0, s, a, a.cu,
                        a.seq_lens, topk);

@@ -384,8 +384,8 @@ struct RowState {
   }
 
   // The same for 32 tokens that lie in LDS as 8-bit numbers, rows of 128 bytes (place8).  Row m = 8 i + 4 h + j of the first product is
-  // token 16 (i / 2) + 8 h + 4 (i % 2) + j, so that a lane's weights are of tokens 8 h ..+7 and 16 + 8 h ..+7: eight of one page each, whose values
-  // (turned by the LDS read, eight tokens of a channel) have one scale.
+  // token 16 (i / 2) + 8 h + 4 (i % 2) + j, so that a lane's weights are of tokens 8 h ..+7 and 16 + 8 h ..+7: eight of one page each,
+  // whose values (turned by the LDS read, eight tokens of a channel) have one scale.
   __device__ __forceinline__ static int token8(int row) { return (row & 16) | ((row & 4) << 1) | ((row & 8) >> 1) | (row & 3); }
   __device__ __forceinline__ void logits8(f32x16_t (&s)[1], const char* k, float scale, int lane) const {
     const int token = token8(lane & 31);
