@@ -604,14 +604,13 @@ struct Walk {
     const int from = ((step - of.first_step) << per_step_log2) + (eight >> shift);
     const float k_scale = from_lane(of.scale.x, from), v_scale = from_lane(of.scale.y, from);
     const int token = eight + (lane >> 3), slot = (lane & 7) * 2;
-    st16(k + k_place(token, slot), halves_of(make_uint2(key.x, key.y), k_scale));
-    st16(k + k_place(token, slot + 1), halves_of(make_uint2(key.z, key.w), k_scale));
-    // (two tokens' values go to LDS at a time: their even chunks and their odd ones, so that all banks are met)
-    const int odd = token & 1;
-    const uint2 a = odd ? make_uint2(value.z, value.w) : make_uint2(value.x, value.y);
-    const uint2 b = odd ? make_uint2(value.x, value.y) : make_uint2(value.z, value.w);
-    st16(v + v_place(token, slot + odd), halves_of(a, v_scale));
-    st16(v + v_place(token, slot + 1 - odd), halves_of(b, v_scale));
+    // (Eight lanes write at a time, to 32 banks: chunks that differ modulo 8.  32k tokens of 32 / 8 heads 8.50 -> 8.43 ms.)
+    const int odd = (lane >> 2) & 1;
+    auto half = [odd](uint4 x, bool second) { return odd != second ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y); };
+    st16(k + k_place(token, slot + odd), halves_of(half(key, false), k_scale));
+    st16(k + k_place(token, slot + 1 - odd), halves_of(half(key, true), k_scale));
+    st16(v + v_place(token, slot + odd), halves_of(half(value, false), v_scale));
+    st16(v + v_place(token, slot + 1 - odd), halves_of(half(value, true), v_scale));
   }
   // 16 bytes of the key and of the value of the step's place `four` + lane / 16 (`four`: a multiple of 4).  Returns whether
   // there is a token; if not, the value has to be zeroed when it has arrived: stale slots may hold anything, and
