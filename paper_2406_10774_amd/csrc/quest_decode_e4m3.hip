@@ -692,14 +692,14 @@ int most_shares(const quest_cache& c) {
 size_t share_bytes(const quest_cache& c) {
   return (size_t)2 * columns_of(c) * (many_heads(c) ? kGroupHeads : 1) * (kHeadDim + 2) * sizeof(float);
 }
-// (The counters' part is as long as that of an fp16 cache of the shape, so that one workspace serves both.)
+// (The counters' part is as long as that of an fp16 cache of the shape, also where these pages need none: one workspace serves
+// both, so nothing else may lie there.)
 size_t counter_bytes(const quest_cache& c) { return decode_counter_bytes(c); }
 
 }  // namespace
 
 size_t decode_e4m3_workspace_bytes(const quest_cache& c) {
-  const int shares = most_shares(c);
-  return shares > 0 ? counter_bytes(c) + shares * share_bytes(c) : 0;
+  return counter_bytes(c) + most_shares(c) * share_bytes(c);
 }
 
 bool decode_e4m3_fits_a_launch(const quest_cache& c) {
