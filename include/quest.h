@@ -136,10 +136,11 @@ typedef struct quest_cache {
  *                    of a (page, KV head), on 8 bytes
  * A number stands for its e4m3 value times its scale.  A scale is a power of two, 2^e:
  * the smallest e from -15 on with which the largest magnitude of the page's tokens is at
- * most 448 * 2^e; magnitudes above 61440 count as 61440.  So a stored number is off by at most 2^-4 of its
- * value or 2^-10 * 2^e, whichever is more, and is always an fp16 number: attention over these pages is
+ * most 448 * 2^e; magnitudes above 61440 count as 61440.  So a number is off by at most 2^-4 of its
+ * value or 2^-10 * 2^e, whichever is more, when it is stored, and is always an fp16 number: attention over these pages is
  * attention over an fp16 cache that holds what they stand for.  A page that gets more tokens keeps its
- * e or takes a larger one; what it holds is then rounded to that (exact, but for what becomes an e4m3 subnormal).
+ * e or takes a larger one; what it holds is then rounded to that (exact, but for what becomes an e4m3 subnormal).  Rounded
+ * once or more in this way a number is off by at most 2^-4 of its value or by less than 2^-9 * 2^e, a subnormal's whole step.
  * Metadata is of the keys in fp16, before they are rounded to 8 bits, so that the same
  * pages are selected as with the fp16 cache.
  * Calls on such a cache: quest_append_tokens and quest_rotate_append_tokens fill it (a decode step's
