@@ -398,6 +398,13 @@ __global__ __launch_bounds__((Shape<kS, k8, kRotate, kApart>::kWaves * kWave)) v
   }
 }
 
+// A launch has at most 2^32 - 1 threads.
+bool fits_a_launch(int64_t blocks, int waves, const char* who) {
+  if (blocks * waves * kWave <= UINT32_MAX) return true;
+  set_error("%s: %lld work-groups of %d waves do not fit a launch", who, (long long)blocks, waves);
+  return false;
+}
+
 int64_t waves_of_rows(const InsertArgs& a) { return ((int64_t)a.total + 3) / 4 * ((a.q_heads + kQHeads - 1) / kQHeads); }
 
 template <int kS, bool k8, bool kRotate, bool kApart = false>
@@ -405,7 +412,9 @@ int launch_insert_as(InsertArgs& a, const char* who, hipStream_t s) {
   using Of = Shape<kS, k8, kRotate, kApart>;
   a.insert_blocks = (a.pairs + Of::kPairs - 1) / Of::kPairs;
   const int64_t rows = kRotate && a.q != nullptr ? (waves_of_rows(a) + Of::kWaves - 1) / Of::kWaves : 0;
-  hipLaunchKernelGGL((insert_kernel<kS, k8, kRotate, kApart>), dim3((unsigned)(a.insert_blocks + rows)), dim3(Of::kWaves * kWave), 0, s, a);
+  const int64_t blocks = a.insert_blocks + rows;
+  if (!fits_a_launch(blocks, Of::kWaves, who)) return QUEST_ERR_SHAPE;
+  hipLaunchKernelGGL((insert_kernel<kS, k8, kRotate, kApart>), dim3((unsigned)blocks), dim3(Of::kWaves * kWave), 0, s, a);
   return check_launch(who);
 }
 template <int kS, bool kRotate>
@@ -482,6 +491,7 @@ int launch_rotate_rows(const quest_cache& c, const PackedTokens& p, const quest_
   a.q_out_stride = out_stride * 2;
   a.q_heads = heads;
   const int64_t blocks = (waves_of_rows(a) + kRowWaves - 1) / kRowWaves;
+  if (!fits_a_launch(blocks, kRowWaves, "quest_rotate_tokens")) return QUEST_ERR_SHAPE;
   hipLaunchKernelGGL(rotate_rows_kernel, dim3((unsigned)blocks), dim3(kRowWaves * kWave), 0, s, a);
   return check_launch("quest_rotate_tokens");
 }
