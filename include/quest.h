@@ -150,7 +150,8 @@ typedef struct quest_cache {
  * quest_decode_step_static, and a token's insertion by the single-token calls (k_pool_write != 0).
  * quest_sparse_decode and its like take any workspace, or NULL, without a refusal: a smaller one makes
  * fewer splits, slower.  Nothing is split where the batch times the KV heads (times parts of eight query
- * heads) is more than 512: a sequence much longer than the others is faster in a call of its own there.
+ * heads) is more than 512: a sequence much longer than the others is faster in a call of its own there (one of 60000 tokens among
+ * 64 of 2000, 8 KV heads, takes the whole call more than four times as long as over fp16 pages).
  * Lists are fastest as quest_topk leaves them, with no more entries than their sequence has pages. */
 
 /* Bytes of device workspace for quest_sparse_decode, quest_select_decode and

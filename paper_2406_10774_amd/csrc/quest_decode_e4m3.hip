@@ -681,7 +681,11 @@ int columns_of(const quest_cache& c) { return kv_heads(c) * attention_subs(c); }
 // 196 us and 201.)  Twice as many where there would be more than one on some units and one on others, or more than a fifth of the units
 // had none: ten sequences of 3000 to 30000 tokens of 32 heads 265 -> 204 us, 40 of 900 to 8000 of 32 / 8 heads 84 -> 69, one of 30000 of
 // 96 heads 119 -> 112. None where the (sequence, KV head) pairs are more than two for a compute unit: the units then even out what
-// sequences differ by (256 sequences of 10 to 2000 tokens and 8 KV heads 94 us, in shares 132; 64 sequences 56 and 56).
+// sequences differ by.  One each and in shares: 128 sequences of 10 to 2000 tokens and 8 KV heads 53 us and 73, 256 96 and 130, 65 of 500
+// to 8000 101 and 123, 80 127 and 130, 100 of 4000 147 and 149, 17 of 2000 to 4000 and 32 heads 89 and 90; but 128 of 500 to 8000 and 8 KV
+// heads 197 and 185, 24 of 300 to 6000 and 32 heads 119 and 98.  One long sequence is what this border is bad at: of 60000 tokens among 64 of 2000,
+// 32 / 8 heads, 549 and 98 (among 63, in shares, 73; fp16 pages 121), among 16, 32 heads, 419 and 144 (fp16 224), among 39 465 and
+// 179 (fp16 333).
 int most_shares(const quest_cache& c) {
   const int columns = columns_of(c);
   const int64_t tiles = ((int64_t)c.max_pages_per_seq * c.page_size / tile_tokens(c) + 1) * c.batch;

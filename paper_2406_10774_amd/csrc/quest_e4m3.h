@@ -1,9 +1,9 @@
 // Pages of 8 bits (QUEST_FLAG_E4M3_PAGES): e4m3 numbers, a power-of-two scale for each (page, KV head) of keys and of values.
 //
 // With e >= -15 the smallest step of a stored number, 2^-9 2^e, is a step of fp16, and with magnitudes up to 61440 = 240 * 2^8 none
-// passes the largest fp16 number: the conversions below, which multiply by the scale, are exact.  Measured against the
-// definition for all 65536 fp16 numbers (all 256 codes) and every e from -15 to 8: the hardware's rounding is to the nearest, ties
-// to even, subnormal results included.
+// passes the largest fp16 number: codes become fp16 numbers exactly.  The other way the hardware rounds to the nearest, ties to even,
+// subnormal results included: tested for every e from -15 to 8 and all finite fp16 numbers that a scale of 2^e holds, and with the codes
+// that come of them the way back.
 #pragma once
 
 #include "quest_common.h"

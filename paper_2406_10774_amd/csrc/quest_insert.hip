@@ -11,7 +11,8 @@
 // Bound by memory: every number is read once and written once.  The waves of a work-group have adjacent heads; queries follow in the
 // same launch, a wave having four tokens (whose table rows it then reads once) of kQHeads heads.  32749 tokens, pages of 16: 32 query / 8
 // KV heads turned into pages of 8 bits 143 us (763 MB, 5.3 TB/s; a large copy 5.3), 32 heads into pages of 8 bits as they are 154 us (5.4).
-// One token each of 16 sequences 4.5 us: lengths -> page -> data -> store.
+// One token each of 16 sequences 5.0 us, of 32 / 8 heads turned into fp16 pages; 1 to 5 of 8 KV heads into pages of 8 bits 5.1 to 5.3:
+// lengths -> page -> data -> store.  Rows alone (rotate_rows_kernel): 32768 of 32 heads 93 to 101 us (537 MB, 5.3 to 5.8 TB/s), 512 4.3.
 //
 // Without any length on the host: the pages of sequence b start at unit floor(cu[b] / S) + 2 b, which leaves
 // room for the floor((n + S - 2) / S) + 1 pages that n >= 1 tokens can touch.
@@ -202,13 +203,17 @@ __device__ __forceinline__ void round_part(char* block, const uint4 (&x)[kLoads]
 
 // How a page is shared out.  fp16 pages are one wave's, 16 tokens at a time.  Pages of 8 bits need all of their keys in registers, and
 // all of their values: one wave's too, or (kApart) 16 tokens a wave, and what belongs to the page goes through LDS: pages of 64 tokens,
-// turned, and pages of 32 and 64 that are no more than the SIMDs, where a wave's latency counts.  Of a turned page of 32 tokens that is
-// one wave's the keys are written before the values are asked for.
+// turned, and pages of 32 and 64 of which the launch has no more than the SIMDs, where a wave's latency counts.  Of a turned page of 32
+// tokens that is one wave's the keys are written before the values are asked for.
 //   21722 tokens of 32 / 32 heads, 32 channels turned (32k of 32 / 8 heads, 128), pages of 32: so 182 (148) us; values asked for with the
 //   keys 170 in the latter; apart 205 (157).  Pages of 64: apart 212 (163), as pages of 32 242 (203), in parts of 32 235 (174).  (Pages
 //   of 16: 172 (141).) Without rotation, 32k tokens of 32 heads in pages of 32 (64): one wave 153 (158), apart 176 (177). One token each
 //   of 16 sequences, 8 KV heads, pages of 64: one wave 6.7, apart 5.4; turned, pages of 32: 7.7 and 6.5.  1180 tokens of 32 heads (850
 //   pairs of page and head) pages of 64 17.2 and 14.3; (1440 pairs) pages of 32 12.3 and 14.1.
+//   Pairs are those that the launch has waves for, the most that there can be.  A step of one token a sequence has half as many or fewer,
+//   but so many waves all the same; replayed, one wave and apart: 16 sequences of 40 heads (1280 pairs, 640 of them with a token) pages of 64
+//   7.2 and 8.8, of 32 5.3 and 6.8, these turned 8.4 and 8.1; 65 of 8 heads 6.8 and 8.4, 5.3 and 6.7, 8.5 and 8.3; 40 of 8 heads (640)
+//   pages of 32 5.0 and 5.8; 800 tokens of 32 heads (864) 6.7 and 8.8.
 constexpr int kFewPairs = 1024;
 template <int kS, bool k8, bool kRotate, bool kApart>
 struct Shape {

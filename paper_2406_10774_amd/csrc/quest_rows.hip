@@ -585,6 +585,11 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const RowsArgs a, const
 //   little work, counted in 256 rows by 64 tokens: 3000 (400 tokens behind 600 of 32 / 8 heads: 22 us and 33; fifteen
 //   prompts of 250 to 500 tokens of 64 / 8 heads: 182 and 82), or 800 where the large one would split (60 tokens in ten
 //   sequences of 6000 of 64 / 8 heads 160 and 153, one of 150 behind 3000 59 and 40).
+//   Pages of 8 bits have the same borders, though the small kernel is faster on them and the large one is not.  The small and the large
+//   one there, us (in brackets with fp32 outputs): 64 rows at 65k tokens of 8 heads 51 and 62 (50, 80), 128 rows 81 and 64 to 67 (81, 86 to
+//   88), 256 145 and 87 (143, 118 to 121); 400 tokens behind 600 of 32 / 8 heads 21 and 38 (22, 44); 60 in ten sequences of 6000 of 64 / 8
+//   heads 240 and 167 to 180 (237, 221 to 235), one of 150 behind 3000 52 and 41 (53, 50), fifteen prompts of 400 186 and 92 (200, 121); 77
+//   in three of 2600, 40 heads, 49 and 68 (49, 92).
 struct Plan {
   int rows;                     // of a row tile: kFewRows or kSharedRows
   int row_tiles;                // of a KV head, at most
